@@ -411,6 +411,74 @@ SEER_API int seer_history_append(int32_t* tokens, const int32_t* seq_start, int3
                         int32_t n_seq, int64_t pool_tokens, int32_t pattern_lookup_max, int32_t* pattern,
                         int32_t* pattern_len, int32_t* status, void* hip_stream);
 
+/*
+ * Log probabilities of given tokens under softmax(logits / temperature), with the entropy of each row and
+ * its most probable alternatives: what a rollout records beside its tokens (the trainer's importance ratios and
+ * entropy terms start from it) and what scoring a batch of responses computes.  Two ways to use it:
+ *   a verify step   logits [B,T,V] as for seer_accept, accepted_path as written by it, tokens = the
+ *                   emitted_tokens of seer_kv_commit: entry (b,i) is the i-th token that request b emitted,
+ *                   judged by the logits of slot accepted_path[b][i]; rows that no token was emitted from
+ *                   are not read.
+ *   given rows      accepted_path NULL: entry (b,i) is judged by row (b,i).
+ *
+ * With z = logits / temperature: logsumexp = ln sum_v exp z_v, logprob = z[token] - logsumexp, entropy =
+ * -sum_v p_v ln p_v with p = softmax(z) and 0 ln 0 = 0.  Alternatives: the top_n largest logits in descending
+ * order, the lowest index first among equal ones (+0 == -0), with their log probabilities.  Sums and
+ * results are fp32 whatever the logits' type.
+ *
+ * Entries without a value -- a token outside [0, V) (padding), a path entry outside [0, T) -- give 0, 0, 0,
+ * and alternatives (0, -1).  Logits of -inf have probability 0 (a token's log probability is then -inf,
+ * an alternative's too); a row of nothing else has logsumexp -inf, log probabilities -inf, entropy 0, and as
+ * alternatives its first indices.  A NaN or +inf among a row's logits makes its log probabilities, entropy and logsumexp NaN
+ * and leaves open which alternatives it gets (their indices stay in range).
+ */
+#define SEER_F32 0
+#define SEER_BF16 1
+#define SEER_MAX_ALTERNATIVES 32
+#define SEER_LOGPROB_MAX_V (1 << 24)
+typedef struct seer_logprob_params {
+    int32_t B, T;              /* B*T entries; any T >= 1                                      */
+    int32_t V;                 /* logits of a row, 1 .. SEER_LOGPROB_MAX_V                     */
+    int64_t ld;                /* elements from one row of logits to the next, >= V            */
+    int32_t dtype;             /* of the logits (and their gradient): SEER_F32 or SEER_BF16    */
+    int32_t top_n;             /* alternatives per entry, 0 .. min(V, SEER_MAX_ALTERNATIVES)   */
+    float temperature;         /* positive and finite, as its reciprocal                       */
+} seer_logprob_params;
+
+/* Bytes of device scratch seer_token_logprobs needs; 0 on invalid params.  Host-only. */
+SEER_API size_t seer_token_logprobs_workspace(const seer_logprob_params* p);
+
+/*
+ *  logits         device [B*T rows of V, ld apart], aligned to its elements only
+ *  tokens         device [B,T] int32
+ *  accepted_path  device [B,T] int32 or NULL
+ *  logprob        device [B,T] fp32, written
+ *  entropy, logsumexp  device [B,T] fp32 or NULL, written
+ *  top_logprob    device [B,T,top_n] fp32, top_token device [B,T,top_n] int32, written; not looked at if top_n is 0
+ *  workspace      device, >= seer_token_logprobs_workspace(p) bytes, 16-byte aligned
+ * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_token_logprobs(const void* logits, const int32_t* tokens, const int32_t* accepted_path, const seer_logprob_params* p,
+                        float* logprob, float* entropy, float* logsumexp, float* top_logprob, int32_t* top_token,
+                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Gradient of sum_r grad_logprob[r] logprob[r] + grad_entropy[r] entropy[r] with respect to the logits, row by row
+ * (accepted_path NULL in the forward call):
+ *   grad[r][v] = ( grad_logprob[r] (1[v = token] - p_v) - grad_entropy[r] p_v (ln p_v + entropy[r]) ) / temperature.
+ * Rows without a token and rows without a finite logit get zeros.
+ *
+ *  grad_logits   device, rows of V elements of the logits' type grad_ld apart, every element of the B*T rows
+ *                written (rounded to nearest), nothing between the rows; the logits themselves may be given (in place, grad_ld = ld), no other overlap
+ *  logsumexp, entropy  device [B,T] fp32 as written by seer_token_logprobs; entropy NULL unless grad_entropy is given
+ *  grad_logprob, grad_entropy  device [B,T] fp32 or NULL (zeros)
+ *  p             top_n is not looked at beyond its range
+ * Asynchronous on hip_stream; no workspace.  Returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_token_logprobs_grad(void* grad_logits, int64_t grad_ld, const void* logits, const int32_t* tokens,
+                             const float* logsumexp, const float* entropy, const float* grad_logprob,
+                             const float* grad_entropy, const seer_logprob_params* p, void* hip_stream);
+
 /* Static text for a return code of either call (negative SEER_E*, or a
  * positive hipError_t). */
 SEER_API const char* seer_strerror(int code);

@@ -11,6 +11,7 @@ def __getattr__(name):
     if name in ("seer_verify_attention", "seer_accept", "seer_verify_attention_workspace",
                 "seer_accept_workspace", "seer_verify_attention_status", "seer_strerror", "load_library",
                 "seer_accept_sampled", "seer_kv_commit", "seer_mba_draft_lengths", "seer_draft", "seer_draft_workspace", "seer_history_append",
+                "seer_token_logprobs", "seer_token_logprobs_workspace", "seer_token_logprobs_grad", "SeerLogprobParams",
                 "SeerDraftParams",
                 "SeerAttnParams", "SeerError", "attn_params"):
         from . import binding

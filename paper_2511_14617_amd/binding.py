@@ -23,7 +23,7 @@ EXPORTS = ("seer_verify_attention_workspace", "seer_verify_attention_status_offs
            "seer_verify_attention_timed", "seer_verify_attention_kernel", "seer_verify_attention_shared_tiles_offset",
            "seer_accept_workspace", "seer_accept", "seer_accept_static", "seer_accept_sampled",
            "seer_kv_commit", "seer_mba_draft_lengths", "seer_acceptance_stats", "seer_acceptance_beta", "seer_draft_workspace", "seer_draft", "seer_history_append",
-           "seer_strerror")
+           "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad", "seer_strerror")
 
 
 class SeerAttnParams(ctypes.Structure):
@@ -40,6 +40,13 @@ class SeerDraftParams(ctypes.Structure):
                 ("pattern_lookup_max", ctypes.c_int32), ("vocab", ctypes.c_int32), ("min_confidence", ctypes.c_float)]
 
 
+class SeerLogprobParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("top_n", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+SEER_F32, SEER_BF16 = 0, 1
+SEER_MAX_ALTERNATIVES = 32
 SEER_ATTN_GENERAL_KERNEL = 1
 SEER_ATTN_FIXED_SPLIT = 2
 SEER_ATTN_STREAM_ONLY = 4
@@ -99,6 +106,12 @@ def load_library() -> ctypes.CDLL:
         lib.seer_draft.restype = ctypes.c_int
         lib.seer_history_append.argtypes = [vp] * 7 + [i32, i32, i32, ctypes.c_int64, i32, vp, vp, vp, vp]
         lib.seer_history_append.restype = ctypes.c_int
+        lib.seer_token_logprobs_workspace.argtypes = [ctypes.POINTER(SeerLogprobParams)]
+        lib.seer_token_logprobs_workspace.restype = sz
+        lib.seer_token_logprobs.argtypes = [vp] * 3 + [ctypes.POINTER(SeerLogprobParams)] + [vp] * 6 + [sz, vp]
+        lib.seer_token_logprobs.restype = ctypes.c_int
+        lib.seer_token_logprobs_grad.argtypes = [vp, ctypes.c_int64] + [vp] * 6 + [ctypes.POINTER(SeerLogprobParams), vp]
+        lib.seer_token_logprobs_grad.restype = ctypes.c_int
         lib.seer_strerror.argtypes = [ctypes.c_int]
         lib.seer_strerror.restype = ctypes.c_char_p
         _lib = lib
@@ -435,3 +448,81 @@ def seer_history_append(tokens: torch.Tensor, seq_start: torch.Tensor, seq_len: 
     _check(lib.seer_history_append(_ptr(tokens), _ptr(seq_start), _ptr(seq_len), _ptr(seq_capacity), _ptr(req_seq),
                                    _ptr(emitted_tokens), _ptr(n_emitted), B, T, n_seq, tokens.shape[0], p_max,
                                    _ptr(pattern), _ptr(pattern_len), _ptr(status), _stream_handle(stream)))
+
+
+def _logprob_rows(t: torch.Tensor, name: str) -> int:
+    """Elements from one row to the next of logits [B,T,V] or [N,V] (rows may be apart, their elements not)."""
+    ld = t.stride(-2) if t.shape[-2] > 1 else (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else max(t.stride(-2), t.shape[-1]))
+    if (not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16) or (t.shape[-1] > 1 and t.stride(-1) != 1)
+            or (t.dim() == 3 and t.shape[0] > 1 and t.stride(0) != t.shape[1] * ld)):
+        raise ValueError("%s: want device rows [B,T,V] or [N,V] of float32 or bfloat16 at one distance, got %s%s with strides %s on %s" %
+                         (name, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return ld
+
+
+def logprob_params(logits: torch.Tensor, temperature: float = 1.0, top_n: int = 0) -> SeerLogprobParams:
+    """logits [B,T,V], or [N,V] (B = N, T = 1)."""
+    if logits.dim() not in (2, 3):
+        raise ValueError("logits: want [B,T,V] or [N,V], got %s" % (tuple(logits.shape),))
+    ld = _logprob_rows(logits, "logits")
+    return SeerLogprobParams(logits.shape[0], logits.shape[1] if logits.dim() == 3 else 1, logits.shape[-1], ld,
+                             SEER_F32 if logits.dtype == torch.float32 else SEER_BF16, int(top_n), float(temperature))
+
+
+def seer_token_logprobs_workspace(params: SeerLogprobParams) -> int:
+    return int(load_library().seer_token_logprobs_workspace(ctypes.byref(params)))
+
+
+def seer_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, accepted_path: Optional[torch.Tensor] = None, *,
+                        temperature: float = 1.0, top_n: int = 0, out: Optional[Tuple[Optional[torch.Tensor], ...]] = None,
+                        workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """(logprob, entropy, logsumexp, top_logprob, top_token) of tokens under softmax(logits / temperature).
+    logits [B,T,V] or [N,V] float32 or bfloat16, rows at one distance; tokens int32 of the same leading shape, outside
+    [0, V) = no entry; accepted_path [B,T] int32 (entry (b,i) is judged by the logits of slot accepted_path[b,i]) or None.
+    The first three are float32 of the tokens' shape, the last two [..., top_n] float32 and int32, None where top_n is 0."""
+    lib = load_library()
+    p = logprob_params(logits, temperature, top_n)
+    lead = tuple(logits.shape[:-1])
+    _want(tokens, torch.int32, lead, "tokens")
+    if accepted_path is not None:
+        _want(accepted_path, torch.int32, lead, "accepted_path")
+    dev = logits.device
+    if out is None:
+        out = tuple(torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
+        out += (torch.empty((*lead, top_n), dtype=torch.float32, device=dev) if top_n > 0 else None,
+                torch.empty((*lead, top_n), dtype=torch.int32, device=dev) if top_n > 0 else None)
+    else:
+        for t, name in zip(out[:3], ("logprob", "entropy", "logsumexp")):
+            _want(t, torch.float32, lead, name)
+        if top_n > 0:
+            _want(out[3], torch.float32, (*lead, top_n), "top_logprob")
+            _want(out[4], torch.int32, (*lead, top_n), "top_token")
+    if workspace is None:
+        need = int(lib.seer_token_logprobs_workspace(ctypes.byref(p)))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    _check(lib.seer_token_logprobs(_ptr(logits), _ptr(tokens), _ptr(accepted_path), ctypes.byref(p), _ptr(out[0]), _ptr(out[1]),
+                                   _ptr(out[2]), _ptr(out[3]) if top_n > 0 else None, _ptr(out[4]) if top_n > 0 else None,
+                                   _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+    return out
+
+
+def seer_token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, logsumexp: torch.Tensor,
+                             grad_logprob: Optional[torch.Tensor], *, entropy: Optional[torch.Tensor] = None,
+                             grad_entropy: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                             out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of sum(grad_logprob * logprob) + sum(grad_entropy * entropy) with respect to the logits, in their type.
+    logsumexp and entropy as seer_token_logprobs gave them without a path; `out` may be the logits themselves."""
+    lib = load_library()
+    p = logprob_params(logits, temperature)
+    lead = tuple(logits.shape[:-1])
+    _want(tokens, torch.int32, lead, "tokens")
+    for t, name in ((logsumexp, "logsumexp"), (entropy, "entropy"), (grad_logprob, "grad_logprob"), (grad_entropy, "grad_entropy")):
+        if t is not None:
+            _want(t, torch.float32, lead, name)
+    if out is None:
+        out = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=logits.device)
+    elif out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out: want %s%s, got %s%s" % (logits.dtype, tuple(logits.shape), out.dtype, tuple(out.shape)))
+    _check(lib.seer_token_logprobs_grad(_ptr(out), _logprob_rows(out, "out"), _ptr(logits), _ptr(tokens), _ptr(logsumexp), _ptr(entropy),
+                                        _ptr(grad_logprob), _ptr(grad_entropy), ctypes.byref(p), _stream_handle(stream)))
+    return out

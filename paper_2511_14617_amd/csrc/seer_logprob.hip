@@ -1,0 +1,478 @@
+// seer_token_logprobs: log probability of given tokens under softmax(logits / temperature), the entropy of each row and
+// its most probable alternatives; seer_token_logprobs_grad: the gradient of log probability and entropy with respect to the logits.
+//
+// With z = x / tau, m = max z, l = sum exp(z - m):  logsumexp = m + ln l,  log p_y = z_y - logsumexp,
+// H = ln l - (sum exp(z - m) (z - m)) / l.  All three sums come from one pass over the row, and so do the alternatives.
+// Gradient: d(log p_y)/dx_v = (1[v = y] - p_v) / tau,  dH/dx_v = -p_v (ln p_v + H) / tau, with p_v = exp(z_v - logsumexp).
+//
+// What bounds it: HBM, one read of the logits (gradient: one read and one write).  Rows are cut into chunks so that a launch
+// fills the chip whatever rows * V is (logprob_scan); a second kernel joins the chunks of a row (logprob_join).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/seer_verify.h"
+#include "seer_device.h"
+#include "seer_tile.h"
+
+namespace seer {
+
+constexpr int kLpThreads = 256;
+constexpr int kLpWaves = kLpThreads / kWave;
+constexpr int kLpMaxCand = 1024;        // candidates for the alternatives that a workgroup keeps in LDS
+constexpr float kLowest = -1e4f;        // exp2 of this is 0: keeps 0 * -inf out of the entropy's sum
+constexpr float kLn2f = 0.693147181f;
+
+// Rows begin at any element (odd vocabularies, padded strides): vector loads and stores that assume the element's alignment only.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <int DTYPE>
+struct Elem;
+template <>
+struct Elem<SEER_F32> {
+    typedef float T;
+    static constexpr int kVec = 4;
+    typedef f32x4 Vec;
+    static __device__ __forceinline__ Vec load(const T* p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p)); }
+    static __device__ __forceinline__ Vec none() { return f32x4{kNegInf, kNegInf, kNegInf, kNegInf}; }
+    static __device__ __forceinline__ float get(const Vec& v, int i) { return v[i]; }
+    static __device__ __forceinline__ float one(const T* p) { return *p; }
+    static __device__ __forceinline__ void store(T* p, const float (&g)[kVec]) {
+        __builtin_nontemporal_store(f32x4{g[0], g[1], g[2], g[3]}, reinterpret_cast<f32x4_any*>(p));
+    }
+    static __device__ __forceinline__ void store_one(T* p, float g) { *p = g; }
+};
+template <>
+struct Elem<SEER_BF16> {
+    typedef uint16_t T;
+    static constexpr int kVec = 8;
+    typedef u32x4 Vec;
+    static __device__ __forceinline__ Vec load(const T* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p)); }
+    static __device__ __forceinline__ Vec none() { return u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u}; }
+    static __device__ __forceinline__ float get(const Vec& v, int i) { return i & 1 ? bf16hi_to_f32(v[i >> 1]) : bf16lo_to_f32(v[i >> 1]); }
+    static __device__ __forceinline__ float one(const T* p) { return bf16_to_f32(*p); }
+    static __device__ __forceinline__ void store(T* p, const float (&g)[kVec]) {
+        __builtin_nontemporal_store(u32x4{cvt_pk_bf16(g[0], g[1]), cvt_pk_bf16(g[2], g[3]), cvt_pk_bf16(g[4], g[5]), cvt_pk_bf16(g[6], g[7])},
+                                    reinterpret_cast<u32x4_any*>(p));
+    }
+    static __device__ __forceinline__ void store_one(T* p, float g) { *p = f32_to_bf16(g); }
+};
+
+struct LogprobArgs {
+    const void* logits;
+    const int32_t* tokens;
+    const int32_t* path;          // nullptr: output row = logits row
+    int64_t ld;
+    int T, V, n_chunks, top_n;
+    float inv_tau;
+    float* part;                  // [rows][n_chunks][3]: maximum of x, sum of exp2(d), sum of exp2(d) d, d = (x - maximum) log2(e) / tau
+    uint64_t* part_top;           // [rows][n_chunks][top_n] keys, descending, 0 = none
+    float* logprob;
+    float* entropy;               // may be nullptr, as the two below
+    float* logsumexp;
+    float* top_logprob;
+    int32_t* top_token;
+};
+
+// The logits row that output row r is about, -1: none (no token, or a place behind the accepted path).
+__device__ __forceinline__ int64_t logits_row(const LogprobArgs& a, int r, int& token) {
+    token = a.tokens[r];
+    if (token < 0 || token >= a.V) return -1;
+    if (!a.path) return r;
+    const int slot = a.path[r];
+    if (slot < 0 || slot >= a.T) return -1;
+    return static_cast<int64_t>(r / a.T) * a.T + slot;
+}
+
+// Whole numbers in the order of the floats they come from (-0 = +0; above 0 for every float but a NaN with its sign bit set).
+__device__ __forceinline__ uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
+constexpr uint32_t kOrderedNegInf = 0x007fffffu;
+// Keys of alternatives: larger value first, then lower index.
+__device__ __forceinline__ uint64_t alt_key(uint32_t value, int index) { return static_cast<uint64_t>(value) << 32 | static_cast<uint32_t>(~index); }
+
+// A value that at least n lanes' values reach (n <= 64): the n-th largest with its low 12 bits cleared, found bit by bit with one ballot each.
+__device__ __forceinline__ uint32_t wave_nth_largest(uint32_t v, int n) {
+    uint32_t at = 0;
+    for (int bit = 31; bit >= 12; --bit) {
+        const uint32_t probe = at | 1u << bit;
+        if (__popcll(__ballot(v >= probe)) >= n) at = probe;
+    }
+    return at;
+}
+
+template <int DTYPE, int kChunk, bool TOP>
+__global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
+    using E = Elem<DTYPE>;
+    constexpr int kVec = E::kVec, kIter = kChunk / (kLpThreads * kVec);
+    __shared__ float s_max[kLpWaves], s_sum[kLpWaves][2];
+    const int r = blockIdx.x / a.n_chunks, chunk = blockIdx.x - r * a.n_chunks;
+    int token;
+    const int64_t row = logits_row(a, r, token);
+    if (row < 0) return;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    const int begin = chunk * kChunk, end = min(a.V, begin + kChunk);
+    const typename E::T* base = static_cast<const typename E::T*>(a.logits) + row * a.ld;
+
+    // whole vectors, then one element of the last, incomplete one
+    typename E::Vec x[kIter];
+#pragma unroll
+    for (int it = 0; it < kIter; ++it) {
+        const int i = begin + (it * kLpThreads + tid) * kVec;
+        x[it] = i + kVec <= end ? E::load(base + i) : E::none();
+    }
+    const int rest = begin + (end - begin) / kVec * kVec + tid;
+    const float x_rest = rest < end ? E::one(base + rest) : kNegInf;
+
+    float top = x_rest;
+#pragma unroll
+    for (int it = 0; it < kIter; ++it)
+#pragma unroll
+        for (int c = 0; c < kVec; ++c) top = fmaxf(top, E::get(x[it], c));
+    const float wave_top = wave_max(top);
+    if (lane == 0) s_max[wave] = wave_top;
+    __syncthreads();
+    float m = s_max[0];
+#pragma unroll
+    for (int w = 1; w < kLpWaves; ++w) m = fmaxf(m, s_max[w]);
+
+    const float scale = a.inv_tau * kLog2e, ref = m == kNegInf ? 0.f : m;
+    float l = 0.f, s = 0.f;
+    auto add = [&](float v) __attribute__((always_inline)) {
+        const float d = (v - ref) * scale, e = fast_exp2(d);       // (a NaN reaches l, and through it every result of the row)
+        l += e;
+        s = fmaf(e, fmaxf(d, kLowest), s);
+    };
+#pragma unroll
+    for (int it = 0; it < kIter; ++it)
+#pragma unroll
+        for (int c = 0; c < kVec; ++c) add(E::get(x[it], c));
+    add(x_rest);
+    l = wave_sum(l), s = wave_sum(s);
+    if (lane == 0) s_sum[wave][0] = l, s_sum[wave][1] = s;
+
+    if constexpr (TOP) {
+        // Alternatives of the chunk: an element below the n-th largest of a wave's 64 lane maxima is none of the n first, so only
+        // the few that reach the largest such bound of the four waves are ranked, each by counting the ones before it.  Elements of
+        // -inf take no part (logprob_join puts them in where a row has too few others).
+        __shared__ uint32_t s_bound[kLpWaves];
+        __shared__ uint64_t s_cand[kLpMaxCand];
+        __shared__ int s_count;
+        const int n = a.top_n;
+        const uint32_t mine = ordered(top), bound_wave = wave_nth_largest(mine, n);
+        if (lane == 0) s_bound[wave] = bound_wave;
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        uint32_t bound = kOrderedNegInf + 1;
+#pragma unroll
+        for (int w = 0; w < kLpWaves; ++w) bound = max(bound, s_bound[w]);
+        auto offer = [&](float v, int index) __attribute__((always_inline)) {
+            const uint32_t k = ordered(v);
+            if (k >= bound) {
+                const int at = atomicAdd(&s_count, 1);
+                if (at < kLpMaxCand) s_cand[at] = alt_key(k, index);
+            }
+        };
+        if (__any(mine >= bound)) {
+#pragma unroll
+            for (int it = 0; it < kIter; ++it) {
+                float v = E::get(x[it], 0);
+#pragma unroll
+                for (int c = 1; c < kVec; ++c) v = fmaxf(v, E::get(x[it], c));
+                if (ordered(v) >= bound) {
+#pragma unroll
+                    for (int c = 0; c < kVec; ++c) offer(E::get(x[it], c), begin + (it * kLpThreads + tid) * kVec + c);
+                }
+            }
+            if (rest < end) offer(x_rest, rest);
+        }
+        __syncthreads();
+        const int count = s_count;
+        uint64_t* out = a.part_top + static_cast<size_t>(blockIdx.x) * n;
+        if (count <= kLpMaxCand) {
+            for (int i = tid; i < count; i += kLpThreads) {
+                const uint64_t k = s_cand[i];
+                int before = 0;
+                for (int j = 0; j < count; ++j) before += s_cand[j] > k ? 1 : 0;
+                if (before < n) out[before] = k;
+            }
+            for (int i = count + tid; i < n; i += kLpThreads) out[i] = 0;
+        } else {
+            // More equal values than the list holds (a flat row): one after the other, the largest key below the last one taken.
+            // (Read again: with the chunk kept in registers for this, the kernel took 167 of them.)
+            uint64_t last = ~0ull;
+            for (int k = 0; k < n; ++k) {
+                uint64_t best = 0;
+                for (int i = begin + tid; i < end; i += kLpThreads) {
+                    const float v = E::one(base + i);
+                    const uint64_t key = alt_key(ordered(v), i);
+                    if (v != kNegInf && key < last && key > best) best = key;
+                }
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), o, kWave)));
+                __syncthreads();
+                if (lane == 0) s_cand[wave] = best;
+                __syncthreads();
+#pragma unroll
+                for (int w = 0; w < kLpWaves; ++w) best = max(best, s_cand[w]);
+                if (tid == 0) out[k] = best;
+                last = best;
+            }
+        }
+    }
+    __syncthreads();
+    if (tid == 0) {
+        float* p = a.part + static_cast<size_t>(blockIdx.x) * 3;
+#pragma unroll
+        for (int w = 1; w < kLpWaves; ++w) l += s_sum[w][0], s += s_sum[w][1];
+        p[0] = m, p[1] = l, p[2] = s;
+    }
+}
+
+// One wave per row: the sums of its chunks brought to the row's maximum, in ascending order of the chunks per lane, and the
+// n first of their sorted lists, each lane holding the head of the lists lane, lane + 64, ...
+template <int DTYPE>
+__global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
+    extern __shared__ uint8_t s_taken[];                    // per chunk: keys taken from its list
+    const int r = blockIdx.x, lane = threadIdx.x, n = a.top_n;
+    int token;
+    const int64_t row = logits_row(a, r, token);
+    if (row < 0) {
+        if (lane == 0) {
+            a.logprob[r] = 0.f;
+            if (a.entropy) a.entropy[r] = 0.f;
+            if (a.logsumexp) a.logsumexp[r] = 0.f;
+        }
+        if (lane < n) a.top_logprob[static_cast<size_t>(r) * n + lane] = 0.f, a.top_token[static_cast<size_t>(r) * n + lane] = -1;
+        return;
+    }
+    const float x_token = Elem<DTYPE>::one(static_cast<const typename Elem<DTYPE>::T*>(a.logits) + row * a.ld + token);
+    const float* part = a.part + static_cast<size_t>(r) * a.n_chunks * 3;
+    float m = kNegInf;
+    for (int c = lane; c < a.n_chunks; c += kWave) m = fmaxf(m, part[c * 3]);
+    m = wave_max(m);
+    const float scale = a.inv_tau * kLog2e;
+    float l = 0.f, s = 0.f;
+    for (int c = lane; c < a.n_chunks; c += kWave) {
+        const float d = part[c * 3] == kNegInf ? kLowest : (part[c * 3] - m) * scale, w = fast_exp2(d);
+        l += w * part[c * 3 + 1];
+        s += w * fmaf(part[c * 3 + 1], fmaxf(d, kLowest), part[c * 3 + 2]);
+    }
+    l = wave_sum(l), s = wave_sum(s);
+    const float ln_l = logf(l);
+    const bool empty = m == kNegInf && l == 0.f;             // every logit is -inf
+    auto logp = [&](float x) __attribute__((always_inline)) { return x == kNegInf ? kNegInf : (x - m) * a.inv_tau - ln_l; };
+    if (lane == 0) {
+        a.logprob[r] = logp(x_token);
+        if (a.entropy) a.entropy[r] = empty ? 0.f : ln_l - kLn2f * (s / l);
+        if (a.logsumexp) a.logsumexp[r] = empty ? kNegInf : fmaf(m, a.inv_tau, ln_l);
+    }
+    if (n == 0) return;
+    const uint64_t* lists = a.part_top + static_cast<size_t>(r) * a.n_chunks * n;
+    for (int c = lane; c < a.n_chunks; c += kWave) s_taken[c] = 0;
+    uint64_t head = 0;
+    int from = 0;
+    auto find_head = [&]() __attribute__((always_inline)) {
+        head = 0;
+        for (int c = lane; c < a.n_chunks; c += kWave) {
+            const int at = s_taken[c];
+            const uint64_t k = at < n ? lists[static_cast<size_t>(c) * n + at] : 0;
+            if (k > head) head = k, from = c;
+        }
+    };
+    find_head();
+    uint64_t mine = 0;                                      // lane k: the k-th alternative
+    int got = 0;
+    for (; got < n; ++got) {
+        uint64_t best = head;
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), o, kWave)));
+        if (best == 0) break;
+        if (lane == got) mine = best;
+        if (head == best) {
+            ++s_taken[from];
+            find_head();
+        }
+    }
+    int index = static_cast<int>(~static_cast<uint32_t>(mine));
+    float x = unordered(static_cast<uint32_t>(mine >> 32));
+    // fewer than n finite logits: the lowest indices that are not among them, whose logits are -inf
+    for (int v = 0; got < n; ++v) {
+        if (__ballot(lane < got && index == v)) continue;
+        if (lane == got) index = v, x = kNegInf;
+        ++got;
+    }
+    if (lane < n) {
+        a.top_logprob[static_cast<size_t>(r) * n + lane] = logp(x);
+        a.top_token[static_cast<size_t>(r) * n + lane] = index;
+    }
+}
+
+struct LogprobGradArgs {
+    void* grad;
+    const void* logits;
+    const int32_t* tokens;
+    const float* logsumexp;
+    const float* entropy;         // nullptr iff grad_entropy is
+    const float* grad_logprob;
+    const float* grad_entropy;
+    int64_t ld, grad_ld;
+    int V, n_chunks;
+    float inv_tau;
+};
+
+// Every thread writes exactly the elements that it has read, so the gradient may take the logits' place.
+template <int DTYPE, int kChunk>
+__global__ __launch_bounds__(kLpThreads) void logprob_grad(LogprobGradArgs a) {
+    using E = Elem<DTYPE>;
+    constexpr int kVec = E::kVec, kIter = kChunk / (kLpThreads * kVec);
+    const int r = blockIdx.x / a.n_chunks, chunk = blockIdx.x - r * a.n_chunks, tid = threadIdx.x;
+    const int begin = chunk * kChunk, end = min(a.V, begin + kChunk);
+    const typename E::T* base = static_cast<const typename E::T*>(a.logits) + r * a.ld;
+    typename E::T* out = static_cast<typename E::T*>(a.grad) + r * a.grad_ld;
+    typename E::Vec x[kIter];
+#pragma unroll
+    for (int it = 0; it < kIter; ++it) {
+        const int i = begin + (it * kLpThreads + tid) * kVec;
+        x[it] = i + kVec <= end ? E::load(base + i) : E::none();
+    }
+    const int rest = begin + (end - begin) / kVec * kVec + tid;
+    const float x_rest = rest < end ? E::one(base + rest) : kNegInf;
+    const int token = a.tokens[r];
+    const float lse = a.logsumexp[r];
+    // no token, or a row without a finite logit: no gradient
+    const bool none = token < 0 || token >= a.V || lse == kNegInf;
+    const float g_lp = a.grad_logprob ? a.grad_logprob[r] * a.inv_tau : 0.f;
+    const float g_h = a.grad_entropy ? a.grad_entropy[r] * a.inv_tau : 0.f;
+    const float h = a.grad_entropy ? a.entropy[r] : 0.f;
+    const float c0 = -g_lp - g_h * h;
+    auto grad = [&](float v, int index) __attribute__((always_inline)) {
+        const float logp = fmaf(v, a.inv_tau, -lse), p = fast_exp2(logp * kLog2e);
+        const float g = p * fmaf(-g_h, fmaxf(logp, kLowest), c0) + (index == token ? g_lp : 0.f);
+        return none ? 0.f : g;
+    };
+#pragma unroll
+    for (int it = 0; it < kIter; ++it) {
+        const int i = begin + (it * kLpThreads + tid) * kVec;
+        if (i + kVec <= end) {
+            float g[kVec];
+#pragma unroll
+            for (int c = 0; c < kVec; ++c) g[c] = grad(E::get(x[it], c), i + c);
+            E::store(out + i, g);
+        }
+    }
+    if (rest < end) E::store_one(out + rest, grad(x_rest, rest));
+}
+
+// Elements of a workgroup's chunk.
+constexpr int kLpChunkLarge = 16384, kLpChunkSmall = 4096;
+inline int lp_chunk(const seer_logprob_params& p) {
+    const int64_t rows = static_cast<int64_t>(p.B) * p.T;
+    return rows * ((p.V + kLpChunkLarge - 1) / kLpChunkLarge) >= 2048 ? kLpChunkLarge : kLpChunkSmall;
+}
+inline int lp_num_chunks(const seer_logprob_params& p) { return (p.V + lp_chunk(p) - 1) / lp_chunk(p); }
+inline size_t lp_sums_bytes(const seer_logprob_params& p) {
+    return (static_cast<size_t>(p.B) * p.T * lp_num_chunks(p) * 3 * sizeof(float) + 255) / 256 * 256;
+}
+
+static int check_logprob_params(const seer_logprob_params* p) {
+    if (!p) return SEER_EINVAL;
+    if (p->B < 0 || p->V < 1) return SEER_EINVAL;
+    if (!(p->temperature > 0.f) || p->temperature > 3.0e38f) return SEER_EINVAL;
+    if (p->T < 1 || p->top_n < 0 || p->top_n > SEER_MAX_ALTERNATIVES || p->top_n > p->V || p->ld < p->V) return SEER_ESHAPE;
+    if (p->dtype != SEER_F32 && p->dtype != SEER_BF16) return SEER_EUNSUPPORTED;
+    if (p->V > SEER_LOGPROB_MAX_V) return SEER_EUNSUPPORTED;
+    if (static_cast<int64_t>(p->B) * p->T > 0x7fffffffLL || (p->B > 0 && static_cast<int64_t>(p->B) * p->T * lp_num_chunks(*p) > 0x7fffffffLL)) return SEER_ESHAPE;
+    if (!(1.0f / p->temperature < 2.0e38f)) return SEER_EINVAL;          // (its reciprocal has to be finite too, also times log2 e)
+    return SEER_OK;
+}
+
+static bool lp_misaligned(const void* ptr, uintptr_t a) { return reinterpret_cast<uintptr_t>(ptr) % a != 0; }
+
+}  // namespace seer
+
+extern "C" size_t seer_token_logprobs_workspace(const seer_logprob_params* p) {
+    if (seer::check_logprob_params(p) != SEER_OK || p->B == 0) return 0;
+    const size_t keys = static_cast<size_t>(p->B) * p->T * seer::lp_num_chunks(*p) * p->top_n * sizeof(uint64_t);
+    return seer::lp_sums_bytes(*p) + (keys + 255) / 256 * 256;
+}
+
+extern "C" int seer_token_logprobs(const void* logits, const int32_t* tokens, const int32_t* accepted_path, const seer_logprob_params* p,
+                                   float* logprob, float* entropy, float* logsumexp, float* top_logprob, int32_t* top_token,
+                                   void* workspace, size_t workspace_bytes, void* hip_stream) {
+    const int rc = seer::check_logprob_params(p);
+    if (rc != SEER_OK) return rc;
+    if (p->B == 0) return SEER_OK;
+    if (!logits || !tokens || !logprob || (p->top_n > 0 && (!top_logprob || !top_token))) return SEER_EINVAL;
+    if (!workspace || workspace_bytes < seer_token_logprobs_workspace(p)) return SEER_EWORKSPACE;
+    const bool f32 = p->dtype == SEER_F32;
+    if (seer::lp_misaligned(logits, f32 ? 4 : 2) || seer::lp_misaligned(workspace, 16) || seer::lp_misaligned(tokens, 4) || seer::lp_misaligned(accepted_path, 4) ||
+        seer::lp_misaligned(logprob, 4) || seer::lp_misaligned(entropy, 4) || seer::lp_misaligned(logsumexp, 4) || seer::lp_misaligned(top_logprob, 4) ||
+        seer::lp_misaligned(top_token, 4))
+        return SEER_EALIGN;
+    seer::LogprobArgs a{};
+    a.logits = logits, a.tokens = tokens, a.path = accepted_path;
+    a.ld = p->ld, a.T = p->T, a.V = p->V, a.n_chunks = seer::lp_num_chunks(*p), a.top_n = p->top_n;
+    a.inv_tau = 1.0f / p->temperature;
+    a.part = static_cast<float*>(workspace);
+    a.part_top = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + seer::lp_sums_bytes(*p));
+    a.logprob = logprob, a.entropy = entropy, a.logsumexp = logsumexp, a.top_logprob = top_logprob, a.top_token = top_token;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const unsigned rows = static_cast<unsigned>(p->B) * static_cast<unsigned>(p->T);
+    const dim3 grid(rows * static_cast<unsigned>(a.n_chunks)), block(seer::kLpThreads);
+    const int chunk = seer::lp_chunk(*p);
+    const bool top = p->top_n > 0;
+#define SEER_LP_SCAN(DTYPE, CHUNK, TOP) \
+    if (p->dtype == DTYPE && chunk == CHUNK && top == TOP) hipLaunchKernelGGL((seer::logprob_scan<DTYPE, CHUNK, TOP>), grid, block, 0, stream, a);
+    SEER_LP_SCAN(SEER_F32, seer::kLpChunkLarge, true)
+    SEER_LP_SCAN(SEER_F32, seer::kLpChunkLarge, false)
+    SEER_LP_SCAN(SEER_F32, seer::kLpChunkSmall, true)
+    SEER_LP_SCAN(SEER_F32, seer::kLpChunkSmall, false)
+    SEER_LP_SCAN(SEER_BF16, seer::kLpChunkLarge, true)
+    SEER_LP_SCAN(SEER_BF16, seer::kLpChunkLarge, false)
+    SEER_LP_SCAN(SEER_BF16, seer::kLpChunkSmall, true)
+    SEER_LP_SCAN(SEER_BF16, seer::kLpChunkSmall, false)
+#undef SEER_LP_SCAN
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return static_cast<int>(err);
+    const unsigned lds = top ? static_cast<unsigned>(a.n_chunks) : 0u;
+    if (f32) hipLaunchKernelGGL((seer::logprob_join<SEER_F32>), dim3(rows), dim3(seer::kWave), lds, stream, a);
+    else hipLaunchKernelGGL((seer::logprob_join<SEER_BF16>), dim3(rows), dim3(seer::kWave), lds, stream, a);
+    err = hipGetLastError();
+    return err == hipSuccess ? SEER_OK : static_cast<int>(err);
+}
+
+extern "C" int seer_token_logprobs_grad(void* grad_logits, int64_t grad_ld, const void* logits, const int32_t* tokens, const float* logsumexp,
+                                        const float* entropy, const float* grad_logprob, const float* grad_entropy,
+                                        const seer_logprob_params* p, void* hip_stream) {
+    const int rc = seer::check_logprob_params(p);
+    if (rc != SEER_OK) return rc;
+    if (grad_ld < p->V) return SEER_ESHAPE;
+    if (p->B == 0) return SEER_OK;
+    if (!grad_logits || !logits || !tokens || !logsumexp || (grad_entropy && !entropy)) return SEER_EINVAL;
+    if (grad_logits == logits && grad_ld != p->ld) return SEER_EINVAL;        // in place: the same rows
+    const bool f32 = p->dtype == SEER_F32;
+    if (seer::lp_misaligned(logits, f32 ? 4 : 2) || seer::lp_misaligned(grad_logits, f32 ? 4 : 2) || seer::lp_misaligned(tokens, 4) ||
+        seer::lp_misaligned(logsumexp, 4) || seer::lp_misaligned(entropy, 4) || seer::lp_misaligned(grad_logprob, 4) || seer::lp_misaligned(grad_entropy, 4))
+        return SEER_EALIGN;
+    seer::LogprobGradArgs a{};
+    a.grad = grad_logits, a.logits = logits, a.tokens = tokens, a.logsumexp = logsumexp, a.entropy = entropy;
+    a.grad_logprob = grad_logprob, a.grad_entropy = grad_entropy;
+    a.ld = p->ld, a.grad_ld = grad_ld, a.V = p->V, a.n_chunks = seer::lp_num_chunks(*p);
+    a.inv_tau = 1.0f / p->temperature;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const dim3 grid(static_cast<unsigned>(p->B) * static_cast<unsigned>(p->T) * static_cast<unsigned>(a.n_chunks)), block(seer::kLpThreads);
+    const int chunk = seer::lp_chunk(*p);
+#define SEER_LP_GRAD(DTYPE, CHUNK) \
+    if (p->dtype == DTYPE && chunk == CHUNK) hipLaunchKernelGGL((seer::logprob_grad<DTYPE, CHUNK>), grid, block, 0, stream, a);
+    SEER_LP_GRAD(SEER_F32, seer::kLpChunkLarge)
+    SEER_LP_GRAD(SEER_F32, seer::kLpChunkSmall)
+    SEER_LP_GRAD(SEER_BF16, seer::kLpChunkLarge)
+    SEER_LP_GRAD(SEER_BF16, seer::kLpChunkSmall)
+#undef SEER_LP_GRAD
+    const hipError_t err = hipGetLastError();
+    return err == hipSuccess ? SEER_OK : static_cast<int>(err);
+}

@@ -1,0 +1,100 @@
+"""Host-side checks, without a GPU, of the calls that record log probabilities and keep the cache small: parameter structs,
+workspace sizes, and bad arguments turned into SEER_E* codes before anything is launched."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE = 0x1000       # never dereferenced: all of these calls fail on the host
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2511_14617_amd import binding, build
+    if not os.path.exists(binding.LIB_PATH):
+        build.build_library()
+    return binding.load_library()
+
+
+def struct_fields(name):
+    header = open(os.path.join(ROOT, "include", "seer_verify.h")).read()
+    body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (name, name), header, flags=re.S).group(1)
+    fields = []
+    for decl in re.sub(r"/\*.*?\*/", "", body, flags=re.S).split(";"):
+        if decl.strip():
+            ctype, names = decl.strip().split(None, 1)
+            fields += [(n.strip(), {"int32_t": ctypes.c_int32, "int64_t": ctypes.c_int64, "float": ctypes.c_float}[ctype]) for n in names.split(",")]
+    return fields
+
+
+def lp(**kw):
+    from paper_2511_14617_amd.binding import SeerLogprobParams
+    base = dict(B=4, T=5, V=1000, ld=1000, dtype=0, top_n=3, temperature=1.0)
+    base.update(kw)
+    return SeerLogprobParams(**base)
+
+
+def test_logprob_struct_matches_header():
+    from paper_2511_14617_amd.binding import SeerLogprobParams
+    assert struct_fields("seer_logprob_params") == list(SeerLogprobParams._fields_)
+
+
+def test_logprob_workspace(lib):
+    from paper_2511_14617_amd import binding as b
+    size = b.seer_token_logprobs_workspace
+    assert size(lp()) > 0 and size(lp()) % 256 == 0
+    assert size(lp(V=152064, ld=152064)) > size(lp()) and size(lp(top_n=32)) > size(lp(top_n=0)) > 0
+    for bad in (lp(B=0), lp(B=-1), lp(T=0), lp(V=0), lp(ld=999), lp(top_n=33), lp(top_n=-1), lp(V=2, ld=2), lp(dtype=2), lp(temperature=0.0)):
+        assert size(bad) == 0
+    assert lib.seer_token_logprobs_workspace(None) == 0
+
+
+def test_logprob_argument_errors_before_any_launch(lib):
+    from paper_2511_14617_amd import binding as b
+
+    def run(p, logits=FAKE, tokens=FAKE, path=None, out=FAKE, ent=None, top=FAKE, topi=FAKE, ws=0x10000, ws_bytes=1 << 40):
+        return lib.seer_token_logprobs(logits, tokens, path, None if p is None else ctypes.byref(p), out, ent, None, top, topi, ws, ws_bytes, None)
+
+    assert run(None) == b.SEER_EINVAL
+    assert run(lp(B=-1)) == b.SEER_EINVAL
+    assert run(lp(V=0)) == b.SEER_EINVAL
+    for t in (0.0, -1.0, float("nan"), float("inf"), 1e-39):
+        assert run(lp(temperature=t)) == b.SEER_EINVAL, t
+    for bad in (dict(T=0), dict(ld=999), dict(top_n=-1), dict(top_n=33), dict(V=2, ld=2), dict(B=1 << 20, T=1 << 12),
+                dict(B=1 << 30, T=1, V=1 << 20, ld=1 << 20)):
+        assert run(lp(**bad)) == b.SEER_ESHAPE, bad
+    assert run(lp(dtype=2)) == b.SEER_EUNSUPPORTED
+    assert run(lp(V=(1 << 24) + 1, ld=1 << 25)) == b.SEER_EUNSUPPORTED
+    assert run(lp(), logits=None) == b.SEER_EINVAL
+    assert run(lp(), tokens=None) == b.SEER_EINVAL
+    assert run(lp(), out=None) == b.SEER_EINVAL
+    assert run(lp(), top=None) == b.SEER_EINVAL
+    assert run(lp(), topi=None) == b.SEER_EINVAL
+    assert run(lp(), ws=None) == b.SEER_EWORKSPACE
+    assert run(lp(), ws_bytes=b.seer_token_logprobs_workspace(lp()) - 1) == b.SEER_EWORKSPACE
+    assert run(lp(), logits=FAKE + 2) == b.SEER_EALIGN
+    assert run(lp(dtype=1), logits=FAKE + 1) == b.SEER_EALIGN
+    assert run(lp(), ws=0x10004) == b.SEER_EALIGN
+    assert run(lp(), ent=FAKE + 2) == b.SEER_EALIGN
+    assert run(lp(B=0)) == b.SEER_OK
+
+
+def test_logprob_grad_argument_errors_before_any_launch(lib):
+    from paper_2511_14617_amd import binding as b
+
+    def run(p, grad=2 * FAKE, ld=1000, logits=FAKE, tokens=FAKE, lse=FAKE, ent=None, g=FAKE, gh=None):
+        return lib.seer_token_logprobs_grad(grad, ld, logits, tokens, lse, ent, g, gh, None if p is None else ctypes.byref(p), None)
+
+    assert run(None) == b.SEER_EINVAL
+    assert run(lp(), ld=999) == b.SEER_ESHAPE
+    assert run(lp(), grad=None) == b.SEER_EINVAL
+    assert run(lp(), lse=None) == b.SEER_EINVAL
+    assert run(lp(), tokens=None) == b.SEER_EINVAL
+    assert run(lp(), gh=FAKE) == b.SEER_EINVAL                    # the entropy's gradient needs the entropy
+    assert run(lp(), grad=FAKE, ld=1001) == b.SEER_EINVAL         # in place with other rows
+    assert run(lp(), grad=FAKE + 2) == b.SEER_EALIGN
+    assert run(lp(), g=FAKE + 1) == b.SEER_EALIGN
+    assert run(lp(temperature=-1.0)) == b.SEER_EINVAL
+    assert run(lp(B=0)) == b.SEER_OK
