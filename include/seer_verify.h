@@ -479,6 +479,41 @@ SEER_API int seer_token_logprobs_grad(void* grad_logits, int64_t grad_ld, const 
                              const float* logsumexp, const float* entropy, const float* grad_logprob,
                              const float* grad_entropy, const seer_logprob_params* p, void* hip_stream);
 
+/* Bytes of device scratch seer_kv_weights needs; 0 on invalid params.  Host-only. */
+SEER_API size_t seer_kv_weights_workspace(const seer_attn_params* p);
+
+/*
+ * Attention weight of every cached position, summed over the steps of a request: what a cache of bounded size
+ * (seer_kv_evict) keeps positions by.  Called once per layer after seer_kv_commit, with the step's queries of that layer.
+ *
+ * Request b holds n = ctx_len[b] positions, the last R of them from this step: R = accepted_len[b] + 1 rows, the i-th
+ * being slot accepted_path[b][i] (its query q[b][accepted_path[b][i]]), or, with accepted_len and accepted_path NULL,
+ * all T slots in order (plain decoding: T = 1).  Row i sees positions 0 .. n - R + i, as it did in the verify
+ * pass.  For KV head h and every position j < n
+ *   weights[b][h][j] = (j < n - R ? decay * weights[b][h][j] : 0) + sum over i, over the heads of group h, of
+ *                      softmax_j(scale * q.K[j]) over what row i sees.
+ * So the entries of positions from before the step have to be there (zeros for a request's first
+ * call), those of the step's own need not; entries from n on are left as they are.  Scores, denominators and sums are
+ * fp32; the result does not depend on anything but the arguments.
+ *
+ *  weights        device [B, Hkv, max_pages_per_seq * page_size] fp32, read and written
+ *  q              device [B,T,Hq,Dqk] bf16
+ *  k_pages        device [num_pages,Hkv,page_size,Dqk] bf16
+ *  block_table, ctx_len  as for seer_verify_attention, ctx_len as seer_kv_commit left it
+ *  accepted_len, accepted_path  device, as written by seer_accept; both NULL or neither
+ *  decay          0 .. 1; 1 = plain sums
+ *  p              B, T, Hq, Hkv, Dqk (64, 128, 192, 256 or 576), page_size (any), num_pages, max_pages_per_seq, scale are used
+ *  status         device [1] int32 or NULL; bits are OR-ed in: 1 = a ctx_len below R or beyond the block table, or an accepted_len
+ *                 out of range, 4 = accepted_path malformed (such requests are left untouched), 2 = a page id outside the pool
+ *                 (it is clamped into the pool).  The caller clears it.
+ *  workspace      device, >= seer_kv_weights_workspace(p) bytes, 256-byte aligned
+ * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_kv_weights(float* weights, const void* q, const void* k_pages, const int32_t* block_table,
+                    const int32_t* ctx_len, const int32_t* accepted_len, const int32_t* accepted_path, float decay,
+                    const seer_attn_params* p, int32_t* status, void* workspace, size_t workspace_bytes,
+                    void* hip_stream);
+
 /* Static text for a return code of either call (negative SEER_E*, or a
  * positive hipError_t). */
 SEER_API const char* seer_strerror(int code);

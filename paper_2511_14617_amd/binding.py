@@ -23,7 +23,8 @@ EXPORTS = ("seer_verify_attention_workspace", "seer_verify_attention_status_offs
            "seer_verify_attention_timed", "seer_verify_attention_kernel", "seer_verify_attention_shared_tiles_offset",
            "seer_accept_workspace", "seer_accept", "seer_accept_static", "seer_accept_sampled",
            "seer_kv_commit", "seer_mba_draft_lengths", "seer_acceptance_stats", "seer_acceptance_beta", "seer_draft_workspace", "seer_draft", "seer_history_append",
-           "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad", "seer_strerror")
+           "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad",
+           "seer_kv_weights_workspace", "seer_kv_weights", "seer_strerror")
 
 
 class SeerAttnParams(ctypes.Structure):
@@ -112,6 +113,10 @@ def load_library() -> ctypes.CDLL:
         lib.seer_token_logprobs.restype = ctypes.c_int
         lib.seer_token_logprobs_grad.argtypes = [vp, ctypes.c_int64] + [vp] * 6 + [ctypes.POINTER(SeerLogprobParams), vp]
         lib.seer_token_logprobs_grad.restype = ctypes.c_int
+        lib.seer_kv_weights_workspace.argtypes = [ctypes.POINTER(SeerAttnParams)]
+        lib.seer_kv_weights_workspace.restype = sz
+        lib.seer_kv_weights.argtypes = [vp] * 7 + [ctypes.c_float, ctypes.POINTER(SeerAttnParams), vp, vp, sz, vp]
+        lib.seer_kv_weights.restype = ctypes.c_int
         lib.seer_strerror.argtypes = [ctypes.c_int]
         lib.seer_strerror.restype = ctypes.c_char_p
         _lib = lib
@@ -526,3 +531,38 @@ def seer_token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, logsume
     _check(lib.seer_token_logprobs_grad(_ptr(out), _logprob_rows(out, "out"), _ptr(logits), _ptr(tokens), _ptr(logsumexp), _ptr(entropy),
                                         _ptr(grad_logprob), _ptr(grad_entropy), ctypes.byref(p), _stream_handle(stream)))
     return out
+
+
+def seer_kv_weights_workspace(params: SeerAttnParams) -> int:
+    return int(load_library().seer_kv_weights_workspace(ctypes.byref(params)))
+
+
+def seer_kv_weights(weights: torch.Tensor, q: torch.Tensor, k_pages: torch.Tensor, block_table: torch.Tensor,
+                    ctx_len: torch.Tensor, accepted_len: Optional[torch.Tensor], accepted_path: Optional[torch.Tensor],
+                    scale: float, *, decay: float = 1.0, status: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Adds the attention weights of a step's accepted tokens to weights [B, Hkv, max_pages * page] float32, in place.
+    q [B,T,Hq,Dqk] bf16; k_pages [num_pages,Hkv,page,Dqk] bf16; ctx_len [B] int32 as seer_kv_commit left it;
+    accepted_len [B] and accepted_path [B,T] int32 as seer_accept wrote them, or both None (all T slots)."""
+    lib = load_library()
+    if q.dim() != 4 or k_pages.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("want q [B,T,Hq,Dqk], k_pages [num_pages,Hkv,page,Dqk] and block_table [B,max_pages]")
+    p = attn_params(q, k_pages, None, block_table, scale, Dv=q.shape[3])
+    _want(q, torch.bfloat16, (p.B, p.T, p.Hq, p.Dqk), "q")
+    _want(k_pages, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size, p.Dqk), "k_pages")
+    _want(block_table, torch.int32, (p.B, p.max_pages_per_seq), "block_table")
+    _want(ctx_len, torch.int32, (p.B,), "ctx_len")
+    _want(weights, torch.float32, (p.B, p.Hkv, p.max_pages_per_seq * p.page_size), "weights")
+    if accepted_len is not None:
+        _want(accepted_len, torch.int32, (p.B,), "accepted_len")
+    if accepted_path is not None:
+        _want(accepted_path, torch.int32, (p.B, p.T), "accepted_path")
+    if status is not None:
+        _want(status, torch.int32, (1,), "status")
+    if workspace is None:
+        need = int(lib.seer_kv_weights_workspace(ctypes.byref(p)))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    _check(lib.seer_kv_weights(_ptr(weights), _ptr(q), _ptr(k_pages), _ptr(block_table), _ptr(ctx_len), _ptr(accepted_len),
+                               _ptr(accepted_path), float(decay), ctypes.byref(p), _ptr(status), _ptr(workspace),
+                               workspace.numel(), _stream_handle(stream)))
+    return weights

@@ -98,3 +98,40 @@ def test_logprob_grad_argument_errors_before_any_launch(lib):
     assert run(lp(), g=FAKE + 1) == b.SEER_EALIGN
     assert run(lp(temperature=-1.0)) == b.SEER_EINVAL
     assert run(lp(B=0)) == b.SEER_OK
+
+
+def attn(**kw):
+    from paper_2511_14617_amd.binding import SeerAttnParams
+    base = dict(B=4, T=5, Hq=8, Hkv=2, Dqk=128, Dv=128, page_size=16, num_pages=100, max_pages_per_seq=32, max_splits=0,
+                kv_shared_latent=0, flags=0, scale=0.088)
+    base.update(kw)
+    return SeerAttnParams(**base)
+
+
+def test_kv_weights_workspace_and_argument_errors_before_any_launch(lib):
+    from paper_2511_14617_amd import binding as b
+    size = b.seer_kv_weights_workspace
+    assert size(attn()) > 0 and size(attn()) % 256 == 0
+    assert size(attn(Dqk=576, Hq=128, Hkv=1, page_size=64)) > 0
+
+    def run(p, w=FAKE, q=FAKE, k=FAKE, table=FAKE, ctx=FAKE, alen=FAKE, path=FAKE, decay=1.0, status=None, ws=0x10000, ws_bytes=1 << 40):
+        return lib.seer_kv_weights(w, q, k, table, ctx, alen, path, decay, None if p is None else ctypes.byref(p), status, ws, ws_bytes, None)
+
+    for bad, code in ((dict(B=-1), b.SEER_EINVAL), (dict(num_pages=0), b.SEER_EINVAL), (dict(scale=0.0), b.SEER_EINVAL), (dict(scale=float("nan")), b.SEER_EINVAL),
+                      (dict(scale=float("inf")), b.SEER_EINVAL), (dict(T=0), b.SEER_ESHAPE), (dict(T=65), b.SEER_ESHAPE), (dict(Hq=7), b.SEER_ESHAPE),
+                      (dict(Dqk=100), b.SEER_EUNSUPPORTED), (dict(page_size=0), b.SEER_EINVAL), (dict(max_pages_per_seq=1 << 30), b.SEER_ESHAPE),
+                      (dict(B=1 << 20, max_pages_per_seq=1 << 16), b.SEER_ESHAPE), (dict(num_pages=1 << 30), b.SEER_ESHAPE)):
+        assert run(attn(**bad)) == code, bad
+        assert size(attn(**bad)) == 0, bad
+    assert run(None) == b.SEER_EINVAL
+    for d in (-0.1, 1.5, float("nan")):
+        assert run(attn(), decay=d) == b.SEER_EINVAL
+    for name in ("w", "q", "k", "table", "ctx", "alen", "path"):
+        assert run(attn(), **{name: None}) == b.SEER_EINVAL, name       # (accepted_len and accepted_path come together)
+    assert run(attn(), ws=None) == b.SEER_EWORKSPACE
+    assert run(attn(), ws_bytes=size(attn()) - 1) == b.SEER_EWORKSPACE
+    assert run(attn(), ws=0x10010) == b.SEER_EALIGN
+    assert run(attn(), q=FAKE + 2) == b.SEER_EALIGN
+    assert run(attn(), w=FAKE + 2) == b.SEER_EALIGN
+    assert run(attn(), status=FAKE + 1) == b.SEER_EALIGN
+    assert run(attn(B=0)) == b.SEER_OK
