@@ -514,6 +514,53 @@ SEER_API int seer_kv_weights(float* weights, const void* q, const void* k_pages,
                     const seer_attn_params* p, int32_t* status, void* workspace, size_t workspace_bytes,
                     void* hip_stream);
 
+/*
+ * A cache of bounded size: requests that hold more than `limit` positions are cut to `budget` of them.  Every KV head
+ * chooses for itself: the first positions (a common prompt, for instance) and the newest keep_last always stay; of those
+ * between, the budget - first - keep_last with the largest sums in `weights`, the lower position first among equal sums (a NaN is
+ * below every other sum).  The verify pass over the cut cache is exact for the positions it holds; what a request
+ * samples from then on is the policy with that cache, whose log probabilities seer_token_logprobs records.
+ *
+ * Where the kept positions go (queries see all of them, so their order matters to nobody; keys carry their rotation):
+ * with E = budget - keep_last, kept positions below E stay where they are, the others fill the free slots below
+ * E, both in ascending order; the newest keep_last become E .. budget - 1, in order.  new_ctx_len[b] = budget.  Rows from budget on keep
+ * stale contents, as do pages that the request no longer needs (they are the caller's to reuse).  Requests of at
+ * most `limit` positions are left as they are, with new_ctx_len[b] = ctx_len[b].
+ * Pages that hold positions from the always-kept first ones on must not be shared between requests.
+ */
+typedef struct seer_evict_params {
+    int32_t limit;             /* requests with more positions are cut                                 */
+    int32_t budget;            /* positions they keep, 1 .. limit                                       */
+    int32_t keep_first;        /* positions from the start that stay (keep_first[b] instead, if given)  */
+    int32_t keep_last;         /* newest positions that stay; keep_first + keep_last <= budget          */
+} seer_evict_params;
+
+/* Bytes of device scratch seer_kv_evict needs; 0 on invalid params.  Host-only. */
+SEER_API size_t seer_kv_evict_workspace(const seer_attn_params* p, const seer_evict_params* e);
+
+/*
+ *  p              B, Hkv, Dqk, Dv (multiples of 8), page_size (any), num_pages, max_pages_per_seq, kv_shared_latent are used
+ *  k_pages, v_pages  device, 16-bit elements, modified in place; v_pages NULL iff kv_shared_latent
+ *  block_table    device [B,max_pages_per_seq] int32;  ctx_len device [B] int32
+ *  keep_first     device [B] int32 or NULL (e->keep_first for every request)
+ *  weights        device [B, Hkv, max_pages_per_seq * page_size] fp32, as kept by seer_kv_weights
+ *  new_ctx_len    device [B] int32, written; may be ctx_len (the layers of a model that share one array of lengths
+ *                 want another one)
+ *  new_weights    device, as weights, or NULL: entries 0 .. new_ctx_len[b] - 1 get the sums of the positions that are there
+ *                 now, others are left as they are; may be weights itself, no other overlap
+ *  kept           device [B,Hkv,budget] int32 or NULL, written: the position that was moved to each slot or stayed in
+ *                 it; -1 throughout for requests that are not cut
+ *  status         device [1] int32 or NULL; bits are OR-ed in: 1 = a ctx_len below 0 or beyond the block table, 2 = a page id
+ *                 outside the pool among a request's pages from its first position that may move, 4 = keep_first[b] below 0
+ *                 or above budget - keep_last (looked at where the request would be cut).  Such requests are left untouched.  The caller clears it.
+ *  workspace      device, >= seer_kv_evict_workspace(p, e) bytes, 16-byte aligned
+ * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_kv_evict(const seer_attn_params* p, const seer_evict_params* e, void* k_pages, void* v_pages,
+                  const int32_t* block_table, const int32_t* ctx_len, const int32_t* keep_first, const float* weights,
+                  int32_t* new_ctx_len, float* new_weights, int32_t* kept, int32_t* status, void* workspace,
+                  size_t workspace_bytes, void* hip_stream);
+
 /* Static text for a return code of either call (negative SEER_E*, or a
  * positive hipError_t). */
 SEER_API const char* seer_strerror(int code);

@@ -24,7 +24,7 @@ EXPORTS = ("seer_verify_attention_workspace", "seer_verify_attention_status_offs
            "seer_accept_workspace", "seer_accept", "seer_accept_static", "seer_accept_sampled",
            "seer_kv_commit", "seer_mba_draft_lengths", "seer_acceptance_stats", "seer_acceptance_beta", "seer_draft_workspace", "seer_draft", "seer_history_append",
            "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad",
-           "seer_kv_weights_workspace", "seer_kv_weights", "seer_strerror")
+           "seer_kv_weights_workspace", "seer_kv_weights", "seer_kv_evict_workspace", "seer_kv_evict", "seer_strerror")
 
 
 class SeerAttnParams(ctypes.Structure):
@@ -44,6 +44,10 @@ class SeerDraftParams(ctypes.Structure):
 class SeerLogprobParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("ld", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("top_n", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class SeerEvictParams(ctypes.Structure):
+    _fields_ = [("limit", ctypes.c_int32), ("budget", ctypes.c_int32), ("keep_first", ctypes.c_int32), ("keep_last", ctypes.c_int32)]
 
 
 SEER_F32, SEER_BF16 = 0, 1
@@ -117,6 +121,10 @@ def load_library() -> ctypes.CDLL:
         lib.seer_kv_weights_workspace.restype = sz
         lib.seer_kv_weights.argtypes = [vp] * 7 + [ctypes.c_float, ctypes.POINTER(SeerAttnParams), vp, vp, sz, vp]
         lib.seer_kv_weights.restype = ctypes.c_int
+        lib.seer_kv_evict_workspace.argtypes = [ctypes.POINTER(SeerAttnParams), ctypes.POINTER(SeerEvictParams)]
+        lib.seer_kv_evict_workspace.restype = sz
+        lib.seer_kv_evict.argtypes = [ctypes.POINTER(SeerAttnParams), ctypes.POINTER(SeerEvictParams)] + [vp] * 11 + [sz, vp]
+        lib.seer_kv_evict.restype = ctypes.c_int
         lib.seer_strerror.argtypes = [ctypes.c_int]
         lib.seer_strerror.restype = ctypes.c_char_p
         _lib = lib
@@ -566,3 +574,53 @@ def seer_kv_weights(weights: torch.Tensor, q: torch.Tensor, k_pages: torch.Tenso
                                _ptr(accepted_path), float(decay), ctypes.byref(p), _ptr(status), _ptr(workspace),
                                workspace.numel(), _stream_handle(stream)))
     return weights
+
+
+def seer_kv_evict_workspace(params: SeerAttnParams, evict: SeerEvictParams) -> int:
+    return int(load_library().seer_kv_evict_workspace(ctypes.byref(params), ctypes.byref(evict)))
+
+
+def seer_kv_evict(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_table: torch.Tensor, ctx_len: torch.Tensor,
+                  weights: torch.Tensor, *, limit: int, budget: int, keep_first=0, keep_last: int = 0,
+                  new_weights: Optional[torch.Tensor] = None, new_ctx_len: Optional[torch.Tensor] = None,
+                  kept: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Cuts requests of more than `limit` positions to `budget` of them, per KV head, by their sums in weights [B, Hkv, max_pages * page]
+    float32; the pools (and new_weights, which may be weights) are changed in place.  keep_first: positions from the start that
+    stay, a number or int32 [B] on the device.  Returns (new_ctx_len [B] int32, kept [B,Hkv,budget] int32)."""
+    lib = load_library()
+    if k_pages.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("want k_pages [num_pages,Hkv,page,Dqk] and block_table [B,max_pages]")
+    num_pages, Hkv, P, Dqk = k_pages.shape
+    B, max_pages = block_table.shape
+    for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+        if t is not None and not (t.is_contiguous() and t.is_cuda and t.element_size() == 2 and t.dim() == 4 and tuple(t.shape[:3]) == (num_pages, Hkv, P)):
+            raise ValueError("%s: want a contiguous 16-bit device tensor [num_pages, Hkv, page, D]" % name)
+    _want(block_table, torch.int32, (B, max_pages), "block_table")
+    _want(ctx_len, torch.int32, (B,), "ctx_len")
+    _want(weights, torch.float32, (B, Hkv, max_pages * P), "weights")
+    per_request = isinstance(keep_first, torch.Tensor)
+    if per_request:
+        _want(keep_first, torch.int32, (B,), "keep_first")
+    p = SeerAttnParams(B, 1, Hkv, Hkv, Dqk, v_pages.shape[3] if v_pages is not None else 0, P, num_pages, max_pages, 0,
+                       1 if v_pages is None else 0, 0, 1.0)
+    e = SeerEvictParams(int(limit), int(budget), 0 if per_request else int(keep_first), int(keep_last))
+    if new_weights is not None:
+        _want(new_weights, torch.float32, (B, Hkv, max_pages * P), "new_weights")
+    if new_ctx_len is None:
+        new_ctx_len = torch.empty(B, dtype=torch.int32, device=k_pages.device)
+    else:
+        _want(new_ctx_len, torch.int32, (B,), "new_ctx_len")
+    if kept is None:
+        kept = torch.empty((B, Hkv, max(e.budget, 0)), dtype=torch.int32, device=k_pages.device)
+    else:
+        _want(kept, torch.int32, (B, Hkv, e.budget), "kept")
+    if status is not None:
+        _want(status, torch.int32, (1,), "status")
+    if workspace is None:
+        need = int(lib.seer_kv_evict_workspace(ctypes.byref(p), ctypes.byref(e)))
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=k_pages.device)
+    _check(lib.seer_kv_evict(ctypes.byref(p), ctypes.byref(e), _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(ctx_len),
+                             _ptr(keep_first) if per_request else None, _ptr(weights), _ptr(new_ctx_len), _ptr(new_weights), _ptr(kept),
+                             _ptr(status), _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+    return new_ctx_len, kept

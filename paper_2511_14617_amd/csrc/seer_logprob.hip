@@ -84,12 +84,6 @@ __device__ __forceinline__ int64_t logits_row(const LogprobArgs& a, int r, int& 
     return static_cast<int64_t>(r / a.T) * a.T + slot;
 }
 
-// Whole numbers in the order of the floats they come from (-0 = +0; above 0 for every float but a NaN with its sign bit set).
-__device__ __forceinline__ uint32_t ordered(float x) {
-    const uint32_t u = __float_as_uint(x + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ float unordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 constexpr uint32_t kOrderedNegInf = 0x007fffffu;
 // Keys of alternatives: larger value first, then lower index.
 __device__ __forceinline__ uint64_t alt_key(uint32_t value, int index) { return static_cast<uint64_t>(value) << 32 | static_cast<uint32_t>(~index); }

@@ -135,3 +135,47 @@ def test_kv_weights_workspace_and_argument_errors_before_any_launch(lib):
     assert run(attn(), w=FAKE + 2) == b.SEER_EALIGN
     assert run(attn(), status=FAKE + 1) == b.SEER_EALIGN
     assert run(attn(B=0)) == b.SEER_OK
+
+
+def ev(**kw):
+    from paper_2511_14617_amd.binding import SeerEvictParams
+    base = dict(limit=300, budget=256, keep_first=16, keep_last=32)
+    base.update(kw)
+    return SeerEvictParams(**base)
+
+
+def test_evict_struct_matches_header():
+    from paper_2511_14617_amd.binding import SeerEvictParams
+    assert struct_fields("seer_evict_params") == list(SeerEvictParams._fields_)
+
+
+def test_kv_evict_workspace_and_argument_errors_before_any_launch(lib):
+    from paper_2511_14617_amd import binding as b
+    size = b.seer_kv_evict_workspace
+    assert size(attn(), ev()) > 0 and size(attn(), ev()) % 256 == 0
+    assert size(attn(max_pages_per_seq=2), ev()) > 0             # a budget beyond the block table: nothing is ever cut
+
+    def run(p, e, k=FAKE, v=FAKE, table=FAKE, ctx=FAKE, first=None, w=FAKE, new=FAKE, neww=None, kept=None, status=None, ws=0x10000, ws_bytes=1 << 40):
+        return lib.seer_kv_evict(None if p is None else ctypes.byref(p), None if e is None else ctypes.byref(e), k, v, table, ctx, first, w, new, neww, kept,
+                                 status, ws, ws_bytes, None)
+
+    assert run(None, ev()) == b.SEER_EINVAL
+    assert run(attn(), None) == b.SEER_EINVAL
+    for bad, code in ((dict(B=-1), b.SEER_EINVAL), (dict(num_pages=0), b.SEER_EINVAL), (dict(Hkv=0), b.SEER_ESHAPE), (dict(Dqk=100), b.SEER_ESHAPE),
+                      (dict(Dv=4), b.SEER_ESHAPE), (dict(Dv=0), b.SEER_ESHAPE), (dict(max_pages_per_seq=1 << 30), b.SEER_ESHAPE),
+                      (dict(B=1 << 20), b.SEER_ESHAPE)):
+        assert run(attn(**bad), ev()) == code, bad
+        assert size(attn(**bad), ev()) == 0, bad
+    for bad, code in ((dict(budget=0), b.SEER_EINVAL), (dict(limit=255), b.SEER_EINVAL), (dict(keep_first=-1), b.SEER_EINVAL), (dict(keep_last=-1), b.SEER_EINVAL),
+                      (dict(keep_first=225), b.SEER_ESHAPE)):
+        assert run(attn(), ev(**bad)) == code, bad
+        assert size(attn(), ev(**bad)) == 0, bad
+    for name in ("k", "v", "table", "ctx", "w", "new"):
+        assert run(attn(), ev(), **{name: None}) == b.SEER_EINVAL, name
+    assert run(attn(kv_shared_latent=1), ev()) == b.SEER_EINVAL          # the shared latent has no v_pages
+    assert run(attn(), ev(), ws=None) == b.SEER_EWORKSPACE
+    assert run(attn(), ev(), ws_bytes=size(attn(), ev()) - 1) == b.SEER_EWORKSPACE
+    assert run(attn(), ev(), ws=0x10008) == b.SEER_EALIGN
+    assert run(attn(), ev(), k=FAKE + 8) == b.SEER_EALIGN
+    assert run(attn(), ev(), w=FAKE + 2) == b.SEER_EALIGN
+    assert run(attn(B=0), ev()) == b.SEER_OK
