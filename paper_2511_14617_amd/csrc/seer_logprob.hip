@@ -12,6 +12,7 @@
 
 #include "../../include/seer_verify.h"
 #include "seer_device.h"
+#include "seer_plan.h"
 #include "seer_tile.h"
 
 namespace seer {
@@ -57,6 +58,23 @@ struct Elem<SEER_BF16> {
     }
     static __device__ __forceinline__ void store_one(T* p, float g) { *p = f32_to_bf16(g); }
 };
+
+// Over the lanes of a wave through DPP, in every lane.
+__device__ __forceinline__ float all_sum(float v) { return last_lane(wave_incl_scan(v)); }
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ float max_step(float v) {
+    const int x = __float_as_int(v);
+    return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(x, x, CTRL, ROW_MASK, 0xf, false)));
+}
+__device__ __forceinline__ float all_max(float v) {
+    v = max_step<0x111, 0xf>(v);
+    v = max_step<0x112, 0xf>(v);
+    v = max_step<0x114, 0xf>(v);
+    v = max_step<0x118, 0xf>(v);
+    v = max_step<0x142, 0xa>(v);
+    v = max_step<0x143, 0xc>(v);
+    return last_lane(v);
+}
 
 struct LogprobArgs {
     const void* logits;
@@ -104,11 +122,12 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
     constexpr int kVec = E::kVec, kIter = kChunk / (kLpThreads * kVec);
     __shared__ float s_max[kLpWaves], s_sum[kLpWaves][2];
     const int r = blockIdx.x / a.n_chunks, chunk = blockIdx.x - r * a.n_chunks;
-    int token;
-    const int64_t row = logits_row(a, r, token);
-    if (row < 0) return;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const int begin = chunk * kChunk, end = min(a.V, begin + kChunk);
+    // (without a path the logits are requested beside the token, not behind it)
+    int token;
+    int64_t row = r;
+    if (a.path && (row = logits_row(a, r, token)) < 0) return;
     const typename E::T* base = static_cast<const typename E::T*>(a.logits) + row * a.ld;
 
     // whole vectors, then one element of the last, incomplete one
@@ -120,32 +139,58 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
     }
     const int rest = begin + (end - begin) / kVec * kVec + tid;
     const float x_rest = rest < end ? E::one(base + rest) : kNegInf;
+    if (!a.path && logits_row(a, r, token) < 0) return;
 
     float top = x_rest;
 #pragma unroll
     for (int it = 0; it < kIter; ++it)
 #pragma unroll
         for (int c = 0; c < kVec; ++c) top = fmaxf(top, E::get(x[it], c));
-    const float wave_top = wave_max(top);
+    const float wave_top = all_max(top);
     if (lane == 0) s_max[wave] = wave_top;
     __syncthreads();
     float m = s_max[0];
 #pragma unroll
     for (int w = 1; w < kLpWaves; ++w) m = fmaxf(m, s_max[w]);
 
-    const float scale = a.inv_tau * kLog2e, ref = m == kNegInf ? 0.f : m;
+    // d = v scale - c with c = m scale rounded: one fused multiply-add, exact but for its last rounding, and an unpacking, two sums and the exponential beside
+    // it are what a logit costs (with the difference, the product and a clamp against -inf apart the bf16 scan was bound by them: 4096
+    // rows of 151 936 in 215 us).  Where a logit of -inf makes the second sum a NaN, or m scale leaves the floats, a wave goes over
+    // its logits again, with more care.
+    const float scale = a.inv_tau * kLog2e, c = m * scale;
+    const bool usual = fabsf(c) < 1e30f;
     float l = 0.f, s = 0.f;
     auto add = [&](float v) __attribute__((always_inline)) {
-        const float d = (v - ref) * scale, e = fast_exp2(d);       // (a NaN reaches l, and through it every result of the row)
+        const float d = fmaf(v, scale, -c), e = fast_exp2(d);      // (a NaN reaches l, and through it every result of the row)
+        l += e;
+        s = fmaf(e, d, s);
+    };
+    auto add_with_care = [&](float v) __attribute__((always_inline)) {
+        const float d = (v - (m == kNegInf ? 0.f : m)) * scale, e = fast_exp2(d);
         l += e;
         s = fmaf(e, fmaxf(d, kLowest), s);
     };
+    auto every = [&](auto&& use) __attribute__((always_inline)) {
 #pragma unroll
-    for (int it = 0; it < kIter; ++it)
+        for (int it = 0; it < kIter; ++it)
+            if (begin + (it * kLpThreads + tid) * kVec + kVec <= end) {
 #pragma unroll
-        for (int c = 0; c < kVec; ++c) add(E::get(x[it], c));
-    add(x_rest);
-    l = wave_sum(l), s = wave_sum(s);
+                for (int i = 0; i < kVec; ++i) use(E::get(x[it], i));
+            }
+    };
+    every(add);
+    if (!usual || __any(s != s)) {
+        l = s = 0.f;
+        every(add_with_care);
+        add_with_care(x_rest);
+        l = all_sum(l), s = all_sum(s);
+    } else {
+        if (rest < end) add(x_rest);
+        l = all_sum(l), s = all_sum(s);
+        // from c to m itself
+        const float off = fmaf(m, scale, -c), f = fast_exp2(-off);
+        s = f * fmaf(-off, l, s), l *= f;
+    }
     if (lane == 0) s_sum[wave][0] = l, s_sum[wave][1] = s;
 
     if constexpr (TOP) {
@@ -190,6 +235,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
             for (int i = tid; i < count; i += kLpThreads) {
                 const uint64_t k = s_cand[i];
                 int before = 0;
+#pragma unroll 8
                 for (int j = 0; j < count; ++j) before += s_cand[j] > k ? 1 : 0;
                 if (before < n) out[before] = k;
             }
@@ -226,28 +272,47 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
     }
 }
 
-// One wave per row: the sums of its chunks brought to the row's maximum, in ascending order of the chunks per lane, and the
-// n first of their sorted lists, each lane holding the head of the lists lane, lane + 64, ...
+// One wave per row: the sums of its chunks brought to the row's maximum, and the n first of their lists.  Few keys (up to kJoinHold * 64) are taken
+// at once: each lane's largest gives a bound that n keys reach (as in logprob_scan), the keys that reach it are ranked by counting.
+// More of them, or more than kJoinCand that reach it, are merged one by one, each lane holding the head of the lists lane, lane + 64, ..
+// (always merged one by one, with the next head read from memory each time, it took 13 us for 38 lists of 20).
+constexpr int kJoinHold = 20, kJoinCand = 256;
+
 template <int DTYPE>
 __global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
     extern __shared__ uint8_t s_taken[];                    // per chunk: keys taken from its list
+    __shared__ uint64_t s_cand[kJoinCand];
     const int r = blockIdx.x, lane = threadIdx.x, n = a.top_n;
+    const float* part = a.part + static_cast<size_t>(r) * a.n_chunks * 3;
+    const uint64_t* lists = a.part_top + static_cast<size_t>(r) * a.n_chunks * n;
+    // (what a row without an entry finds here is not used)
+    float m = kNegInf;
+    for (int c = lane; c < a.n_chunks; c += kWave) m = fmaxf(m, part[c * 3]);
+    const int64_t total = static_cast<int64_t>(a.n_chunks) * n;
+    const bool few = total <= kJoinHold * kWave;
+    uint64_t key[kJoinHold];
+    if (few) {
+#pragma unroll
+        for (int x = 0; x < kJoinHold; ++x) {
+            key[x] = 0;
+            if (x * kWave < total && x * kWave + lane < total) key[x] = lists[x * kWave + lane];
+        }
+    }
     int token;
     const int64_t row = logits_row(a, r, token);
+    float* const alt_logp = a.top_logprob + static_cast<size_t>(r) * n;
+    int32_t* const alt_token = a.top_token + static_cast<size_t>(r) * n;
     if (row < 0) {
         if (lane == 0) {
             a.logprob[r] = 0.f;
             if (a.entropy) a.entropy[r] = 0.f;
             if (a.logsumexp) a.logsumexp[r] = 0.f;
         }
-        if (lane < n) a.top_logprob[static_cast<size_t>(r) * n + lane] = 0.f, a.top_token[static_cast<size_t>(r) * n + lane] = -1;
+        if (lane < n) alt_logp[lane] = 0.f, alt_token[lane] = -1;
         return;
     }
     const float x_token = Elem<DTYPE>::one(static_cast<const typename Elem<DTYPE>::T*>(a.logits) + row * a.ld + token);
-    const float* part = a.part + static_cast<size_t>(r) * a.n_chunks * 3;
-    float m = kNegInf;
-    for (int c = lane; c < a.n_chunks; c += kWave) m = fmaxf(m, part[c * 3]);
-    m = wave_max(m);
+    m = all_max(m);
     const float scale = a.inv_tau * kLog2e;
     float l = 0.f, s = 0.f;
     for (int c = lane; c < a.n_chunks; c += kWave) {
@@ -255,7 +320,7 @@ __global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
         l += w * part[c * 3 + 1];
         s += w * fmaf(part[c * 3 + 1], fmaxf(d, kLowest), part[c * 3 + 2]);
     }
-    l = wave_sum(l), s = wave_sum(s);
+    l = all_sum(l), s = all_sum(s);
     const float ln_l = logf(l);
     const bool empty = m == kNegInf && l == 0.f;             // every logit is -inf
     auto logp = [&](float x) __attribute__((always_inline)) { return x == kNegInf ? kNegInf : (x - m) * a.inv_tau - ln_l; };
@@ -265,43 +330,75 @@ __global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
         if (a.logsumexp) a.logsumexp[r] = empty ? kNegInf : fmaf(m, a.inv_tau, ln_l);
     }
     if (n == 0) return;
-    const uint64_t* lists = a.part_top + static_cast<size_t>(r) * a.n_chunks * n;
-    for (int c = lane; c < a.n_chunks; c += kWave) s_taken[c] = 0;
-    uint64_t head = 0;
-    int from = 0;
-    auto find_head = [&]() __attribute__((always_inline)) {
-        head = 0;
-        for (int c = lane; c < a.n_chunks; c += kWave) {
-            const int at = s_taken[c];
-            const uint64_t k = at < n ? lists[static_cast<size_t>(c) * n + at] : 0;
-            if (k > head) head = k, from = c;
-        }
+    auto write = [&](int at, uint64_t k) __attribute__((always_inline)) {
+        alt_logp[at] = logp(unordered(static_cast<uint32_t>(k >> 32)));
+        alt_token[at] = static_cast<int>(~static_cast<uint32_t>(k));
     };
-    find_head();
-    uint64_t mine = 0;                                      // lane k: the k-th alternative
-    int got = 0;
-    for (; got < n; ++got) {
-        uint64_t best = head;
+
+    uint64_t mine = 0;                                      // (fewer than n finite logits: lane k's is the k-th alternative)
+    int got = kWave;                                        // how many there are
+    bool ranked = false;
+    if (few) {
+        uint64_t top = 0;
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), o, kWave)));
-        if (best == 0) break;
-        if (lane == got) mine = best;
-        if (head == best) {
-            ++s_taken[from];
-            find_head();
+        for (int x = 0; x < kJoinHold; ++x) top = max(top, key[x]);
+        const uint32_t bound = wave_nth_largest(static_cast<uint32_t>(top >> 32), n);
+        int count = 0;
+#pragma unroll
+        for (int x = 0; x < kJoinHold; ++x) {
+            if (x * kWave < total) {
+                const bool in = key[x] != 0 && static_cast<uint32_t>(key[x] >> 32) >= bound;
+                const uint64_t who = __ballot(in);
+                const int at = count + __popcll(who & ((1ull << lane) - 1));
+                if (in && at < kJoinCand) s_cand[at] = key[x];
+                count += __popcll(who);
+            }
+        }
+        if (count <= kJoinCand) {
+            ranked = true;
+            __syncthreads();
+            for (int i = lane; i < count; i += kWave) {
+                const uint64_t k = s_cand[i];
+                int before = 0;
+#pragma unroll 8
+                for (int j = 0; j < count; ++j) before += s_cand[j] > k ? 1 : 0;
+                if (before < n) write(before, k);
+            }
+            got = count;
+            if (count < n && lane < count) mine = s_cand[lane];
         }
     }
-    int index = static_cast<int>(~static_cast<uint32_t>(mine));
-    float x = unordered(static_cast<uint32_t>(mine >> 32));
-    // fewer than n finite logits: the lowest indices that are not among them, whose logits are -inf
-    for (int v = 0; got < n; ++v) {
-        if (__ballot(lane < got && index == v)) continue;
-        if (lane == got) index = v, x = kNegInf;
-        ++got;
+    if (!ranked) {
+        for (int c = lane; c < a.n_chunks; c += kWave) s_taken[c] = 0;
+        uint64_t head = 0;
+        int from = 0;
+        auto find_head = [&]() __attribute__((always_inline)) {
+            head = 0;
+            for (int c = lane; c < a.n_chunks; c += kWave) {
+                const int at = s_taken[c];
+                const uint64_t k = at < n ? lists[static_cast<size_t>(c) * n + at] : 0;
+                if (k > head) head = k, from = c;
+            }
+        };
+        find_head();
+        for (got = 0; got < n; ++got) {
+            uint64_t best = head;
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) best = max(best, static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(best), o, kWave)));
+            if (best == 0) break;
+            if (lane == got) mine = best, write(got, best);
+            if (head == best) {
+                ++s_taken[from];
+                find_head();
+            }
+        }
     }
-    if (lane < n) {
-        a.top_logprob[static_cast<size_t>(r) * n + lane] = logp(x);
-        a.top_token[static_cast<size_t>(r) * n + lane] = index;
+    // fewer than n finite logits: the lowest indices that are not among them, whose logits are -inf
+    const int index = static_cast<int>(~static_cast<uint32_t>(mine)), found = got;
+    for (int v = 0; got < n; ++v) {
+        if (__ballot(lane < found && index == v)) continue;
+        if (lane == 0) alt_logp[got] = kNegInf, alt_token[got] = v;
+        ++got;
     }
 }
 

@@ -109,6 +109,50 @@ def test_empty_requests_and_one_position():
     check(s, 1, 1, 0, 1, False)
 
 
+WIDE = 700       # pages of 16 beyond the longest request: a table of more than 8192 positions, whose rows are cut into segments
+
+
+@pytest.mark.parametrize("limit,budget,first,last", [(64, 64, 0, 0), (64, 64, 16, 48), (100, 64, 0, 64), (99, 1, 0, 1), (64, 2, 1, 1), (4096, 4096, 0, 0),
+                                                     (4095, 4000, 3, 1), (8000, 7000, 300, 500), (4200, 4100, 4, 4096)])
+@pytest.mark.parametrize("in_place", [True, False])
+def test_rows_of_segments(limit, budget, first, last, in_place):
+    """Lengths around one, two and three segments of candidates."""
+    s = build(8, 1, 64, 64, 16, [65, 4096, 4097, 4100 + last, 8192 + first + last, 8193 + first + last, 9000, 12345], budget, extra_pages=WIDE)
+    check(s, limit, budget, first, last, in_place)
+
+
+def test_rows_of_segments_with_equal_negative_infinite_and_nan_sums():
+    s = build(8, 1, 64, 64, 16, [9000] * 8, 9, extra_pages=WIDE)
+    w = s["w"]
+    w[0] = 1.0                                               # all equal: the lowest positions stay
+    w[1] = -w[1]
+    w[2, :, ::3] = float("inf")
+    w[3, :, ::2] = float("nan")
+    w[4] = 0.0
+    w[4, :, ::2] = -0.0
+    w[5] = float("nan")
+    w[5, :, 5000] = -float("inf")
+    w[6] = torch.arange(w.shape[2], device="cuda", dtype=torch.float32)
+    w[7] = -w[6]
+    check(s, 8999, 2000, 3, 20)
+    check(s, 8999, 8990, 3, 20, False)
+
+
+@pytest.mark.parametrize("seen", ["low", "high"])
+def test_rows_whose_sampled_sums_mislead(seen):
+    """The search looks at 512 sums, spread evenly, to know where to look closer: here these are the smallest (largest) of all."""
+    n, first, last = 40000, 100, 50
+    s = build(2, 1, 64, 64, 16, [n, n], 12)
+    total = n - first - last
+    at = first + (2 * torch.arange(512, device="cuda") + 1) * total // 1024
+    s["w"].add_(1.0)
+    s["w"][:, :, at] = 0.5 if seen == "low" else 1e6
+    check(s, 20000, 15000, first, last)
+    check(s, 20000, 400, first, last, False)
+    check(s, 20000, 700, first, last, False)
+    check(s, 39990, 39980, first, last)
+
+
 @pytest.mark.parametrize("n", [70000, 131072])
 def test_long_caches(n):
     s = build(2, 1, 64, 64, 16, [n, n // 3], 5)
@@ -161,9 +205,10 @@ def test_without_optional_outputs():
     assert np.array_equal(k.view(torch.int16).cpu().numpy(), want[3][0]) and np.array_equal(v.view(torch.int16).cpu().numpy(), want[3][1])
 
 
-def test_unusable_requests_are_left_alone_and_reported():
+@pytest.mark.parametrize("extra", [1, WIDE])
+def test_unusable_requests_are_left_alone_and_reported(extra):
     from paper_2511_14617_amd import binding
-    s = build(4, 2, 128, 128, 16, [300, 300, 300, 250], 12)
+    s = build(4, 2, 128, 128, 16, [300, 300, 300, 250], 12, extra_pages=extra)
     firsts = np.asarray([5, 5, 5, 5], dtype=np.int32)
     for what, at, value, bit in (("ctx", 1, -1, 1), ("ctx", 1, 16 * s["table"].shape[1] + 1, 1), ("first", 1, -1, 4), ("first", 1, 181, 4), ("table", (1, 0), -1, 2),
                                  ("table", (1, 18), 1 << 29, 2)):
@@ -197,9 +242,10 @@ def test_a_page_of_the_common_prefix_may_be_shared():
     assert torch.equal(k[shared].view(torch.int16), s["k"][shared].view(torch.int16)) and torch.equal(v[shared].view(torch.int16), s["v"][shared].view(torch.int16))
 
 
-def test_other_stream_and_graph():
+@pytest.mark.parametrize("extra", [1, WIDE])
+def test_other_stream_and_graph(extra):
     from paper_2511_14617_amd import binding
-    s = build(6, 2, 128, 128, 16, [300, 500, 260, 100, 777, 1000], 14)
+    s = build(6, 2, 128, 128, 16, [300, 500, 260, 100, 777, 1000], 14, extra_pages=extra)
     p = binding.SeerAttnParams(6, 1, 2, 2, 128, 128, 16, s["k"].shape[0], s["table"].shape[1], 0, 0, 0, 1.0)
     ws = torch.full((binding.seer_kv_evict_workspace(p, binding.SeerEvictParams(256, 200, 8, 33)),), 0x77, dtype=torch.uint8, device="cuda")
     side = torch.cuda.Stream()
