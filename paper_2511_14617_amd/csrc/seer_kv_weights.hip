@@ -5,13 +5,17 @@
 // lse_r = ln sum_j exp s_rj over what the row sees,
 //   w_j <- decay w_j (0 for the step's own positions) + sum_r exp(s_rj - lse_r).
 //
-// What bounds it: HBM for a few rows, the matrix cores for the many rows of a shared latent.  A weight needs its row's denominator, so the keys are swept
-// twice, with the same loads and matrix products: kv_sweep<.., false> leaves each row's running maximum and sum per piece,
-// kv_lse joins them, kv_sweep<.., true> exponentiates again and adds up the rows of each position.
+// What bounds it: HBM for a few rows, LDS reads and matrix products in turn for the many rows of a shared latent.  A weight needs its row's
+// denominator first:
+//   up to 16 rows   one sweep over the keys (kModeKeep) that leaves each row's maximum and sum per piece and the scores, kv_lse, which joins the
+//                   denominators, and kv_apply, which reads the scores.  64 requests of 512 .. 32 768 tokens on 32/8 heads, one row each: 278 us with two
+//                   sweeps, 167 with one.
+//   more            the scores would cost more than the keys: two sweeps with the same loads and matrix products, kModeSums and
+//                   kModeWeights, kv_lse between them.
 //
 // Work decomposition: per KV head the 32-token tiles of all requests, each times its row blocks of 32 NW rows, lie on one line, cut
 // into equal stretches, one per workgroup, all of them resident at once.  Every workgroup finds its stretch from the lengths
-// (line_of, one request per lane).  A piece is a request's part of a stretch; piece (w, b) has partial slot w + b (along the line every
+// (for_pieces, one request per lane).  A piece is a request's part of a stretch; piece (w, b) has partial slot w + b (along the line every
 // next piece raises one of the two).  Tiles go from the pool to LDS directly (32 rows of 16-byte chunks, swizzled as in
 // seer_tile.h), wave i holds 32 query rows in registers.  The first sweep multiplies K.Q^T (a row per lane: its maximum and
 // sum stay in the lane), the second Q.K^T (a token per lane: the sum over the rows stays in the lane).
@@ -20,15 +24,21 @@
 
 #include "../../include/seer_verify.h"
 #include "seer_device.h"
+#include "seer_plan.h"
 #include "seer_tile.h"
 
 namespace seer {
 
 constexpr int kSwTile = 32;            // tokens of a tile
 constexpr int kSwChunk = 32;           // tiles whose sums are collected in LDS before they go to memory
-constexpr int kSwStages = 2;
+constexpr int kModeSums = 0, kModeWeights = 1, kModeKeep = 2;          // (see kv_sweep)
+// Stages of the ring of tiles in LDS, waves per SIMD that the registers have to leave room for.
+constexpr int sweep_stages(int Dqk, int mode) { return mode == kModeKeep && Dqk <= 256 ? 3 : 2; }
+constexpr int sweep_waves_per_simd(int Dqk) { return Dqk <= 128 ? 3 : 2; }
 constexpr int kSwMaxStretches = 2048;
+constexpr int64_t kCacheable = int64_t{192} << 20;
 constexpr int kLseThreads = 256, kLseRows = 8;
+constexpr int kApplyThreads = 256, kApplyPositions = 2048;
 
 struct KvWeightsArgs {
     float* weights;
@@ -42,6 +52,7 @@ struct KvWeightsArgs {
     int32_t* line;                     // [B + 2]: units per stretch, then each request's first unit on the line and the line's end
     float2* part;                      // [W + B][Hkv][G T] maximum (log2 units, scaled) and sum
     float* lse;                        // [B][Hkv][G T] log2 of the denominators
+    float* scores;                     // [B][Hkv][ldw][kept rows] scaled, in log2 units (few rows only)
     int64_t ldw;                       // positions of a row of weights
     int B, T, Hq, Hkv, G, P, num_pages, max_pages, max_ctx, W, block_rows;
     float scale_log2, decay;
@@ -60,13 +71,60 @@ __device__ __forceinline__ StepRows step_rows(const KvWeightsArgs& a, int b, boo
 __device__ __forceinline__ int row_blocks_of(const KvWeightsArgs& a, int rows) { return (rows * a.G + a.block_rows - 1) / a.block_rows; }
 __device__ __forceinline__ int units_of(const KvWeightsArgs& a, const StepRows& s) { return s.rows ? (s.n + kSwTile - 1) / kSwTile * row_blocks_of(a, s.rows) : 0; }
 
-__device__ __forceinline__ int wave_scan(int v) {          // inclusive
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-        const int x = __shfl_up(v, o, kWave);
-        if ((static_cast<int>(threadIdx.x) & (kWave - 1)) >= o) v += x;
+// The step's slots (lane i: row i's), which have to ascend from the root; `wrong` if they do not.
+__device__ __forceinline__ int step_slot(const KvWeightsArgs& a, int b, int rows, bool& wrong) {
+    const int lane = static_cast<int>(threadIdx.x) & (kWave - 1);
+    wrong = false;
+    if (!a.accepted_path) return lane;
+    const int slot = lane < rows ? a.accepted_path[static_cast<size_t>(b) * a.T + lane] : a.T, up = __shfl_up(slot, 1, kWave);
+    wrong = __any(lane < rows && (lane == 0 ? slot != 0 : slot <= up || slot >= a.T));
+    return slot;
+}
+
+// body(request, its positions, rows of the step, step_slot's, row blocks, first and last tile, units of the whole line) for every piece of stretch w.  The line: per KV head the
+// tiles of all requests, each times the request's row blocks, cut into equal stretches.  PUBLISH: the first workgroup leaves the line for kv_lse,
+// and status bits are raised.
+template <bool PUBLISH, class Body>
+__device__ __forceinline__ void for_pieces(const KvWeightsArgs& a, int w, int& found, Body&& body) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const bool publish = PUBLISH && blockIdx.x == 0;
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {               // 64 requests at a time
+        bool bad = false;
+        int u = 0;
+        if (b0 + lane < a.B) u = units_of(a, step_rows(a, b0 + lane, bad));
+        if (publish && bad) found |= 1;
+        const int incl = wave_incl_scan(u);
+        if (publish && tid < kWave && b0 + lane < a.B) a.line[1 + b0 + lane] = total + incl - u;
+        total += last_lane(incl);
     }
-    return v;
+    const int step = max(1, (total + a.W - 1) / a.W);
+    if (publish && tid == 0) a.line[0] = step, a.line[1 + a.B] = total;
+    const int u_begin = min(w * step, total), u_end = min(u_begin + step, total);
+    int before = 0;                                         // units of the requests in front of b0
+    for (int b0 = 0; b0 < a.B && before < u_end; b0 += kWave) {
+        bool bad = false;
+        StepRows mine{0, 0};
+        if (b0 + lane < a.B) mine = step_rows(a, b0 + lane, bad);
+        const int my_units = units_of(a, mine), incl = wave_incl_scan(my_units), my_off = before + incl - my_units;
+        uint64_t todo = __ballot(my_units > 0 && my_off < u_end && my_off + my_units > u_begin);
+        before += last_lane(incl);
+        for (; todo; todo &= todo - 1) {
+            const int bit = __builtin_ctzll(todo), b = b0 + bit;
+            const int off = __builtin_amdgcn_readlane(my_off, bit), n = __builtin_amdgcn_readlane(mine.n, bit);
+            const int rows = __builtin_amdgcn_readlane(mine.rows, bit), blocks = row_blocks_of(a, rows);
+            const int n_tiles = (n + kSwTile - 1) / kSwTile;
+            const int t_begin = min(n_tiles, (max(u_begin - off, 0) + blocks - 1) / blocks);
+            const int t_end = min(n_tiles, (u_end - off + blocks - 1) / blocks);
+            bool wrong;
+            const int slot = step_slot(a, b, rows, wrong);
+            if (wrong) {
+                if (PUBLISH) found |= 4;
+                continue;
+            }
+            body(b, n, rows, slot, blocks, t_begin, t_end, total);
+        }
+    }
 }
 
 template <int DQK>
@@ -96,13 +154,44 @@ __device__ __forceinline__ f32x16 sweep_scores(int at, int k_rd, const bf16x8 (&
     return s;
 }
 
-template <int DQK, int NW, bool WEIGHTS>
-__global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
+// A word of LDS (as asm with its wait, like the tiles' reads: through the compiler it would wait for the tile loads in flight).
+__device__ __forceinline__ float lds_word(int at) {
+    float v;
+    asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v) : "v"(at) : "memory");
+    return v;
+}
+
+// Sum of NW words 128 bytes apart, in their order.
+template <int NW>
+__device__ __forceinline__ float lds_sum(int at) {
+    if constexpr (NW == 2) {
+        float v[2];
+        asm volatile("ds_read_b32 %0, %2\n\tds_read_b32 %1, %2 offset:128\n\ts_waitcnt lgkmcnt(0)" : "=&v"(v[0]), "=&v"(v[1]) : "v"(at) : "memory");
+        return v[0] + v[1];
+    } else {
+        static_assert(NW == 8, "");
+        float v[8];
+        asm volatile("ds_read_b32 %0, %8\n\tds_read_b32 %1, %8 offset:128\n\tds_read_b32 %2, %8 offset:256\n\tds_read_b32 %3, %8 offset:384\n\t"
+                     "ds_read_b32 %4, %8 offset:512\n\tds_read_b32 %5, %8 offset:640\n\tds_read_b32 %6, %8 offset:768\n\tds_read_b32 %7, %8 offset:896\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+                     : "v"(at)
+                     : "memory");
+        return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
+}
+
+// MODE: kModeSums leaves each row's maximum and sum, kModeWeights the weights, kModeKeep (KEPT rows at most, one wave) maximum, sum and the scores themselves.
+template <int DQK, int NW, int MODE, int KEPT>
+__global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW == 8 ? 2 : 1))) void kv_sweep(KvWeightsArgs a) {
     using K = Keys<DQK>;
-    constexpr int kLoads = K::kBytes / 1024 / NW;           // direct-to-LDS loads of a wave per tile
-    static_assert(K::kBytes % (1024 * NW) == 0 && kLoads * (kSwStages - 1) < 64, "");
+    constexpr bool WEIGHTS = MODE == kModeWeights;
+    constexpr int kSwStages = sweep_stages(DQK, MODE);
+    constexpr int kTileLoads = K::kBytes / 1024, kLoads = (kTileLoads + NW - 1) / NW;      // direct-to-LDS loads of a tile, of a wave at most
+    static_assert(kSwStages == 2 || kLoads * (kSwStages - 1) < 64, "");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[kSwStages * K::kBytes];
-    __shared__ float s_sums[WEIGHTS ? NW : 1][WEIGHTS ? kSwChunk * kSwTile : 1];
+    __shared__ float s_sums[WEIGHTS ? kSwChunk * kSwTile : 1];
+    __shared__ __attribute__((aligned(16))) float s_denom[NW][WEIGHTS ? 32 : 1];       // of the waves' rows
+    __shared__ float s_part[2][WEIGHTS && NW > 1 ? NW : 1][WEIGHTS && NW > 1 ? kSwTile : 1];      // the waves' sums of a tile
 
     const int kvh = blockIdx.x % a.Hkv, w = blockIdx.x / a.Hkv;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
@@ -115,48 +204,10 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
     auto page_of = [&](int tok) __attribute__((always_inline)) -> int { return page_pow2 ? tok >> page_shift : tok / a.P; };
     int found = 0;                                          // status bits
 
-    // ---- the line: its length, then the pieces of this stretch, 64 requests at a time -------------------------------
-    int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        bool bad = false;
-        int u = 0;
-        if (b0 + lane < a.B) u = units_of(a, step_rows(a, b0 + lane, bad));
-        if (!WEIGHTS && blockIdx.x == 0 && bad) found |= 1;
-        const int incl = wave_scan(u);
-        if (!WEIGHTS && blockIdx.x == 0 && wave == 0 && b0 + lane < a.B) a.line[1 + b0 + lane] = total + incl - u;
-        total += __builtin_amdgcn_readlane(incl, kWave - 1);
-    }
-    const int step = max(1, (total + a.W - 1) / a.W);
-    if (!WEIGHTS && blockIdx.x == 0 && tid == 0) a.line[0] = step, a.line[1 + a.B] = total;
-    const int u_begin = min(w * step, total), u_end = min(u_begin + step, total);
-
-    int before = 0;                                         // units of the requests in front of b0
-    for (int b0 = 0; b0 < a.B && before < u_end; b0 += kWave) {
-        bool bad = false;
-        StepRows mine{0, 0};
-        if (b0 + lane < a.B) mine = step_rows(a, b0 + lane, bad);
-        const int my_units = units_of(a, mine), incl = wave_scan(my_units), my_off = before + incl - my_units;
-        uint64_t todo = __ballot(my_units > 0 && my_off < u_end && my_off + my_units > u_begin);
-        before += __builtin_amdgcn_readlane(incl, kWave - 1);
-        for (; todo; todo &= todo - 1) {
-            const int bit = __builtin_ctzll(todo), b = b0 + bit;
-            const int off = __builtin_amdgcn_readlane(my_off, bit), n = __builtin_amdgcn_readlane(mine.n, bit);
-            const int rows = __builtin_amdgcn_readlane(mine.rows, bit), R = rows * a.G, blocks = row_blocks_of(a, rows);
-            const int n_tiles = (n + kSwTile - 1) / kSwTile;
-            const int t_begin = min(n_tiles, (max(u_begin - off, 0) + blocks - 1) / blocks);
-            const int t_end = min(n_tiles, (u_end - off + blocks - 1) / blocks);
-
-            // the step's slots (lane i: row i's), which have to ascend from the root
-            int slot = lane;
-            if (a.accepted_path) {
-                slot = lane < rows ? a.accepted_path[static_cast<size_t>(b) * a.T + lane] : a.T;
-                const int up = __shfl_up(slot, 1, kWave);
-                const bool wrong = lane < rows && (lane == 0 ? slot != 0 : slot <= up || slot >= a.T);
-                if (__any(wrong)) {
-                    if (!WEIGHTS) found |= 4;
-                    continue;
-                }
-            }
+    for_pieces<MODE != kModeWeights>(a, w, found, [&](int b, int n, int rows, int slot, int blocks, int t_begin, int t_end, int total) __attribute__((always_inline)) {
+            const int R = rows * a.G;
+            // Keys that the memory-side cache cannot hold for the second sweep are streamed past it, and so are those that are read once.
+            const bool stream = MODE == kModeKeep || static_cast<int64_t>(total) * K::kBytes * a.Hkv > kCacheable;
 
             // ---- tile loads --------------------------------------------------------------------------
             const int32_t* __restrict__ table = a.block_table + static_cast<size_t>(b) * a.max_pages;
@@ -180,30 +231,46 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
                 const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + kvh) * static_cast<uint32_t>(a.P) + (tok - lp * a.P);
 #pragma unroll
                 for (int j = 0; j < kLoads; ++j) {
-                    const int c = (wave * kLoads + j) * kWave + lane, row = c / K::kRowChunks, pos = c - row * K::kRowChunks;
+                    const int piece = wave + j * NW;
+                    if (kTileLoads % NW != 0 && piece >= kTileLoads) break;
+                    const int c = piece * kWave + lane, row = c / K::kRowChunks, pos = c - row * K::kRowChunks;
                     const uint32_t r = __builtin_amdgcn_ds_bpermute(row << 2, row_idx);
                     const unsigned char* src = kbase + static_cast<size_t>(r) * K::kRow + ((pos ^ tile::k_swz<K::kRow>(row)) << 4);
-                    __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage * K::kBytes + (wave * kLoads + j) * 1024), 16, 0, 0);
+                    if (stream) __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage * K::kBytes + piece * 1024), 16, 0, 2);
+                    else __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage * K::kBytes + piece * 1024), 16, 0, 0);
                 }
             };
 
-            // Tiles t0 .. t1 - 1, each handed to `use` with its LDS address once it has landed for every wave.
-            auto sweep = [&](int t0, int t1, auto&& use) __attribute__((always_inline)) {
+            // Tiles t0 .. t1 - 1, each handed to `use` with its LDS address once it has landed for every wave; `after` is called behind the
+            // barrier that follows a tile.
+            auto sweep = [&](int t0, int t1, auto&& use, auto&& after) __attribute__((always_inline)) {
                 if (NW > 1) bare_barrier();                 // every wave is done with the stages
 #pragma unroll
                 for (int s = 0; s < kSwStages - 1; ++s)
                     if (t0 + s < t1) issue_tile(t0 + s, s);
                 int stage = 0;
                 for (int t = t0; t < t1; ++t) {
-                    if (t + kSwStages - 1 <= t1) wait_vmcnt<kLoads * (kSwStages - 2)>(); else wait_vmcnt<0>();
-                    if (NW > 1) bare_barrier();
+                    // (this wave's loads of the tiles behind this one may be on their way; near the end none are waited for apart)
+                    if (kSwStages == 2 || t + kSwStages - 1 > t1) wait_vmcnt<0>();
+                    else if (kTileLoads % NW == 0 || wave < kTileLoads % NW) wait_vmcnt<kLoads * (kSwStages - 2)>();
+                    else wait_vmcnt<(kLoads - 1) * (kSwStages - 2)>();
+                    if (NW > 1) {
+                        __builtin_amdgcn_s_waitcnt(0xc07f); // (lgkmcnt: what `use` wrote)
+                        bare_barrier();
+                    }
                     const int next = stage == 0 ? kSwStages - 1 : stage - 1;
                     if (t + kSwStages - 1 < t1) issue_tile(t + kSwStages - 1, next);
                     __builtin_amdgcn_sched_barrier(0);
+                    if (t > t0) after(t - 1);
                     use(t, lds0 + stage * K::kBytes);
                     __builtin_amdgcn_sched_barrier(0);
                     stage = stage + 1 == kSwStages ? 0 : stage + 1;
                 }
+                if (NW > 1) {
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    bare_barrier();
+                }
+                if (t1 > t0) after(t1 - 1);
             };
 
             bf16x8 q[K::kSteps];
@@ -224,12 +291,14 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
             };
             const int first_own = n - rows;                 // row i sees positions up to first_own + i
 
-            if constexpr (!WEIGHTS) {
+            if constexpr (MODE == kModeSums) {
                 for (int block = 0; block < blocks; ++block) {
                     const int r = load_rows(block);
                     const int seen = first_own + min(r, R - 1) / a.G + 1;
                     float m_run = kNegInf, l_run = 0.f;
+                    const bool idle = block * a.block_rows + wave * 32 >= R;      // (uniform: none of the wave's rows exists)
                     sweep(t_begin, t_end, [&](int t, int at) __attribute__((always_inline)) {
+                        if (NW > 1 && idle) return;
                         f32x16 s = sweep_scores<DQK, false>(at, k_rd, q);
                         const int tb = t * kSwTile;
                         if (tb + kSwTile > first_own + 1) {
@@ -246,9 +315,50 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum += fast_exp2(fmaf(s[i], a.scale_log2, -m_use));
                         l_run = fmaf(l_run, alpha, sum);
-                    });
+                    }, [](int) {});
                     const float l = l_run + __shfl_xor(l_run, 32, kWave);
                     if (lg == 0 && r < R) a.part[(static_cast<size_t>(w + b) * a.Hkv + kvh) * (a.G * a.T) + r] = make_float2(m_run, l);
+                }
+            } else if constexpr (MODE == kModeKeep) {
+                // a token per lane, its few rows in the first registers: maximum and sum per row and lane, joined at the end
+                constexpr int kRegs = KEPT <= 8 ? 4 : 8;
+                const int r_own = load_rows(0), row_i = min(r_own, R - 1) / a.G;
+                float m[kRegs], l[kRegs];
+#pragma unroll
+                for (int i = 0; i < kRegs; ++i) m[i] = kNegInf, l[i] = 0.f;
+                float* __restrict__ to = a.scores + (static_cast<size_t>(b) * a.Hkv + kvh) * a.ldw * KEPT;
+                sweep(t_begin, t_end, [&](int t, int at) __attribute__((always_inline)) {
+                    f32x16 s = sweep_scores<DQK, true>(at, k_rd, q);
+                    const int tok = t * kSwTile + ln;
+#pragma unroll
+                    for (int i = 0; i < kRegs; ++i) s[i] *= a.scale_log2;
+                    if (t * kSwTile + kSwTile > first_own + 1) {
+#pragma unroll
+                        for (int i = 0; i < kRegs; ++i)
+                            if (__shfl(row_i, (i >> 2) * 8 + lg * 4 + (i & 3), kWave) < tok - first_own) s[i] = kNegInf;
+                    }
+#pragma unroll
+                    for (int i = 0; i < kRegs; ++i) {
+                        const float top = fmaxf(m[i], s[i]), use = top == kNegInf ? 0.f : top;
+                        l[i] = fmaf(l[i], fast_exp2(m[i] - use), fast_exp2(s[i] - use));
+                        m[i] = top;
+                    }
+                    if (tok < n && (KEPT > 4 || lg == 0)) {
+#pragma unroll
+                        for (int i = 0; i < kRegs; i += 4)
+                            *reinterpret_cast<f32x4*>(to + static_cast<size_t>(tok) * KEPT + (i >> 2) * 8 + lg * 4) = f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]};
+                    }
+                }, [](int) {});
+#pragma unroll
+                for (int i = 0; i < kRegs; ++i) {
+                    float top = m[i];
+#pragma unroll
+                    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+                    float sum = m[i] == kNegInf ? l[i] * 0.f : l[i] * fast_exp2(m[i] - top);       // (nothing seen: 0, or a NaN that was)
+#pragma unroll
+                    for (int o = 16; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+                    const int r = (i >> 2) * 8 + lg * 4 + (i & 3);
+                    if (ln == 0 && r < R) a.part[(static_cast<size_t>(w + b) * a.Hkv + kvh) * (a.G * a.T) + r] = make_float2(top, sum);
                 }
             } else {
                 float* __restrict__ to = a.weights + (static_cast<size_t>(b) * a.Hkv + kvh) * a.ldw;
@@ -260,19 +370,26 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
                         float own = -kNegInf;               // (no such row: exp2 gives 0)
                         if (r < R) own = a.lse[(static_cast<size_t>(b) * a.Hkv + kvh) * (a.G * a.T) + r];
                         const bool partial = __any(!(own < -kNegInf));
-                        float denom[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) denom[i] = __shfl(own, (i >> 2) * 8 + lg * 4 + (i & 3), kWave);
+                        if (lg == 0) s_denom[wave][ln] = own;
+                        const int denom_at = tile::lds_addr(reinterpret_cast<const unsigned char*>(&s_denom[wave][lg * 4]));
                         const int row_i = min(r, R - 1) / a.G;
+                        const bool idle = block * a.block_rows + wave * 32 >= R;
                         sweep(c0, c1, [&](int t, int at) __attribute__((always_inline)) {
+                            if (NW > 1 && idle) {
+                                if (lg == 0) s_part[t & 1][wave][ln] = 0.f;
+                                return;
+                            }
                             f32x16 s = sweep_scores<DQK, true>(at, k_rd, q);
                             const int tb = t * kSwTile;
+                            u32x4 denom[4];                 // (read for every tile: kept in registers they are what the 576-wide rows have not)
+                            tile::read_k4(denom, denom_at, denom_at + 32, denom_at + 64, denom_at + 96);
+                            auto denom_of = [&](int i) __attribute__((always_inline)) { return __uint_as_float(denom[i >> 2][i & 3]); };
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], a.scale_log2, -denom[i]));
+                            for (int i = 0; i < 16; ++i) s[i] = fast_exp2(fmaf(s[i], a.scale_log2, -denom_of(i)));
                             if (partial) {
 #pragma unroll
                                 for (int i = 0; i < 16; ++i)
-                                    if (denom[i] == -kNegInf) s[i] = 0.f;
+                                    if (denom_of(i) == -kNegInf) s[i] = 0.f;
                             }
                             if (tb + kSwTile > first_own + 1) {
                                 const int behind = tb + ln - first_own;     // rows from this one on see the position
@@ -284,24 +401,34 @@ __global__ __launch_bounds__(NW * kWave) void kv_sweep(KvWeightsArgs a) {
 #pragma unroll
                             for (int i = 0; i < 16; ++i) sum += s[i];
                             sum += __shfl_xor(sum, 32, kWave);
-                            float* at_sum = &s_sums[wave][(t - c0) * kSwTile + ln];
-                            if (lg == 0) *at_sum = block ? *at_sum + sum : sum;
+                            if constexpr (NW > 1) {
+                                if (lg == 0) s_part[t & 1][wave][ln] = sum;
+                            } else {
+                                const int to_sum = tile::lds_addr(reinterpret_cast<const unsigned char*>(&s_sums[(t - c0) * kSwTile + ln]));
+                                if (block) sum += lds_word(to_sum);
+                                if (lg == 0) s_sums[(t - c0) * kSwTile + ln] = sum;
+                            }
+                        }, [&](int t) __attribute__((always_inline)) {
+                            if constexpr (NW > 1) {         // the waves' sums of the tile, in their order, by one of them
+                                if (wave != (t & (NW - 1))) return;
+                                const int from = tile::lds_addr(reinterpret_cast<const unsigned char*>(&s_part[t & 1][0][ln]));
+                                float sum = lds_sum<NW>(from);
+                                const int to_sum = tile::lds_addr(reinterpret_cast<const unsigned char*>(&s_sums[(t - c0) * kSwTile + ln]));
+                                if (block) sum += lds_word(to_sum);
+                                if (lg == 0) s_sums[(t - c0) * kSwTile + ln] = sum;
+                            }
                         });
                     }
                     __syncthreads();
                     const int tokens = min(n, c1 * kSwTile) - c0 * kSwTile;
                     for (int j = tid; j < tokens; j += NW * kWave) {
-                        float sum = s_sums[0][j];
-#pragma unroll
-                        for (int x = 1; x < NW; ++x) sum += s_sums[x][j];
                         const int pos = c0 * kSwTile + j;
-                        to[pos] = pos < first_own ? fmaf(a.decay, to[pos], sum) : sum;
+                        to[pos] = pos < first_own ? fmaf(a.decay, to[pos], s_sums[j]) : s_sums[j];
                     }
                     __syncthreads();
                 }
             }
-        }
-    }
+    });
     if (!WEIGHTS && a.status && found) atomicOr(a.status, found);
 }
 
@@ -341,20 +468,67 @@ __global__ __launch_bounds__(kLseThreads) void kv_lse(KvWeightsArgs a) {
     a.lse[(static_cast<size_t>(b) * a.Hkv + kvh) * GT + r] = top == kNegInf ? -kNegInf : top + log2f(sum);
 }
 
+// The weights from the scores that kModeKeep left: a position per thread.
+template <int KEPT>
+__global__ __launch_bounds__(kApplyThreads) void kv_apply(KvWeightsArgs a, int parts) {
+    const size_t bh = blockIdx.x / parts;
+    const int part = static_cast<int>(blockIdx.x - bh * parts), b = static_cast<int>(bh) / a.Hkv;
+    bool bad, wrong;
+    const StepRows step = step_rows(a, b, bad);
+    if (part * kApplyPositions >= step.n || step.rows == 0) return;
+    step_slot(a, b, step.rows, wrong);
+    if (wrong) return;
+    const int R = step.rows * a.G, first_own = step.n - step.rows;
+    const float* lse = a.lse + bh * (a.G * a.T);
+    float denom[KEPT];
+#pragma unroll
+    for (int r = 0; r < KEPT; ++r) denom[r] = r < R ? lse[r] : 0.f;
+    const float* scores = a.scores + bh * a.ldw * KEPT;
+    float* to = a.weights + bh * a.ldw;
+    for (int p0 = part * kApplyPositions; p0 < step.n; p0 += parts * kApplyPositions)
+#pragma unroll 4
+        for (int x = 0; x < kApplyPositions / kApplyThreads; ++x) {
+            const int pos = p0 + x * kApplyThreads + static_cast<int>(threadIdx.x);
+            if (pos >= step.n) break;
+            float sum = 0.f;
+#pragma unroll
+            for (int r = 0; r < KEPT; r += 4) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(scores + static_cast<size_t>(pos) * KEPT + r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (r + i < R) sum += fast_exp2(s[i] - denom[r + i]);
+            }
+            to[pos] = pos < first_own ? fmaf(a.decay, to[pos], sum) : sum;
+        }
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+// Rows whose scores are kept between the sweeps: written and read once they cost 8 bytes a position each, the second sweep
+// 2 Dqk; up to a quarter of that, and up to 16 (the workspace holds them for every position of the block table).  0: none.
+inline int kept_rows(int rows, int Dqk) {
+    const int kept = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
+    return rows <= 16 && kept <= Dqk / 8 ? kept : 0;
+}
 struct KvWeightsLayout {
-    int waves, W;
-    size_t off_part, off_lse, total;
+    int waves, W, kept;
+    size_t off_part, off_lse, off_scores, total;
 };
 inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     KvWeightsLayout w{};
     const int rows = (p.Hq / p.Hkv) * p.T;
-    w.waves = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    const int lds_kb = (kSwStages * kSwTile * p.Dqk * 2 + w.waves * kSwChunk * kSwTile * 4) / 1024 + 1;
-    int per_cu = 159 / lds_kb;
-    if (per_cu > 8 / w.waves) per_cu = 8 / w.waves;
+    w.kept = kept_rows(rows, p.Dqk);
+    // Waves of a workgroup.  Up to 256-wide keys: one per 32 rows that a request may have, at most two (of a step's slots only the accepted ones come, so
+    // most requests have fewer: 64 requests of 72 rows at most, two waves 53 us, four 58, one 62).  Shared latent: eight, since every
+    // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 293).
+    w.waves = p.Dqk > 256 ? (w.kept ? 1 : 8) : rows <= 32 ? 1 : 2;
+    // what a CU holds at once, by LDS and by registers
+    const int tile_bytes = kSwTile * p.Dqk * 2;
+    const int lds = w.kept ? sweep_stages(p.Dqk, kModeKeep) * tile_bytes : sweep_stages(p.Dqk, kModeWeights) * tile_bytes + kSwChunk * kSwTile * 4 + 3 * w.waves * kSwTile * 4;
+    const int waves_per_cu = 4 * sweep_waves_per_simd(p.Dqk);
+    int per_cu = (159 << 10) / lds;
+    if (per_cu > waves_per_cu / w.waves) per_cu = waves_per_cu / w.waves;
     if (per_cu < 1) per_cu = 1;
     w.W = 256 * per_cu / p.Hkv;
     if (w.W < 1) w.W = 1;
@@ -363,7 +537,9 @@ inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     const size_t per_head = static_cast<size_t>(p.Hq) * p.T;          // Hkv * G * T
     w.off_part = up(sizeof(int32_t) * (static_cast<size_t>(p.B) + 2));
     w.off_lse = w.off_part + up(sizeof(float2) * (static_cast<size_t>(w.W) + p.B) * per_head);
-    w.total = w.off_lse + up(sizeof(float) * static_cast<size_t>(p.B) * per_head);
+    w.off_scores = w.off_lse + up(sizeof(float) * static_cast<size_t>(p.B) * per_head);
+    w.total = w.off_scores + sizeof(float) * w.kept * static_cast<size_t>(p.B) * p.Hkv * p.max_pages_per_seq * p.page_size;
+    w.total = up(w.total);
     return w;
 }
 
@@ -382,13 +558,35 @@ static int check_kv_weights_params(const seer_attn_params* p) {
     return SEER_OK;
 }
 
-template <int DQK, int NW>
-hipError_t launch_kv_weights(const KvWeightsArgs& a, hipStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(a.W) * static_cast<unsigned>(a.Hkv)), block(NW * kWave);
-    hipLaunchKernelGGL((kv_sweep<DQK, NW, false>), grid, block, 0, stream, a);
+static void launch_kv_lse(const KvWeightsArgs& a, hipStream_t stream) {
     const unsigned groups = static_cast<unsigned>((a.G * a.T + kLseRows - 1) / kLseRows);
     hipLaunchKernelGGL(kv_lse, dim3(static_cast<unsigned>(a.B) * static_cast<unsigned>(a.Hkv) * groups), dim3(kLseThreads), 0, stream, a);
-    hipLaunchKernelGGL((kv_sweep<DQK, NW, true>), grid, block, 0, stream, a);
+}
+template <int DQK, int NW>
+hipError_t launch_kv_weights(const KvWeightsArgs& a, int kept, hipStream_t stream) {
+    const dim3 grid(static_cast<unsigned>(a.W) * static_cast<unsigned>(a.Hkv)), block(NW * kWave);
+    if constexpr (NW == 1) {
+        const int64_t heads = static_cast<int64_t>(a.B) * a.Hkv, most = (8192 + heads - 1) / heads, chunks = (a.ldw + kApplyPositions - 1) / kApplyPositions;
+        const int parts = static_cast<int>(chunks < most ? chunks : most);
+        const dim3 apply(static_cast<unsigned>(heads * parts));
+#define SEER_KEEP(KEPT)                                                                                       \
+    if constexpr (KEPT <= DQK / 8)                                                                            \
+        if (kept == KEPT) {                                                                                   \
+            hipLaunchKernelGGL((kv_sweep<DQK, 1, kModeKeep, KEPT>), grid, block, 0, stream, a);                \
+            launch_kv_lse(a, stream);                                                                         \
+            hipLaunchKernelGGL((kv_apply<KEPT>), apply, dim3(kApplyThreads), 0, stream, a, parts);             \
+            return hipGetLastError();                                                                         \
+        }
+        SEER_KEEP(4)
+        SEER_KEEP(8)
+        SEER_KEEP(16)
+#undef SEER_KEEP
+    }
+    if constexpr (DQK <= 256 || NW == 8) {
+        hipLaunchKernelGGL((kv_sweep<DQK, NW, kModeSums, 0>), grid, block, 0, stream, a);
+        launch_kv_lse(a, stream);
+        hipLaunchKernelGGL((kv_sweep<DQK, NW, kModeWeights, 0>), grid, block, 0, stream, a);
+    }
     return hipGetLastError();
 }
 
@@ -420,20 +618,23 @@ extern "C" int seer_kv_weights(float* weights, const void* q, const void* k_page
     a.line = reinterpret_cast<int32_t*>(ws);
     a.part = reinterpret_cast<float2*>(ws + w.off_part);
     a.lse = reinterpret_cast<float*>(ws + w.off_lse);
+    a.scores = reinterpret_cast<float*>(ws + w.off_scores);
     a.ldw = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size;
     a.B = p->B, a.T = p->T, a.Hq = p->Hq, a.Hkv = p->Hkv, a.G = p->Hq / p->Hkv, a.P = p->page_size;
     a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq, a.max_ctx = static_cast<int>(a.ldw);
     a.W = w.W, a.block_rows = 32 * w.waves;
+
     a.scale_log2 = p->scale * seer::kLog2e, a.decay = decay;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
 #define SEER_SWEEP(DQK, NW) \
-    if (p->Dqk == DQK && w.waves == NW) return static_cast<int>(seer::launch_kv_weights<DQK, NW>(a, stream));
-#define SEER_SWEEPS(DQK) SEER_SWEEP(DQK, 1) SEER_SWEEP(DQK, 2) SEER_SWEEP(DQK, 4)
+    if (p->Dqk == DQK && w.waves == NW) return static_cast<int>(seer::launch_kv_weights<DQK, NW>(a, w.kept, stream));
+#define SEER_SWEEPS(DQK) SEER_SWEEP(DQK, 1) SEER_SWEEP(DQK, 2)
     SEER_SWEEPS(64)
     SEER_SWEEPS(128)
     SEER_SWEEPS(192)
     SEER_SWEEPS(256)
-    SEER_SWEEPS(576)
+    SEER_SWEEP(576, 1)
+    SEER_SWEEP(576, 8)
 #undef SEER_SWEEPS
 #undef SEER_SWEEP
     return SEER_EUNSUPPORTED;
