@@ -502,6 +502,97 @@ __global__ __launch_bounds__(kApplyThreads) void kv_apply(KvWeightsArgs a, int p
         }
 }
 
+// Short block tables: one workgroup per request and KV head keeps all scores in LDS, and the three launches become one.  Wave i takes tiles i, i + 4, .. (the keys
+// go from memory to the operand registers, the next tile's while this one is multiplied), then a wave each row for its denominator, then a
+// thread each position for its sum.  Against three launches: 4 requests of 64 .. 512 tokens, 8/2 heads, 20 rows at most 12.4 | 17.3 us, 64 of them with 32/8
+// heads 20.3 | 30.6; but 16 of up to 3000 tokens with 4 rows 40.4 | 26.3 and 16 of up to 400 with 36 rows 21.9 | 18.9.
+constexpr int kShortWaves = 4, kShortPositions = 512, kShortRows = 32, kShortScores = 16000;      // of the table, rows, scores in LDS at most
+inline bool weights_short(int rows, int Dqk, int64_t positions) {
+    return Dqk <= 256 && positions <= kShortPositions && rows <= kShortRows && (positions + 36) * rows <= kShortScores;
+}
+
+template <int DQK>
+__global__ __launch_bounds__(kShortWaves * kWave) void kv_short(KvWeightsArgs a, int stride) {
+    extern __shared__ __attribute__((aligned(16))) float s_score[];       // [rows][stride]: stride positions, a multiple of 32 and 4 more
+    __shared__ float s_lse[kShortRows];
+    constexpr int kSteps = DQK / 16;
+    const int b = blockIdx.x / a.Hkv, kvh = blockIdx.x - b * a.Hkv, tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    bool bad, wrong;
+    const StepRows step = step_rows(a, b, bad);
+    const int slot = step_slot(a, b, step.rows, wrong);
+    if (bad || wrong) {
+        if (tid == 0 && a.status) atomicOr(a.status, bad ? 1 : 4);
+        return;
+    }
+    const int n = step.n, rows = step.rows, R = rows * a.G, first_own = n - rows, n_tiles = (n + kSwTile - 1) / kSwTile, last_page = (n - 1) / a.P;
+    const int32_t* __restrict__ table = a.block_table + static_cast<size_t>(b) * a.max_pages;
+    int found = 0;
+    auto load_tile = [&](int t, u32x4 (&k)[kSteps]) __attribute__((always_inline)) {        // (behind the last one: it again)
+        const int tok = min(t, n_tiles - 1) * kSwTile + ln, lp = tok / a.P;
+        int pg = table[min(lp, a.max_pages - 1)];
+        if (pg < 0 || pg >= a.num_pages) {
+            if (lp <= last_page) found |= 2;
+            pg = min(max(pg, 0), a.num_pages - 1);
+        }
+        const u32x4* from = reinterpret_cast<const u32x4*>(
+            static_cast<const uint16_t*>(a.k_pages) + ((static_cast<size_t>(pg) * a.Hkv + kvh) * a.P + (tok - lp * a.P)) * DQK) + lg;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) k[kk] = from[2 * kk];
+    };
+    u32x4 key[2][kSteps];
+    if (wave < n_tiles) load_tile(wave, key[0]);
+    const int r = ln, rc = min(r, R - 1), i_row = rc / a.G;
+    const int t_slot = __builtin_amdgcn_ds_bpermute(i_row << 2, slot), seen = first_own + i_row + 1;
+    const u32x4* from = reinterpret_cast<const u32x4*>(
+        static_cast<const uint16_t*>(a.q) + ((static_cast<size_t>(b) * a.T + t_slot) * a.Hq + kvh * a.G + (rc - i_row * a.G)) * DQK) + lg;
+    u32x4 q[kSteps];
+#pragma unroll
+    for (int kk = 0; kk < kSteps; ++kk) q[kk] = from[2 * kk];
+    auto scores = [&](int t, const u32x4 (&k)[kSteps]) __attribute__((always_inline)) {
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int kk = 0; kk < kSteps; ++kk) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[kk]), as_bf16x8(q[kk]), s, 0, 0, 0);
+        if (r < R) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int tok = t * kSwTile + (i >> 2) * 8 + lg * 4;
+                f32x4 v;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[x] = tok + x < seen ? s[i + x] * a.scale_log2 : kNegInf;
+                *reinterpret_cast<f32x4*>(&s_score[r * stride + tok]) = v;
+            }
+        }
+    };
+    for (int t = wave; t < n_tiles; t += 2 * kShortWaves) {            // two tiles in turn, each requested a tile ahead
+        load_tile(t + kShortWaves, key[1]);
+        scores(t, key[0]);
+        load_tile(t + 2 * kShortWaves, key[0]);
+        if (t + kShortWaves < n_tiles) scores(t + kShortWaves, key[1]);
+    }
+    __syncthreads();
+    for (int r = wave; r < R; r += kShortWaves) {
+        float m = kNegInf, l = 0.f;
+        for (int j = lane; j < n; j += kWave) m = fmaxf(m, s_score[r * stride + j]);
+        m = wave_max(m);
+        for (int j = lane; j < n; j += kWave) l += fast_exp2(s_score[r * stride + j] - (m == kNegInf ? 0.f : m));
+        l = wave_sum(l);
+        if (lane == 0) s_lse[r] = m == kNegInf && l == 0.f ? -kNegInf : m + log2f(l);      // (nothing weighs: +inf, so that exp2 gives 0)
+    }
+    __syncthreads();
+    float* __restrict__ to = a.weights + (static_cast<size_t>(b) * a.Hkv + kvh) * a.ldw;
+    for (int j = tid; j < n; j += kShortWaves * kWave) {
+        const float old = j < first_own ? to[j] : 0.f;
+        float sum = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < R; ++r) sum += fast_exp2(s_score[r * stride + j] - s_lse[r]);
+        to[j] = j < first_own ? fmaf(a.decay, old, sum) : sum;
+    }
+    if (a.status && found) atomicOr(a.status, found);
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
@@ -513,11 +604,13 @@ inline int kept_rows(int rows, int Dqk) {
 }
 struct KvWeightsLayout {
     int waves, W, kept;
+    bool whole;                        // kv_short, which needs no workspace
     size_t off_part, off_lse, off_scores, total;
 };
 inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     KvWeightsLayout w{};
     const int rows = (p.Hq / p.Hkv) * p.T;
+    w.whole = weights_short(rows, p.Dqk, static_cast<int64_t>(p.max_pages_per_seq) * p.page_size);
     w.kept = kept_rows(rows, p.Dqk);
     // Waves of a workgroup.  Up to 256-wide keys: one per 32 rows that a request may have, at most two (of a step's slots only the accepted ones come, so
     // most requests have fewer: 64 requests of 72 rows at most, two waves 53 us, four 58, one 62).  Shared latent: eight, since every
@@ -626,6 +719,21 @@ extern "C" int seer_kv_weights(float* weights, const void* q, const void* k_page
 
     a.scale_log2 = p->scale * seer::kLog2e, a.decay = decay;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (w.whole) {
+        const int stride = static_cast<int>((a.ldw + 31) / 32 * 32 + 4);
+        const unsigned lds = static_cast<unsigned>(sizeof(float) * stride * a.G * a.T);
+        const dim3 grid(static_cast<unsigned>(p->B) * static_cast<unsigned>(p->Hkv)), block(seer::kShortWaves * seer::kWave);
+#define SEER_SHORT(DQK)                                                                                                        \
+    if (p->Dqk == DQK) {                                                                                                       \
+        hipLaunchKernelGGL(seer::kv_short<DQK>, grid, block, lds, stream, a, stride);                                          \
+        return static_cast<int>(hipGetLastError());                                                                            \
+    }
+        SEER_SHORT(64)
+        SEER_SHORT(128)
+        SEER_SHORT(192)
+        SEER_SHORT(256)
+#undef SEER_SHORT
+    }
 #define SEER_SWEEP(DQK, NW) \
     if (p->Dqk == DQK && w.waves == NW) return static_cast<int>(seer::launch_kv_weights<DQK, NW>(a, w.kept, stream));
 #define SEER_SWEEPS(DQK) SEER_SWEEP(DQK, 1) SEER_SWEEP(DQK, 2)

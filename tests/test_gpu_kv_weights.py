@@ -94,9 +94,21 @@ def test_many_rows_of_one_head(D, Hq, rows):
     check(build(3, rows, Hq, 1, D, 16, [rows + 200, rows, 1100], rows, True))
 
 
-def test_lengths_from_one_token_on():
-    check(build(40, 1, 8, 2, 128, 16, list(range(1, 41)), 3))
-    check(build(40, 4, 8, 2, 128, 16, list(range(4, 44)), 3, True))
+WIDER = pytest.mark.parametrize("extra", [0, 40], ids=["short table", "long table"])       # (tables of up to 512 positions have a kernel of their own)
+
+
+@WIDER
+def test_lengths_from_one_token_on(extra):
+    check(build(40, 1, 8, 2, 128, 16, list(range(1, 41)), 3, extra_pages=extra))
+    check(build(40, 4, 8, 2, 128, 16, list(range(4, 44)), 3, True, extra_pages=extra))
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,P", [(64, 8, 2, 16), (128, 29, 1, 20), (192, 6, 2, 64), (256, 8, 8, 1), (128, 8, 2, 512)])
+@pytest.mark.parametrize("T,path", [(1, False), (4, True), (8, True)])
+def test_short_tables(D, Hq, Hkv, P, T, path):
+    if Hq // Hkv * T > 32:
+        T = 32 // (Hq // Hkv)
+    check(build(7, T, Hq, Hkv, D, P, [T, 31 + T, 32 + T, 33 + T, 300, 499, 500], D + T, path and T > 1), 0.75)
 
 
 def test_more_requests_than_lanes_and_than_stretches():
@@ -117,9 +129,10 @@ def test_shared_pages_and_tables_wider_than_the_requests():
     check(build(6, 5, 8, 2, 128, 16, [600, 610, 640, 515, 520, 900], 10, True, share=32, extra_pages=9))
 
 
+@WIDER
 @pytest.mark.parametrize("decay", [0.0, 0.5, 1.0])
-def test_decay_and_positions_behind_the_end(decay):
-    s = build(3, 4, 8, 2, 128, 16, [100, 37, 4], 11, extra_pages=3)
+def test_decay_and_positions_behind_the_end(decay, extra):
+    s = build(3, 4, 8, 2, 128, 16, [100, 37, 4], 11, extra_pages=3 + extra)
     s["w"][:, :, 100:] = float("nan")                        # never read, never written
     from paper_2511_14617_amd import binding
     s["w"][0, :, 96:100] = float("nan")                      # the step's own entries need not be there
@@ -133,8 +146,9 @@ def test_decay_and_positions_behind_the_end(decay):
     assert np.array_equal(got[1, :, 37:100], want[1, :, 37:100])
 
 
-def test_keys_behind_the_end_may_hold_anything():
-    s = build(3, 2, 8, 2, 128, 16, [17, 33, 250], 12)
+@WIDER
+def test_keys_behind_the_end_may_hold_anything(extra):
+    s = build(3, 2, 8, 2, 128, 16, [17, 33, 250], 12, extra_pages=extra)
     clean = check(s)
     table, ctx = s["table"].cpu().numpy(), s["ctx"].cpu().numpy()
     for b, n in enumerate(ctx):
@@ -163,12 +177,13 @@ def test_the_weights_of_a_step_sum_to_its_rows():
         assert (total - rows[b]).abs().max() < 1e-4 * rows[b]
 
 
-def test_unusable_requests_are_left_alone_and_reported():
+@WIDER
+def test_unusable_requests_are_left_alone_and_reported(extra):
     from paper_2511_14617_amd import binding
-    s = build(8, 5, 8, 2, 128, 16, [100] * 8, 16, True)
+    s = build(8, 5, 8, 2, 128, 16, [100] * 8, 16, True, extra_pages=extra)
     s["alen"][:], s["path"][:] = 2, torch.tensor([0, 1, 3, -1, -1], dtype=torch.int32)
     clean = s["w"].clone()
-    for what, value, bit in (("ctx", 2, 1), ("ctx", 0, 1), ("ctx", -5, 1), ("ctx", 113, 1), ("alen", -1, 1), ("alen", 5, 1), ("path", [1, 2, 3, -1, -1], 4),
+    for what, value, bit in (("ctx", 2, 1), ("ctx", 0, 1), ("ctx", -5, 1), ("ctx", 113 + 16 * extra, 1), ("alen", -1, 1), ("alen", 5, 1), ("path", [1, 2, 3, -1, -1], 4),
                              ("path", [0, 2, 2, -1, -1], 4), ("path", [0, 3, 1, -1, -1], 4), ("path", [0, 1, 5, -1, -1], 4), ("path", [0, -1, 1, 2, 3], 4)):
         t = dict(s, ctx=s["ctx"].clone(), alen=s["alen"].clone(), path=s["path"].clone())
         t[what][3] = torch.tensor(value, dtype=torch.int32)
@@ -182,9 +197,10 @@ def test_unusable_requests_are_left_alone_and_reported():
         assert (np.abs(w.double().cpu().numpy() - want) <= tol)[ok].all()
 
 
-def test_page_ids_outside_the_pool_are_clamped_and_reported():
+@WIDER
+def test_page_ids_outside_the_pool_are_clamped_and_reported(extra):
     from paper_2511_14617_amd import binding
-    s = build(3, 1, 8, 2, 128, 16, [100, 200, 300], 17, extra_pages=2)
+    s = build(3, 1, 8, 2, 128, 16, [100, 200, 300], 17, extra_pages=2 + extra)
     s["table"][:, -2:] = 1 << 30                             # behind the end: never looked at
     check(s)
     s["table"][1, 3], s["table"][1, 7] = -1, 1 << 30
@@ -195,9 +211,10 @@ def test_page_ids_outside_the_pool_are_clamped_and_reported():
     assert status.item() == 2 and torch.equal(w, want)
 
 
-def test_not_finite_keys_and_queries_show_in_their_head_only():
+@WIDER
+def test_not_finite_keys_and_queries_show_in_their_head_only(extra):
     from paper_2511_14617_amd import binding
-    s = build(2, 1, 8, 2, 128, 16, [100, 100], 18)
+    s = build(2, 1, 8, 2, 128, 16, [100, 100], 18, extra_pages=extra)
     clean = check(s)
     s["k"][s["table"][0, 2].item(), 1, 5, 7] = float("nan")
     w = s["w"].clone()
@@ -205,9 +222,10 @@ def test_not_finite_keys_and_queries_show_in_their_head_only():
     assert torch.isnan(w[0, 1, :100]).all() and torch.equal(w[0, 0], clean[0, 0]) and torch.equal(w[1], clean[1])
 
 
-def test_a_row_whose_scores_are_all_minus_infinity_adds_nothing():
+@WIDER
+def test_a_row_whose_scores_are_all_minus_infinity_adds_nothing(extra):
     from paper_2511_14617_amd import binding
-    s = build(1, 2, 4, 1, 64, 16, [50], 19)
+    s = build(1, 2, 4, 1, 64, 16, [50], 19, extra_pages=extra)
     s["k"].abs_()
     s["q"][0, :, 2] = 0.0
     s["q"][0, :, 2, 3] = -float("inf")                        # (positive keys: every score of this head is -inf)
