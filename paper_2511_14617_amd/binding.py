@@ -463,6 +463,25 @@ def seer_history_append(tokens: torch.Tensor, seq_start: torch.Tensor, seq_len: 
                                    _ptr(pattern), _ptr(pattern_len), _ptr(status), _stream_handle(stream)))
 
 
+def _here(stream: Optional[torch.cuda.Stream], **tensors: Optional[torch.Tensor]) -> None:
+    """A launch goes to the current device: what it is given must be there."""
+    device = torch.cuda.current_device()
+    if stream is not None and stream.device_index != device:
+        raise ValueError("stream: want one of the current device, cuda:%d, got one of cuda:%d" % (device, stream.device_index))
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != device:
+            raise ValueError("%s: want it on the current device, cuda:%d, got %s" % (name, device, t.device))
+
+
+def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """New memory of the stream that writes it: what the allocator hands out on the current stream may have work pending there, and a workspace
+    that is given back there may be handed out again, while the other stream is still at work."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _logprob_rows(t: torch.Tensor, name: str) -> int:
     """Elements from one row to the next of logits [B,T,V] or [N,V] (rows may be apart, their elements not)."""
     ld = t.stride(-2) if t.shape[-2] > 1 else (t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else max(t.stride(-2), t.shape[-1]))
@@ -501,9 +520,9 @@ def seer_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, accepted_pat
         _want(accepted_path, torch.int32, lead, "accepted_path")
     dev = logits.device
     if out is None:
-        out = tuple(torch.empty(lead, dtype=torch.float32, device=dev) for _ in range(3))
-        out += (torch.empty((*lead, top_n), dtype=torch.float32, device=dev) if top_n > 0 else None,
-                torch.empty((*lead, top_n), dtype=torch.int32, device=dev) if top_n > 0 else None)
+        out = _empty((3, *lead), torch.float32, dev, stream).unbind()      # (one allocation: short calls are bound by the host)
+        out += (_empty((*lead, top_n), torch.float32, dev, stream) if top_n > 0 else None,
+                _empty((*lead, top_n), torch.int32, dev, stream) if top_n > 0 else None)
     else:
         for t, name in zip(out[:3], ("logprob", "entropy", "logsumexp")):
             _want(t, torch.float32, lead, name)
@@ -512,7 +531,9 @@ def seer_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, accepted_pat
             _want(out[4], torch.int32, (*lead, top_n), "top_token")
     if workspace is None:
         need = int(lib.seer_token_logprobs_workspace(ctypes.byref(p)))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        workspace = _empty(max(need, 256), torch.uint8, dev, stream)
+    _here(stream, logits=logits, tokens=tokens, accepted_path=accepted_path, logprob=out[0], entropy=out[1], logsumexp=out[2],
+          top_logprob=out[3] if top_n > 0 else None, top_token=out[4] if top_n > 0 else None, workspace=workspace)
     _check(lib.seer_token_logprobs(_ptr(logits), _ptr(tokens), _ptr(accepted_path), ctypes.byref(p), _ptr(out[0]), _ptr(out[1]),
                                    _ptr(out[2]), _ptr(out[3]) if top_n > 0 else None, _ptr(out[4]) if top_n > 0 else None,
                                    _ptr(workspace), workspace.numel(), _stream_handle(stream)))
@@ -533,10 +554,12 @@ def seer_token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, logsume
         if t is not None:
             _want(t, torch.float32, lead, name)
     if out is None:
-        out = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=logits.device)
+        out = _empty(tuple(logits.shape), logits.dtype, logits.device, stream)
     elif out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out: want %s%s, got %s%s" % (logits.dtype, tuple(logits.shape), out.dtype, tuple(out.shape)))
-    _check(lib.seer_token_logprobs_grad(_ptr(out), _logprob_rows(out, "out"), _ptr(logits), _ptr(tokens), _ptr(logsumexp), _ptr(entropy),
+    out_ld = _logprob_rows(out, "out")
+    _here(stream, logits=logits, tokens=tokens, logsumexp=logsumexp, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy, out=out)
+    _check(lib.seer_token_logprobs_grad(_ptr(out), out_ld, _ptr(logits), _ptr(tokens), _ptr(logsumexp), _ptr(entropy),
                                         _ptr(grad_logprob), _ptr(grad_entropy), ctypes.byref(p), _stream_handle(stream)))
     return out
 
@@ -569,7 +592,9 @@ def seer_kv_weights(weights: torch.Tensor, q: torch.Tensor, k_pages: torch.Tenso
         _want(status, torch.int32, (1,), "status")
     if workspace is None:
         need = int(lib.seer_kv_weights_workspace(ctypes.byref(p)))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(need, 256), torch.uint8, q.device, stream)
+    _here(stream, weights=weights, q=q, k_pages=k_pages, block_table=block_table, ctx_len=ctx_len, accepted_len=accepted_len,
+          accepted_path=accepted_path, status=status, workspace=workspace)
     _check(lib.seer_kv_weights(_ptr(weights), _ptr(q), _ptr(k_pages), _ptr(block_table), _ptr(ctx_len), _ptr(accepted_len),
                                _ptr(accepted_path), float(decay), ctypes.byref(p), _ptr(status), _ptr(workspace),
                                workspace.numel(), _stream_handle(stream)))
@@ -608,18 +633,20 @@ def seer_kv_evict(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_
     if new_weights is not None:
         _want(new_weights, torch.float32, (B, Hkv, max_pages * P), "new_weights")
     if new_ctx_len is None:
-        new_ctx_len = torch.empty(B, dtype=torch.int32, device=k_pages.device)
+        new_ctx_len = _empty(B, torch.int32, k_pages.device, stream)
     else:
         _want(new_ctx_len, torch.int32, (B,), "new_ctx_len")
     if kept is None:
-        kept = torch.empty((B, Hkv, max(e.budget, 0)), dtype=torch.int32, device=k_pages.device)
+        kept = _empty((B, Hkv, max(e.budget, 0)), torch.int32, k_pages.device, stream)
     else:
         _want(kept, torch.int32, (B, Hkv, e.budget), "kept")
     if status is not None:
         _want(status, torch.int32, (1,), "status")
     if workspace is None:
         need = int(lib.seer_kv_evict_workspace(ctypes.byref(p), ctypes.byref(e)))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=k_pages.device)
+        workspace = _empty(max(need, 256), torch.uint8, k_pages.device, stream)
+    _here(stream, k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, weights=weights, keep_first=keep_first if per_request else None,
+          new_weights=new_weights, new_ctx_len=new_ctx_len, kept=kept, status=status, workspace=workspace)
     _check(lib.seer_kv_evict(ctypes.byref(p), ctypes.byref(e), _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(ctx_len),
                              _ptr(keep_first) if per_request else None, _ptr(weights), _ptr(new_ctx_len), _ptr(new_weights), _ptr(kept),
                              _ptr(status), _ptr(workspace), workspace.numel(), _stream_handle(stream)))

@@ -179,3 +179,35 @@ def test_kv_evict_workspace_and_argument_errors_before_any_launch(lib):
     assert run(attn(), ev(), k=FAKE + 8) == b.SEER_EALIGN
     assert run(attn(), ev(), w=FAKE + 2) == b.SEER_EALIGN
     assert run(attn(B=0), ev()) == b.SEER_OK
+
+
+def test_tensors_and_streams_of_another_device_are_refused(monkeypatch):
+    import torch
+    from paper_2511_14617_amd import binding as b
+
+    class On:
+        def __init__(self, i):
+            self.device, self.device_index = "cuda:%d" % i, i
+
+        def get_device(self):
+            return self.device_index
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    b._here(None, logits=On(1), tokens=On(1), out=None)
+    b._here(On(1), logits=On(1))
+    with pytest.raises(ValueError, match="tokens: want it on the current device, cuda:1, got cuda:0"):
+        b._here(None, logits=On(1), tokens=On(0))
+    with pytest.raises(ValueError, match="stream"):
+        b._here(On(0), logits=On(1))
+
+
+@pytest.mark.parametrize("name", ["seer_token_logprobs", "seer_token_logprobs_grad", "seer_kv_weights", "seer_kv_evict"])
+def test_every_tensor_of_a_call_is_looked_at(name):
+    """Each tensor argument of the call, and each tensor that it makes, stands in its check of devices."""
+    import inspect
+    from paper_2511_14617_amd import binding as b
+    source = inspect.getsource(getattr(b, name))
+    looked = source[source.index("    _here("):source.index("    _check(lib." + name)]
+    named = {n for n, a in inspect.signature(getattr(b, name)).parameters.items() if "Tensor" in str(a.annotation) and "Tuple" not in str(a.annotation)}
+    assert named and all(re.search(r"\b%s=" % n, looked) for n in named), named
+    assert "torch.empty(" not in source
