@@ -179,13 +179,13 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
             }
     };
     every(add);
+    if (rest < end) add(x_rest);
     if (!usual || __any(s != s)) {
         l = s = 0.f;
         every(add_with_care);
         add_with_care(x_rest);
         l = all_sum(l), s = all_sum(s);
     } else {
-        if (rest < end) add(x_rest);
         l = all_sum(l), s = all_sum(s);
         // from c to m itself
         const float off = fmaf(m, scale, -c), f = fast_exp2(-off);

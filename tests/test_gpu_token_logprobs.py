@@ -141,6 +141,20 @@ def test_masked_and_equal_logits(N, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", DT, ids=["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 3, 1001, 4099, 16391])
+def test_masked_logits_behind_the_last_whole_vector(V, dtype):
+    x, tok = make(6, V, dtype, V)
+    x = x.clone()
+    x[0, -1] = -float("inf")
+    x[1, V // 4 * 4:] = -float("inf")
+    x[2, V // 8 * 8:] = -float("inf")
+    x[3, :V // 8 * 8] = -float("inf")
+    x[4, -1] = torch.finfo(dtype).min
+    tok[:] = 0
+    check(x, tok, 1.25, min(3, V))                          # (below 1 the lowest value over the temperature leaves the floats)
+
+
+@pytest.mark.parametrize("dtype", DT, ids=["f32", "bf16"])
 def test_few_distinct_values_give_the_lowest_indices(dtype):
     g = torch.Generator(device="cuda").manual_seed(6)
     x = torch.randint(0, 4, (3, 70001), device="cuda", generator=g).to(dtype)
