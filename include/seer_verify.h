@@ -437,7 +437,8 @@ SEER_API int seer_history_append(int32_t* tokens, const int32_t* seq_start, int3
 #define SEER_MAX_ALTERNATIVES 32
 #define SEER_LOGPROB_MAX_V (1 << 24)
 typedef struct seer_logprob_params {
-    int32_t B, T;              /* B*T entries; any T >= 1                                      */
+    int32_t B, T;              /* B*T entries; any T >= 1; fewer than 2^24 pieces of a row, the pieces
+                                * of at least 4096 logits (SEER_ESHAPE beyond)                 */
     int32_t V;                 /* logits of a row, 1 .. SEER_LOGPROB_MAX_V                     */
     int64_t ld;                /* elements from one row of logits to the next, >= V            */
     int32_t dtype;             /* of the logits (and their gradient): SEER_F32 or SEER_BF16    */
@@ -503,7 +504,8 @@ SEER_API size_t seer_kv_weights_workspace(const seer_attn_params* p);
  *  block_table, ctx_len  as for seer_verify_attention, ctx_len as seer_kv_commit left it
  *  accepted_len, accepted_path  device, as written by seer_accept; both NULL or neither
  *  decay          0 .. 1; 1 = plain sums
- *  p              B, T, Hq, Hkv, Dqk (64, 128, 192, 256 or 576), page_size (any), num_pages, max_pages_per_seq, scale are used
+ *  p              B, T, Hq, Hkv, Dqk (64, 128, 192, 256 or 576), page_size (any), num_pages, max_pages_per_seq, scale are used;
+ *                 B*Hkv times a KV head's rows in eights below 2^24 - 8192 (SEER_ESHAPE beyond)
  *  status         device [1] int32 or NULL; bits are OR-ed in: 1 = a ctx_len below R or beyond the block table, or an accepted_len
  *                 out of range, 4 = accepted_path malformed (such requests are left untouched), 2 = a page id outside the pool
  *                 (it is clamped into the pool).  The caller clears it.
@@ -540,7 +542,8 @@ typedef struct seer_evict_params {
 SEER_API size_t seer_kv_evict_workspace(const seer_attn_params* p, const seer_evict_params* e);
 
 /*
- *  p              B, Hkv, Dqk, Dv (multiples of 8), page_size (any), num_pages, max_pages_per_seq, kv_shared_latent are used
+ *  p              B, Hkv, Dqk, Dv (multiples of 8), page_size (any), num_pages, max_pages_per_seq, kv_shared_latent are used;
+ *                 B*Hkv below 2^19, and below 2^24 - 8192 when multiplied by the table's positions / 4096 or a row's bytes / 128
  *  k_pages, v_pages  device, 16-bit elements, modified in place; v_pages NULL iff kv_shared_latent
  *  block_table    device [B,max_pages_per_seq] int32;  ctx_len device [B] int32
  *  keep_first     device [B] int32 or NULL (e->keep_first for every request)

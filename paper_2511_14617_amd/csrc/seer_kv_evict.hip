@@ -632,6 +632,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a) {
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+inline int evict_columns(int chunks) { return (chunks * 16 + kColumn - 1) / kColumn; }
+
 static int check_evict_params(const seer_attn_params* p, const seer_evict_params* e) {
     if (!p || !e) return SEER_EINVAL;
     if (p->B < 0 || p->num_pages < 1 || p->max_pages_per_seq < 1 || p->page_size < 1) return SEER_EINVAL;
@@ -641,7 +643,10 @@ static int check_evict_params(const seer_attn_params* p, const seer_evict_params
     if (static_cast<int64_t>(e->keep_first) + e->keep_last > e->budget) return SEER_ESHAPE;
     const int64_t ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size;
     if (ctx > 0x7fffffffLL - 4096 || p->Dqk > 1 << 16 || p->Dv > 1 << 16) return SEER_ESHAPE;
-    if (static_cast<int64_t>(p->B) * p->Hkv > 0x7fffffffLL / 4096 || static_cast<int64_t>(p->B) * p->Hkv > 0x7fffffffLL / (ctx / kSegment + 2)) return SEER_ESHAPE;
+    // launches count their threads in 32 bits: up to one workgroup per segment, or per column (and the sums', and one for the other rows, 8192 on top)
+    const int64_t heads = static_cast<int64_t>(p->B) * p->Hkv, columns = e->keep_last > 0 ? evict_columns(p->Dqk / 8) + evict_columns(shared ? 0 : p->Dv / 8) + 1 : 0;
+    const int64_t most = 0xffffffffLL / 256 - 8192;
+    if (heads > 0x7fffffffLL / 4096 || heads > most / (ctx / kSegment + 1) || heads > most / (columns + 1)) return SEER_ESHAPE;
     return SEER_OK;
 }
 // Rows of one request and KV head that can move to free slots, at most.
@@ -708,8 +713,7 @@ extern "C" int seer_kv_evict(const seer_attn_params* p, const seer_evict_params*
     a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.limit = e->limit, a.budget = e->budget, a.first = e->keep_first, a.last = e->keep_last;
     a.k_chunks = p->Dqk / 8, a.v_chunks = shared ? 0 : p->Dv / 8;
-    auto columns = [](int chunks) { return (chunks * 16 + seer::kColumn - 1) / seer::kColumn; };
-    a.columns = e->keep_last > 0 ? columns(a.k_chunks) + columns(a.v_chunks) + 1 : 0;
+    a.columns = e->keep_last > 0 ? seer::evict_columns(a.k_chunks) + seer::evict_columns(a.v_chunks) + 1 : 0;
     // workgroups for the other rows: one per 64 that may move, as long as the launch is no larger than the chip can use
     const int64_t heads = static_cast<int64_t>(p->B) * p->Hkv, most = (8192 + heads - 1) / heads;
     int64_t rows = (a.capacity + seer::kMoveRows - 1) / seer::kMoveRows;

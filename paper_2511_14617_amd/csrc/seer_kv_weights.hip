@@ -648,6 +648,9 @@ static int check_kv_weights_params(const seer_attn_params* p) {
     const int64_t blocks = (static_cast<int64_t>(p->Hq / p->Hkv) * p->T + 31) / 32;
     if ((static_cast<int64_t>(p->B) + 1) * (ctx / 32 + 1) > 0x7fffffffLL / 2 / blocks || static_cast<int64_t>(p->B) * p->Hq * p->T > 0x7fffffffLL) return SEER_ESHAPE;
     if (static_cast<int64_t>(p->num_pages) * p->Hkv > 0xffffffffLL / p->page_size) return SEER_ESHAPE;
+    // and so are the threads of a launch (kv_lse and kv_apply, whose 8192 workgroups come on top, have the most workgroups for many requests)
+    const int64_t heads = static_cast<int64_t>(p->B) * p->Hkv, groups = (static_cast<int64_t>(p->Hq / p->Hkv) * p->T + kLseRows - 1) / kLseRows;
+    if (heads * groups > 0xffffffffLL / 256 - 8192) return SEER_ESHAPE;
     return SEER_OK;
 }
 

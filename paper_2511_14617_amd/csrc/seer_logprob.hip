@@ -476,7 +476,9 @@ static int check_logprob_params(const seer_logprob_params* p) {
     if (p->T < 1 || p->top_n < 0 || p->top_n > SEER_MAX_ALTERNATIVES || p->top_n > p->V || p->ld < p->V) return SEER_ESHAPE;
     if (p->dtype != SEER_F32 && p->dtype != SEER_BF16) return SEER_EUNSUPPORTED;
     if (p->V > SEER_LOGPROB_MAX_V) return SEER_EUNSUPPORTED;
-    if (static_cast<int64_t>(p->B) * p->T > 0x7fffffffLL || (p->B > 0 && static_cast<int64_t>(p->B) * p->T * lp_num_chunks(*p) > 0x7fffffffLL)) return SEER_ESHAPE;
+    // a launch counts its threads in 32 bits
+    const int64_t rows = static_cast<int64_t>(p->B) * p->T, most = 0xffffffffLL / kLpThreads;
+    if (rows > most || (p->B > 0 && rows * lp_num_chunks(*p) > most)) return SEER_ESHAPE;
     if (!(1.0f / p->temperature < 2.0e38f)) return SEER_EINVAL;          // (its reciprocal has to be finite too, also times log2 e)
     return SEER_OK;
 }

@@ -211,3 +211,22 @@ def test_every_tensor_of_a_call_is_looked_at(name):
     named = {n for n, a in inspect.signature(getattr(b, name)).parameters.items() if "Tensor" in str(a.annotation) and "Tuple" not in str(a.annotation)}
     assert named and all(re.search(r"\b%s=" % n, looked) for n in named), named
     assert "torch.empty(" not in source
+
+
+def test_launches_that_a_device_cannot_count_are_refused(lib):
+    """2^32 threads or more in one launch: refused on the host, below that the call has a workspace."""
+    from paper_2511_14617_amd import binding as b
+    lps, kvw, kve = b.seer_token_logprobs_workspace, b.seer_kv_weights_workspace, b.seer_kv_evict_workspace
+    rows = (2 ** 32 - 1) // 256
+    assert lps(lp(B=rows, T=1, V=100, ld=100)) > 0 and lps(lp(B=rows + 1, T=1, V=100, ld=100)) == 0
+    assert lps(lp(B=rows // 2, T=1, V=20000, ld=20000)) > 0 and lps(lp(B=rows // 2 + 1, T=1, V=20000, ld=20000)) == 0
+    heads = rows - 8192
+    one = dict(T=1, Hq=1, Hkv=1, max_pages_per_seq=1)
+    assert kvw(attn(B=heads, **one)) > 0 and kvw(attn(B=heads + 1, **one)) == 0
+    assert kvw(attn(B=heads // 2, T=16, Hq=1, Hkv=1, max_pages_per_seq=1)) > 0 and kvw(attn(B=heads // 2 + 1, T=16, Hq=1, Hkv=1, max_pages_per_seq=1)) == 0
+    assert kve(attn(B=(1 << 19) - 1, **one), ev()) > 0 and kve(attn(B=1 << 19, **one), ev()) == 0
+    wide = dict(one, Dqk=8192, Dv=8192)                                                                     # 257 columns of 128 bytes, one workgroup more
+    assert kve(attn(B=heads // 258, **wide), ev()) > 0 and kve(attn(B=heads // 258 + 1, **wide), ev()) == 0
+    assert kve(attn(B=heads // 258 + 1, **wide), ev(keep_last=0)) > 0
+    long = dict(one, max_pages_per_seq=1 << 14)                                                             # 64 segments and one
+    assert kve(attn(B=heads // 65, **long), ev(keep_last=0)) > 0 and kve(attn(B=heads // 65 + 1, **long), ev(keep_last=0)) == 0
