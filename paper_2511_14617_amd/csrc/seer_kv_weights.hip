@@ -22,6 +22,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/seer_verify.h"
 #include "seer_device.h"
 #include "seer_plan.h"
@@ -154,6 +156,30 @@ __device__ __forceinline__ f32x16 sweep_scores(int at, int k_rd, const bf16x8 (&
     return s;
 }
 
+// The same from one of the stages, which are arrays of their own so that the compiler can tell them apart and overlaps the reads with the products.
+template <int DQK, bool ROWS>
+__device__ __forceinline__ f32x16 stage_scores(const unsigned char* stage, const int (&rd)[4], const bf16x8 (&q)[DQK / 16]) {
+    constexpr int kXorBits = Keys<DQK>::kRow % 256 == 0 ? 4 : 3, kPerXor = 1 << (kXorBits - 1);
+    static_assert(kPerXor == 4, "");
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < DQK / 16; ++kk) {
+        const bf16x8 k = as_bf16x8(*reinterpret_cast<const u32x4*>(stage + rd[kk % kPerXor] + kk / kPerXor * (kPerXor * 32)));
+        s = ROWS ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[kk], k, s, 0, 0, 0) : __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, q[kk], s, 0, 0, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);      // (0x100: reads, 0x008: products)
+#pragma unroll
+    for (int h = 1; h < DQK / 64; ++h) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    return s;
+}
+
 // A word of LDS (as asm with its wait, like the tiles' reads: through the compiler it would wait for the tile loads in flight).
 __device__ __forceinline__ float lds_word(int at) {
     float v;
@@ -188,7 +214,9 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
     constexpr int kSwStages = sweep_stages(DQK, MODE);
     constexpr int kTileLoads = K::kBytes / 1024, kLoads = (kTileLoads + NW - 1) / NW;      // direct-to-LDS loads of a tile, of a wave at most
     static_assert(kSwStages == 2 || kLoads * (kSwStages - 1) < 64, "");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[kSwStages * K::kBytes];
+    constexpr bool APART = NW == 8;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[APART ? 1024 : kSwStages * K::kBytes];
+    __shared__ __attribute__((aligned(1024))) unsigned char lds_even[APART ? K::kBytes : 1], lds_odd[APART ? K::kBytes : 1];
     __shared__ float s_sums[WEIGHTS ? kSwChunk * kSwTile : 1];
     __shared__ __attribute__((aligned(16))) float s_denom[NW][WEIGHTS ? 32 : 1];       // of the waves' rows
     __shared__ float s_part[2][WEIGHTS && NW > 1 ? NW : 1][WEIGHTS && NW > 1 ? kSwTile : 1];      // the waves' sums of a tile
@@ -197,11 +225,17 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const unsigned char* __restrict__ kbase = static_cast<const unsigned char*>(a.k_pages);
-    const int lds0 = tile::lds_addr(lds);
     const int k_rd = ln * K::kRow + ((lg ^ tile::k_swz<K::kRow>(ln)) << 4);
     const bool page_pow2 = (a.P & (a.P - 1)) == 0;
     const int page_shift = __builtin_ctz(static_cast<unsigned>(a.P));
     auto page_of = [&](int tok) __attribute__((always_inline)) -> int { return page_pow2 ? tok >> page_shift : tok / a.P; };
+    int rd[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) rd[x] = k_rd ^ x << 5;
+    auto scores = [&](auto rows, const unsigned char* at, const bf16x8 (&q)[K::kSteps]) __attribute__((always_inline)) {
+        if constexpr (APART) return stage_scores<DQK, decltype(rows)::value>(at, rd, q);
+        else return sweep_scores<DQK, decltype(rows)::value>(tile::lds_addr(at), k_rd, q);
+    };
     int found = 0;                                          // status bits
 
     for_pieces<MODE != kModeWeights>(a, w, found, [&](int b, int n, int rows, int slot, int blocks, int t_begin, int t_end, int total) __attribute__((always_inline)) {
@@ -214,7 +248,7 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
             const int last_page = (n - 1) / a.P;
             int win = 0, pg_win = 0;                        // lane l holds the (clamped) page id of logical page win + l
             bool have_window = false;
-            auto issue_tile = [&](int t, int stage) __attribute__((always_inline)) {
+            auto issue_tile = [&](int t, unsigned char* to) __attribute__((always_inline)) {
                 const int tb = t * kSwTile, first = page_of(tb);
                 if (!have_window || first < win || page_of(tb + kSwTile - 1) >= win + kWave) {       // (uniform; a tile spans at most 32 pages)
                     have_window = true;
@@ -229,15 +263,25 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                 const int tok = tb + ln, lp = page_of(tok);
                 const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
                 const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + kvh) * static_cast<uint32_t>(a.P) + (tok - lp * a.P);
+                uint32_t at[kLoads];                        // (all asked for, then waited for once: a lane's value comes from another one through LDS)
 #pragma unroll
-                for (int j = 0; j < kLoads; ++j) {
-                    const int piece = wave + j * NW;
-                    if (kTileLoads % NW != 0 && piece >= kTileLoads) break;
-                    const int c = piece * kWave + lane, row = c / K::kRowChunks, pos = c - row * K::kRowChunks;
-                    const uint32_t r = __builtin_amdgcn_ds_bpermute(row << 2, row_idx);
-                    const unsigned char* src = kbase + static_cast<size_t>(r) * K::kRow + ((pos ^ tile::k_swz<K::kRow>(row)) << 4);
-                    if (stream) __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage * K::kBytes + piece * 1024), 16, 0, 2);
-                    else __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage * K::kBytes + piece * 1024), 16, 0, 0);
+                for (int j = 0; j < kLoads; ++j) at[j] = __builtin_amdgcn_ds_bpermute(((wave + j * NW) * kWave + lane) / K::kRowChunks << 2, row_idx);
+                __builtin_amdgcn_sched_barrier(0);
+                auto from = [&](int j) __attribute__((always_inline)) {
+                    const int c = (wave + j * NW) * kWave + lane, row = c / K::kRowChunks, pos = c - row * K::kRowChunks;
+                    return kbase + static_cast<size_t>(at[j]) * K::kRow + ((pos ^ tile::k_swz<K::kRow>(row)) << 4);
+                };
+                to += wave * 1024;
+                if (stream) {
+#pragma unroll
+                    for (int j = 0; j < kLoads; ++j)
+                        if (kTileLoads % NW == 0 || wave + j * NW < kTileLoads)
+                            __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(from(j)), (SEER_AS3 void*)(to + j * NW * 1024), 16, 0, 2);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kLoads; ++j)
+                        if (kTileLoads % NW == 0 || wave + j * NW < kTileLoads)
+                            __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(from(j)), (SEER_AS3 void*)(to + j * NW * 1024), 16, 0, 0);
                 }
             };
 
@@ -245,9 +289,28 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
             // barrier that follows a tile.
             auto sweep = [&](int t0, int t1, auto&& use, auto&& after) __attribute__((always_inline)) {
                 if (NW > 1) bare_barrier();                 // every wave is done with the stages
+                if constexpr (APART) {
+                    auto one = [&](int t, unsigned char* here, unsigned char* other) __attribute__((always_inline)) {
+                        wait_vmcnt<0>();
+                        __builtin_amdgcn_s_waitcnt(0xc07f);
+                        bare_barrier();
+                        if (t + 1 < t1) issue_tile(t + 1, other);
+                        if (t > t0) after(t - 1);
+                        use(t, here);
+                    };
+                    if (t0 < t1) issue_tile(t0, lds_even);
+                    for (int t = t0; t < t1; t += 2) {
+                        one(t, lds_even, lds_odd);
+                        if (t + 1 < t1) one(t + 1, lds_odd, lds_even);
+                    }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    bare_barrier();
+                    if (t1 > t0) after(t1 - 1);
+                    return;
+                }
 #pragma unroll
                 for (int s = 0; s < kSwStages - 1; ++s)
-                    if (t0 + s < t1) issue_tile(t0 + s, s);
+                    if (t0 + s < t1) issue_tile(t0 + s, lds + s * K::kBytes);
                 int stage = 0;
                 for (int t = t0; t < t1; ++t) {
                     // (this wave's loads of the tiles behind this one may be on their way; near the end none are waited for apart)
@@ -259,10 +322,10 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                         bare_barrier();
                     }
                     const int next = stage == 0 ? kSwStages - 1 : stage - 1;
-                    if (t + kSwStages - 1 < t1) issue_tile(t + kSwStages - 1, next);
+                    if (t + kSwStages - 1 < t1) issue_tile(t + kSwStages - 1, lds + next * K::kBytes);
                     __builtin_amdgcn_sched_barrier(0);
                     if (t > t0) after(t - 1);
-                    use(t, lds0 + stage * K::kBytes);
+                    use(t, lds + stage * K::kBytes);
                     __builtin_amdgcn_sched_barrier(0);
                     stage = stage + 1 == kSwStages ? 0 : stage + 1;
                 }
@@ -297,9 +360,9 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                     const int seen = first_own + min(r, R - 1) / a.G + 1;
                     float m_run = kNegInf, l_run = 0.f;
                     const bool idle = block * a.block_rows + wave * 32 >= R;      // (uniform: none of the wave's rows exists)
-                    sweep(t_begin, t_end, [&](int t, int at) __attribute__((always_inline)) {
+                    sweep(t_begin, t_end, [&](int t, const unsigned char* at) __attribute__((always_inline)) {
                         if (NW > 1 && idle) return;
-                        f32x16 s = sweep_scores<DQK, false>(at, k_rd, q);
+                        f32x16 s = scores(std::integral_constant<bool, false>{}, at, q);
                         const int tb = t * kSwTile;
                         if (tb + kSwTile > first_own + 1) {
 #pragma unroll
@@ -327,8 +390,8 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
 #pragma unroll
                 for (int i = 0; i < kRegs; ++i) m[i] = kNegInf, l[i] = 0.f;
                 float* __restrict__ to = a.scores + (static_cast<size_t>(b) * a.Hkv + kvh) * a.ldw * KEPT;
-                sweep(t_begin, t_end, [&](int t, int at) __attribute__((always_inline)) {
-                    f32x16 s = sweep_scores<DQK, true>(at, k_rd, q);
+                sweep(t_begin, t_end, [&](int t, const unsigned char* at) __attribute__((always_inline)) {
+                    f32x16 s = scores(std::integral_constant<bool, true>{}, at, q);
                     const int tok = t * kSwTile + ln;
 #pragma unroll
                     for (int i = 0; i < kRegs; ++i) s[i] *= a.scale_log2;
@@ -374,12 +437,12 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                         const int denom_at = tile::lds_addr(reinterpret_cast<const unsigned char*>(&s_denom[wave][lg * 4]));
                         const int row_i = min(r, R - 1) / a.G;
                         const bool idle = block * a.block_rows + wave * 32 >= R;
-                        sweep(c0, c1, [&](int t, int at) __attribute__((always_inline)) {
+                        sweep(c0, c1, [&](int t, const unsigned char* at) __attribute__((always_inline)) {
                             if (NW > 1 && idle) {
                                 if (lg == 0) s_part[t & 1][wave][ln] = 0.f;
                                 return;
                             }
-                            f32x16 s = sweep_scores<DQK, true>(at, k_rd, q);
+                            f32x16 s = scores(std::integral_constant<bool, true>{}, at, q);
                             const int tb = t * kSwTile;
                             u32x4 denom[4];                 // (read for every tile: kept in registers they are what the 576-wide rows have not)
                             tile::read_k4(denom, denom_at, denom_at + 32, denom_at + 64, denom_at + 96);
