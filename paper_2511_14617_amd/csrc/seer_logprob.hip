@@ -81,7 +81,7 @@ struct LogprobArgs {
     const int32_t* tokens;
     const int32_t* path;          // nullptr: output row = logits row
     int64_t ld;
-    int T, V, n_chunks, top_n;
+    int T, V, n_chunks, chunk, top_n;      // chunk: elements of one
     float inv_tau;
     float* part;                  // [rows][n_chunks][3]: maximum of x, sum of exp2(d), sum of exp2(d) d, d = (x - maximum) log2(e) / tau
     uint64_t* part_top;           // [rows][n_chunks][top_n] keys, descending, 0 = none
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
     __shared__ float s_max[kLpWaves], s_sum[kLpWaves][2];
     const int r = blockIdx.x / a.n_chunks, chunk = blockIdx.x - r * a.n_chunks;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-    const int begin = chunk * kChunk, end = min(a.V, begin + kChunk);
+    const int begin = min(a.V, chunk * a.chunk), end = min(a.V, begin + a.chunk);
     // (without a path the logits are requested beside the token, not behind it)
     int token;
     int64_t row = r;
@@ -458,13 +458,20 @@ __global__ __launch_bounds__(kLpThreads) void logprob_grad(LogprobGradArgs a) {
     if (rest < end) E::store_one(out + rest, grad(x_rest, rest));
 }
 
-// Elements of a workgroup's chunk.
+// Elements of a workgroup's chunk, at most.
 constexpr int kLpChunkLarge = 16384, kLpChunkSmall = 4096;
 inline int lp_chunk(const seer_logprob_params& p) {
     const int64_t rows = static_cast<int64_t>(p.B) * p.T;
     return rows * ((p.V + kLpChunkLarge - 1) / kLpChunkLarge) >= 2048 ? kLpChunkLarge : kLpChunkSmall;
 }
 inline int lp_num_chunks(const seer_logprob_params& p) { return (p.V + lp_chunk(p) - 1) / lp_chunk(p); }
+// With alternatives to find, which cost a workgroup much the same whatever its length, chunks of one length (in pieces of 512), else whole ones and a short last
+// one, whose loads are all full: 1023 rows of 50 257 bf16 with one alternative 30.0 | 34.2 us, 576 rows of 152 064 fp32 with five 32.2 | 32.5; 4096 rows of
+// 151 936 bf16 without 186 | 181.
+inline int lp_chunk_length(const seer_logprob_params& p) {
+    const int n = lp_num_chunks(p);
+    return p.top_n > 0 ? ((p.V + n - 1) / n + 511) / 512 * 512 : lp_chunk(p);
+}
 inline size_t lp_sums_bytes(const seer_logprob_params& p) {
     return (static_cast<size_t>(p.B) * p.T * lp_num_chunks(p) * 3 * sizeof(float) + 255) / 256 * 256;
 }
@@ -508,7 +515,7 @@ extern "C" int seer_token_logprobs(const void* logits, const int32_t* tokens, co
         return SEER_EALIGN;
     seer::LogprobArgs a{};
     a.logits = logits, a.tokens = tokens, a.path = accepted_path;
-    a.ld = p->ld, a.T = p->T, a.V = p->V, a.n_chunks = seer::lp_num_chunks(*p), a.top_n = p->top_n;
+    a.ld = p->ld, a.T = p->T, a.V = p->V, a.n_chunks = seer::lp_num_chunks(*p), a.chunk = seer::lp_chunk_length(*p), a.top_n = p->top_n;
     a.inv_tau = 1.0f / p->temperature;
     a.part = static_cast<float*>(workspace);
     a.part_top = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + seer::lp_sums_bytes(*p));
