@@ -19,6 +19,8 @@
  *                           every request over its paged KV cache (once per layer)
  *   seer_accept           : target token per position from the logits, then the
  *                           longest accepted root path (once per step)
+ * The others stand before and after it: drafting and histories, the commit of the accepted path, draft lengths and their
+ * statistics, log probabilities of what was emitted (and their gradient), weights of cached positions and eviction by them.
  *
  * Common rules
  *  - Calls are asynchronous on `hip_stream` (a hipStream_t passed as void*,

@@ -156,7 +156,9 @@ __device__ __forceinline__ f32x16 sweep_scores(int at, int k_rd, const bf16x8 (&
     return s;
 }
 
-// The same from one of the stages, which are arrays of their own so that the compiler can tell them apart and overlaps the reads with the products.
+// The same from one of the stages, which are arrays of their own so that the compiler can tell a read of this one from the loads in flight into the other.  It waits for
+// all reads at once while such loads are in flight: four reads go behind the first product of the four before, a product's time ahead of their use (16
+// requests of 8192 .. 24 576 tokens on 128 heads: 300 us with reads and products in turn, 278 so).
 template <int DQK, bool ROWS>
 __device__ __forceinline__ f32x16 stage_scores(const unsigned char* stage, const int (&rd)[4], const bf16x8 (&q)[DQK / 16]) {
     constexpr int kXorBits = Keys<DQK>::kRow % 256 == 0 ? 4 : 3, kPerXor = 1 << (kXorBits - 1);
@@ -291,9 +293,11 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                 if (NW > 1) bare_barrier();                 // every wave is done with the stages
                 if constexpr (APART) {
                     auto one = [&](int t, unsigned char* here, unsigned char* other) __attribute__((always_inline)) {
+                        asm volatile("" ::: "memory");      // (the barrier alone does not keep reads of the stage behind it)
                         wait_vmcnt<0>();
                         __builtin_amdgcn_s_waitcnt(0xc07f);
                         bare_barrier();
+                        asm volatile("" ::: "memory");
                         if (t + 1 < t1) issue_tile(t + 1, other);
                         if (t > t0) after(t - 1);
                         use(t, here);
@@ -677,7 +681,7 @@ inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     w.kept = kept_rows(rows, p.Dqk);
     // Waves of a workgroup.  Up to 256-wide keys: one per 32 rows that a request may have, at most two (of a step's slots only the accepted ones come, so
     // most requests have fewer: 64 requests of 72 rows at most, two waves 53 us, four 58, one 62).  Shared latent: eight, since every
-    // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 293).
+    // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 300, 278 with stage_scores).
     w.waves = p.Dqk > 256 ? (w.kept ? 1 : 8) : rows <= 32 ? 1 : 2;
     // what a CU holds at once, by LDS and by registers
     const int tile_bytes = kSwTile * p.Dqk * 2;
