@@ -69,7 +69,10 @@ struct EvictArgs {
     int32_t* kept;                           // may be nullptr
     int32_t* status;                         // may be nullptr
     EvictHeader* header;                     // [B][Hkv]
-    int2* moves;                             // [B][Hkv][capacity]: slot, position
+    // [B][Hkv][capacity]: where the i-th moving row goes, and, `ahead` further, where it is.  Two lists, since different segments write them: lines of memory that two
+    // L2 caches hold parts of cost more than what is in them (64 rows of 65 536 .. 131 072 sums: evict_list 38 us with pairs in one list, 35 so).
+    int32_t* moves;
+    int64_t ahead;
     EvictSegment* segment;                   // [B][Hkv][segments], longer rows only, as the two below
     EvictRank* rank;                         // [B][Hkv][segments]
     uint2* bound;                            // [B][Hkv] the bracket
@@ -230,16 +233,17 @@ __device__ __forceinline__ int2 list_positions(const EvictArgs& a, size_t bh, co
     int hole = from.holes + block_before<THREADS>(my_holes, s_wave[1], wave);
     int mover = from.movers + block_before<THREADS>(my_movers, s_wave[2], wave);
     int leaving = 0;
-    int2* moves = a.moves + bh * a.capacity;
+    int32_t* slot = a.moves + bh * a.capacity;
+    int32_t* position = slot + a.ahead;
 #pragma unroll 4
     for (int i = i0; i < i1; ++i) {
         const uint32_t k = s_key[i];
         const bool stays = k > least || (k == least && ties_left-- > 0);
         const int j = begin + i;
         if (i < below) {
-            if (!stays) moves[hole++].x = j;
+            if (!stays) slot[hole++] = j;
         } else if (stays) {
-            moves[mover++].y = j;
+            position[mover++] = j;
             leaving += j < a.budget ? 1 : 0;
         }
         s_key[i] = stays ? 1u : 0u;
@@ -248,10 +252,9 @@ __device__ __forceinline__ int2 list_positions(const EvictArgs& a, size_t bh, co
     const float* w = a.weights + bh * a.ldw + begin;
     float* to = a.new_weights && a.new_weights != a.weights ? a.new_weights + bh * a.ldw + begin : nullptr;
     int32_t* kept = a.kept ? a.kept + bh * a.budget + begin : nullptr;
-    if (kept)
+    if (kept)                                               // (every slot: evict_move comes later and writes over the filled ones)
 #pragma unroll 4
-        for (int i = tid; i < below; i += THREADS)
-            if (s_key[i]) kept[i] = begin + i;
+        for (int i = tid; i < below; i += THREADS) kept[i] = begin + i;
     if (to)
         for (int b0 = tid; b0 < below; b0 += 4 * THREADS) {
             float v[4];
@@ -537,7 +540,8 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a) {
     if (kvh == 0 && part == 0 && tid == 0) a.new_ctx_len[b] = h.cut ? a.budget : h.n;
     if (!h.cut) return;
     const int32_t* __restrict__ table = a.block_table + static_cast<size_t>(b) * a.max_pages;
-    const int2* __restrict__ moves = a.moves + bh * a.capacity;
+    const int32_t* __restrict__ slots = a.moves + bh * a.capacity;
+    const int32_t* __restrict__ positions = slots + a.ahead;
     const float* w = a.weights + bh * a.ldw;
     float* new_w = a.new_weights ? a.new_weights + bh * a.ldw : nullptr;
     int32_t* kept = a.kept ? a.kept + bh * a.budget : nullptr;
@@ -550,7 +554,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a) {
         // the rows that leave the slots from `end` on, then the newest ones (row i: slot, position)
         const int count = h.leaving + a.last;
         auto row = [&](int i) __attribute__((always_inline)) {
-            return i < h.leaving ? moves[i] : make_int2(end + i - h.leaving, h.n - count + i);
+            return i < h.leaving ? make_int2(slots[i], positions[i]) : make_int2(end + i - h.leaving, h.n - count + i);
         };
         if (part == a.columns - 1) {                        // their sums
             for (int i0 = 0; i0 < count; i0 += kMoveThreads) {
@@ -606,7 +610,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move(EvictArgs a) {
             const int64_t at = min(x0 + static_cast<int64_t>(x) * threads, total - 1);
             const int i = static_cast<int>(at / per_row);
             c[x] = static_cast<int>(at - static_cast<int64_t>(i) * per_row);
-            m[x] = moves[h.leaving + i];
+            m[x] = make_int2(slots[h.leaving + i], positions[h.leaving + i]);
         }
 #pragma unroll
         for (int x = 0; x < kMoveAhead; ++x) {
@@ -666,7 +670,7 @@ inline EvictLayout evict_layout(const seer_attn_params& p, const seer_evict_para
     w.segments = ctx <= kShortKeys ? 0 : static_cast<int>((ctx + kSegment - 1) / kSegment);
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     w.off_moves = up(sizeof(EvictHeader) * heads);
-    w.off_segment = w.off_moves + up(sizeof(int2) * static_cast<size_t>(evict_capacity(p, e)) * heads);
+    w.off_segment = w.off_moves + 2 * up(sizeof(int32_t) * static_cast<size_t>(evict_capacity(p, e)) * heads);
     w.off_rank = w.off_segment + up(sizeof(EvictSegment) * w.segments * heads);
     w.off_bound = w.off_rank + up(sizeof(EvictRank) * w.segments * heads);
     w.off_list = w.off_bound + (w.segments ? up(sizeof(uint2) * heads) : 0);
@@ -701,7 +705,8 @@ extern "C" int seer_kv_evict(const seer_attn_params* p, const seer_evict_params*
     a.new_ctx_len = new_ctx_len, a.new_weights = new_weights, a.kept = kept, a.status = status;
     char* ws = static_cast<char*>(workspace);
     a.header = reinterpret_cast<seer::EvictHeader*>(ws);
-    a.moves = reinterpret_cast<int2*>(ws + layout.off_moves);
+    a.moves = reinterpret_cast<int32_t*>(ws + layout.off_moves);
+    a.ahead = static_cast<int64_t>((layout.off_segment - layout.off_moves) / 2 / sizeof(int32_t));
     a.segment = reinterpret_cast<seer::EvictSegment*>(ws + layout.off_segment);
     a.rank = reinterpret_cast<seer::EvictRank*>(ws + layout.off_rank);
     a.bound = reinterpret_cast<uint2*>(ws + layout.off_bound);
