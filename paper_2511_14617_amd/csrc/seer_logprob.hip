@@ -155,10 +155,11 @@ __global__ __launch_bounds__(kLpThreads) void logprob_scan(LogprobArgs a) {
 
     // d = v scale - c with c = m scale rounded: one fused multiply-add, exact but for its last rounding, and an unpacking, two sums and the exponential beside
     // it are what a logit costs (with the difference, the product and a clamp against -inf apart the bf16 scan was bound by them: 4096
-    // rows of 151 936 in 215 us).  Where a logit of -inf makes the second sum a NaN, or m scale leaves the floats, a wave goes over
-    // its logits again, with more care.
+    // rows of 151 936 in 215 us).  m itself then has the rounding of c for its d, a quarter at most below 2^22; beyond (chunks of a
+    // finite mask value, small temperatures), where it would grow until exp2 overflows or vanishes, and where a logit of -inf makes the second sum a
+    // NaN, a wave goes over its logits again, with the difference taken first.
     const float scale = a.inv_tau * kLog2e, c = m * scale;
-    const bool usual = fabsf(c) < 1e30f;
+    const bool usual = fabsf(c) < 0x1p22f;
     float l = 0.f, s = 0.f;
     auto add = [&](float v) __attribute__((always_inline)) {
         const float d = fmaf(v, scale, -c), e = fast_exp2(d);      // (a NaN reaches l, and through it every result of the row)
