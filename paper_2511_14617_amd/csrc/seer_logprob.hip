@@ -324,7 +324,8 @@ __global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
     l = all_sum(l), s = all_sum(s);
     const float ln_l = logf(l);
     const bool empty = m == kNegInf && l == 0.f;             // every logit is -inf
-    auto logp = [&](float x) __attribute__((always_inline)) { return x == kNegInf ? kNegInf : (x - m) * a.inv_tau - ln_l; };
+    // (a row with a NaN or +inf, whose sum is a NaN, has no log probabilities, not even of its logits of -inf)
+    auto logp = [&](float x) __attribute__((always_inline)) { return x == kNegInf && ln_l == ln_l ? kNegInf : (x - m) * a.inv_tau - ln_l; };
     if (lane == 0) {
         a.logprob[r] = logp(x_token);
         if (a.entropy) a.entropy[r] = empty ? 0.f : ln_l - kLn2f * (s / l);
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(kWave) void logprob_join(LogprobArgs a) {
     const int index = static_cast<int>(~static_cast<uint32_t>(mine)), found = got;
     for (int v = 0; got < n; ++v) {
         if (__ballot(lane < found && index == v)) continue;
-        if (lane == 0) alt_logp[got] = kNegInf, alt_token[got] = v;
+        if (lane == 0) alt_logp[got] = logp(kNegInf), alt_token[got] = v;
         ++got;
     }
 }
