@@ -469,7 +469,8 @@ SEER_API int seer_token_logprobs(const void* logits, const int32_t* tokens, cons
  * Gradient of sum_r grad_logprob[r] logprob[r] + grad_entropy[r] entropy[r] with respect to the logits, row by row
  * (accepted_path NULL in the forward call):
  *   grad[r][v] = ( grad_logprob[r] (1[v = token] - p_v) - grad_entropy[r] p_v (ln p_v + entropy[r]) ) / temperature.
- * Rows without a token and rows without a finite logit get zeros.
+ * Rows without a token and rows without a finite logit get zeros.  p_v = exp(z_v - logsumexp[r]); where |logsumexp[r]| is 4096 or more, and fp32 too coarse for it (rows of a
+ * finite mask value, small temperatures), the row's maximum and sum are taken again from its logits.
  *
  *  grad_logits   device, rows of V elements of the logits' type grad_ld apart, every element of the B*T rows
  *                written (rounded to nearest), nothing between the rows; the logits themselves may be given (in place, grad_ld = ld), no other overlap

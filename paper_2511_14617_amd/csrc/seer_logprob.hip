@@ -417,6 +417,77 @@ struct LogprobGradArgs {
     float inv_tau;
 };
 
+// d(row) / d(logit) from its log probability; c0 = -g_lp - g_h entropy.
+__device__ __forceinline__ float logit_grad(float logp, float g_lp, float g_h, float c0, bool is_token) {
+    return fast_exp2(logp * kLog2e) * fmaf(-g_h, fmaxf(logp, kLowest), c0) + (is_token ? g_lp : 0.f);
+}
+
+// fp32 holds a logsumexp beyond this to steps of which p = exp(z - logsumexp) takes 2^-12 and more, until ln l is lost (a row that -1e9 masks
+// throughout: steps of 64).  Such a row is the business of its first workgroup alone, which takes the row's own maximum and sum and then every element from its distance to
+// the maximum: 16 rows of 152 064 fp32 logits 114 us (9 where all are near zero), 4096 of bf16 1020 (452).
+constexpr float kLpFar = 4096.f;
+constexpr int kFarHold = 4;              // vectors that a thread has in flight there (eight: 82 registers for bf16, and five workgroups a CU for all rows)
+
+template <int DTYPE>
+__device__ __forceinline__ void far_row_grad(const typename Elem<DTYPE>::T* base, typename Elem<DTYPE>::T* out, int V, int token, float inv_tau, float g_lp, float g_h, float c0) {
+    using E = Elem<DTYPE>;
+    constexpr int kVec = E::kVec, kStep = kLpThreads * kVec;
+    __shared__ float s_max[kLpWaves], s_sum[kLpWaves];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, rest = V / kVec * kVec + tid;
+    const float x_rest = rest < V ? E::one(base + rest) : kNegInf, scale = inv_tau * kLog2e;
+    typename E::Vec x[kFarHold];
+    auto load = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < kFarHold; ++k) x[k] = i0 + k * kStep + kVec <= V ? E::load(base + i0 + k * kStep) : E::none();
+    };
+    float m = x_rest, l = x_rest == kNegInf ? 0.f : fast_exp2((x_rest - x_rest) * scale);      // of the thread's elements (a NaN reaches l)
+    for (int i0 = tid * kVec; i0 < V; i0 += kFarHold * kStep) {
+        load(i0);
+        const float before = m;
+#pragma unroll
+        for (int k = 0; k < kFarHold; ++k)
+#pragma unroll
+            for (int c = 0; c < kVec; ++c) m = fmaxf(m, E::get(x[k], c));
+        const float from = m == kNegInf ? 0.f : m;
+        l *= fast_exp2((before - from) * scale);
+#pragma unroll
+        for (int k = 0; k < kFarHold; ++k)
+#pragma unroll
+            for (int c = 0; c < kVec; ++c) l += fast_exp2((E::get(x[k], c) - from) * scale);
+    }
+    const float wave_top = all_max(m);
+    if (lane == 0) s_max[wave] = wave_top;
+    __syncthreads();
+    float top = s_max[0];
+#pragma unroll
+    for (int w = 1; w < kLpWaves; ++w) top = fmaxf(top, s_max[w]);
+    const float from = top == kNegInf ? 0.f : top;          // (every logit is -inf: l is 0, and so is the gradient)
+    l = all_sum(l * fast_exp2((m - from) * scale));
+    if (lane == 0) s_sum[wave] = l;
+    __syncthreads();                                        // (everything has been read)
+    l = s_sum[0];
+#pragma unroll
+    for (int w = 1; w < kLpWaves; ++w) l += s_sum[w];
+    const float ln_l = logf(l);
+    auto grad = [&](float v, int index) __attribute__((always_inline)) {
+        return l == 0.f ? 0.f : logit_grad((v - from) * inv_tau - ln_l, g_lp, g_h, c0, index == token);
+    };
+    for (int i0 = tid * kVec; i0 < V; i0 += kFarHold * kStep) {
+        load(i0);
+#pragma unroll
+        for (int k = 0; k < kFarHold; ++k) {
+            const int i = i0 + k * kStep;
+            if (i + kVec <= V) {
+                float g[kVec];
+#pragma unroll
+                for (int c = 0; c < kVec; ++c) g[c] = grad(E::get(x[k], c), i + c);
+                E::store(out + i, g);
+            }
+        }
+    }
+    if (rest < V) E::store_one(out + rest, grad(x_rest, rest));
+}
+
 // Every thread writes exactly the elements that it has read, so the gradient may take the logits' place.
 template <int DTYPE, int kChunk>
 __global__ __launch_bounds__(kLpThreads) void logprob_grad(LogprobGradArgs a) {
@@ -436,16 +507,17 @@ __global__ __launch_bounds__(kLpThreads) void logprob_grad(LogprobGradArgs a) {
     const float x_rest = rest < end ? E::one(base + rest) : kNegInf;
     const int token = a.tokens[r];
     const float lse = a.logsumexp[r];
-    // no token, or a row without a finite logit: no gradient
-    const bool none = token < 0 || token >= a.V || lse == kNegInf;
+    const bool none = token < 0 || token >= a.V;            // no token: no gradient
     const float g_lp = a.grad_logprob ? a.grad_logprob[r] * a.inv_tau : 0.f;
     const float g_h = a.grad_entropy ? a.grad_entropy[r] * a.inv_tau : 0.f;
     const float h = a.grad_entropy ? a.entropy[r] : 0.f;
     const float c0 = -g_lp - g_h * h;
+    if (__builtin_amdgcn_readfirstlane(!none && fabsf(lse) >= kLpFar)) {
+        if (chunk == 0) far_row_grad<DTYPE>(base, out, a.V, token, a.inv_tau, g_lp, g_h, c0);
+        return;
+    }
     auto grad = [&](float v, int index) __attribute__((always_inline)) {
-        const float logp = fmaf(v, a.inv_tau, -lse), p = fast_exp2(logp * kLog2e);
-        const float g = p * fmaf(-g_h, fmaxf(logp, kLowest), c0) + (index == token ? g_lp : 0.f);
-        return none ? 0.f : g;
+        return none ? 0.f : logit_grad(fmaf(v, a.inv_tau, -lse), g_lp, g_h, c0, index == token);
     };
 #pragma unroll
     for (int it = 0; it < kIter; ++it) {
