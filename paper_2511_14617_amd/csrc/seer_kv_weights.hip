@@ -499,6 +499,9 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
     if (!WEIGHTS && a.status && found) atomicOr(a.status, found);
 }
 
+// A piece's sum brought from its maximum to `to`.  Without a maximum nothing was seen there, or nothing but -inf and NaN: 0, or a NaN that has to stay.
+__device__ __forceinline__ float part_sum(float2 p, float to) { return p.x == kNegInf ? p.y * 0.f : p.y * fast_exp2(p.x - to); }
+
 // log2 of the denominators: eight rows of a request and KV head per workgroup, 32 threads of a row share its pieces.
 __global__ __launch_bounds__(kLseThreads) void kv_lse(KvWeightsArgs a) {
     __shared__ float2 s_part[kLseThreads];
@@ -517,7 +520,7 @@ __global__ __launch_bounds__(kLseThreads) void kv_lse(KvWeightsArgs a) {
         for (int w = first + slice; w <= last; w += kSlices) {
             const float2 p = at[w * stride];
             const float top = fmaxf(m, p.x), use = top == kNegInf ? 0.f : top;
-            l = l * fast_exp2(m - use) + (p.x == kNegInf ? 0.f : p.y * fast_exp2(p.x - use));
+            l = l * fast_exp2(m - use) + part_sum(p, use);
             m = top;
         }
     }
@@ -528,11 +531,10 @@ __global__ __launch_bounds__(kLseThreads) void kv_lse(KvWeightsArgs a) {
     for (int s = 0; s < kSlices; ++s) top = fmaxf(top, s_part[s * kLseRows + tid].x);
     float sum = 0.f;
     for (int s = 0; s < kSlices; ++s) {
-        const float2 p = s_part[s * kLseRows + tid];
-        sum += p.x == kNegInf ? 0.f : p.y * fast_exp2(p.x - top);
+        sum += part_sum(s_part[s * kLseRows + tid], top);
     }
     // a row that weighs nothing (all its scores -inf): +inf, so that exp2 gives 0
-    a.lse[(static_cast<size_t>(b) * a.Hkv + kvh) * GT + r] = top == kNegInf ? -kNegInf : top + log2f(sum);
+    a.lse[(static_cast<size_t>(b) * a.Hkv + kvh) * GT + r] = top == kNegInf && sum == 0.f ? -kNegInf : top + log2f(sum);
 }
 
 // The weights from the scores that kModeKeep left: a position per thread.
