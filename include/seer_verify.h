@@ -499,7 +499,8 @@ SEER_API size_t seer_kv_weights_workspace(const seer_attn_params* p);
  *                      softmax_j(scale * q.K[j]) over what row i sees.
  * So the entries of positions from before the step have to be there (zeros for a request's first
  * call), those of the step's own need not; entries from n on are left as they are.  Scores, denominators and sums are
- * fp32; the result does not depend on anything but the arguments.
+ * fp32; the result does not depend on anything but the arguments.  A row with a NaN or +inf among its scores makes the weights of every position
+ * that it sees NaN, and of no other; a row of nothing but -inf adds nothing.
  *
  *  weights        device [B, Hkv, max_pages_per_seq * page_size] fp32, read and written
  *  q              device [B,T,Hq,Dqk] bf16

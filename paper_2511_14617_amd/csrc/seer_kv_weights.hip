@@ -559,13 +559,14 @@ __global__ __launch_bounds__(kApplyThreads) void kv_apply(KvWeightsArgs a, int p
         for (int x = 0; x < kApplyPositions / kApplyThreads; ++x) {
             const int pos = p0 + x * kApplyThreads + static_cast<int>(threadIdx.x);
             if (pos >= step.n) break;
+            const int from_row = pos > first_own ? (pos - first_own) * a.G : 0;      // (a row whose denominator is a NaN leaves what it does not see alone)
             float sum = 0.f;
 #pragma unroll
             for (int r = 0; r < KEPT; r += 4) {
                 const f32x4 s = *reinterpret_cast<const f32x4*>(scores + static_cast<size_t>(pos) * KEPT + r);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (r + i < R) sum += fast_exp2(s[i] - denom[r + i]);
+                    if (r + i < R && r + i >= from_row) sum += fast_exp2(s[i] - denom[r + i]);
             }
             to[pos] = pos < first_own ? fmaf(a.decay, to[pos], sum) : sum;
         }
@@ -656,7 +657,7 @@ __global__ __launch_bounds__(kShortWaves * kWave) void kv_short(KvWeightsArgs a,
         const float old = j < first_own ? to[j] : 0.f;
         float sum = 0.f;
 #pragma unroll 4
-        for (int r = 0; r < R; ++r) sum += fast_exp2(s_score[r * stride + j] - s_lse[r]);
+        for (int r = max(0, j - first_own) * a.G; r < R; ++r) sum += fast_exp2(s_score[r * stride + j] - s_lse[r]);       // (the rows that see the position)
         to[j] = j < first_own ? fmaf(a.decay, old, sum) : sum;
     }
     if (a.status && found) atomicOr(a.status, found);
