@@ -484,7 +484,7 @@ SEER_API int seer_token_logprobs_grad(void* grad_logits, int64_t grad_ld, const 
                              const float* grad_entropy, const seer_logprob_params* p, void* hip_stream);
 
 /* Bytes of device scratch seer_kv_weights needs; 0 on invalid params.  Host-only.  (Up to 16 query rows per KV head, T * Hq / Hkv, it keeps
- * 4, 8 or 16 scores for every position of the block table.) */
+ * 4, 8 or 16 fp32 scores for every position of the block table, as far as they take no more than 2 GiB, which reads the keys once; else the keys are read twice.) */
 SEER_API size_t seer_kv_weights_workspace(const seer_attn_params* p);
 
 /*

@@ -8,8 +8,8 @@
 // What bounds it: HBM for a few rows, LDS reads and matrix products in turn for the many rows of a shared latent.  A weight needs its row's
 // denominator first:
 //   up to 16 rows   one sweep over the keys (kModeKeep) that leaves each row's maximum and sum per piece and the scores, kv_lse, which joins the
-//                   denominators, and kv_apply, which reads the scores.  64 requests of 512 .. 32 768 tokens on 32/8 heads, one row each: 278 us with two
-//                   sweeps, 167 with one.
+//                   denominators, and kv_apply, which reads the scores.  64 requests of 512 .. 32 768 tokens on 32/8 heads, one row each: 251 us with two
+//                   sweeps, 168 with one.
 //   more            the scores would cost more than the keys: two sweeps with the same loads and matrix products, kModeSums and
 //                   kModeWeights, kv_lse between them.
 //
@@ -667,10 +667,15 @@ __global__ __launch_bounds__(kShortWaves * kWave) void kv_short(KvWeightsArgs a,
 // host
 // ---------------------------------------------------------------------------
 // Rows whose scores are kept between the sweeps: written and read once they cost 8 bytes a position each, the second sweep
-// 2 Dqk; up to a quarter of that, and up to 16 (the workspace holds them for every position of the block table).  0: none.
-inline int kept_rows(int rows, int Dqk) {
+// 2 Dqk; up to a quarter of that, and up to 16.  The workspace holds them for every position of the block table, so not where that is more than 2 GiB (some cache of
+// many requests on long tables would have no room for it; there the keys are read twice, 64 requests of 512 .. 32 768 tokens on 32/8 heads 251 us instead of
+// 168, with 0.1 MB of workspace instead of 268).  0: none.
+constexpr size_t kMaxScoreBytes = size_t{2} << 30;
+static_assert(kMaxScoreBytes / 16 + size_t{8192} * kApplyPositions < (size_t{1} << 31), "kv_apply counts positions in 32 bits, with a stride of its launch on top");
+inline int kept_rows(const seer_attn_params& p, int rows) {
     const int kept = rows <= 4 ? 4 : rows <= 8 ? 8 : 16;
-    return rows <= 16 && kept <= Dqk / 8 ? kept : 0;
+    const int64_t positions = static_cast<int64_t>(p.max_pages_per_seq) * p.page_size, most = static_cast<int64_t>(kMaxScoreBytes / sizeof(float)) / kept;
+    return rows <= 16 && kept <= p.Dqk / 8 && static_cast<int64_t>(p.B) * p.Hkv <= most / positions ? kept : 0;
 }
 struct KvWeightsLayout {
     int waves, W, kept;
@@ -681,7 +686,7 @@ inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     KvWeightsLayout w{};
     const int rows = (p.Hq / p.Hkv) * p.T;
     w.whole = weights_short(rows, p.Dqk, static_cast<int64_t>(p.max_pages_per_seq) * p.page_size);
-    w.kept = kept_rows(rows, p.Dqk);
+    w.kept = kept_rows(p, rows);
     // Waves of a workgroup.  Up to 256-wide keys: one per 32 rows that a request may have, at most two (of a step's slots only the accepted ones come, so
     // most requests have fewer: 64 requests of 72 rows at most, two waves 53 us, four 58, one 62).  Shared latent: eight, since every
     // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 300, 278 with stage_scores).
