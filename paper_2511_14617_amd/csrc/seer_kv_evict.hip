@@ -271,10 +271,11 @@ __device__ __forceinline__ void fixed_positions(const EvictArgs& a, size_t bh, b
     const float* w = a.weights + bh * a.ldw;
     float* to = usable && a.new_weights && a.new_weights != a.weights ? a.new_weights + bh * a.ldw : nullptr;
     int32_t* kept = a.kept ? a.kept + bh * a.budget : nullptr;
+    // (unsigned: a position and a stride on top may pass 2^31)
     if (kept)
-        for (int j = at; j < (cut ? first : a.budget); j += step) kept[j] = cut ? j : -1;
+        for (uint32_t j = at, stop = cut ? first : a.budget; j < stop; j += step) kept[j] = cut ? static_cast<int>(j) : -1;
     if (to)
-        for (int j = at; j < (cut ? first : n); j += step) to[j] = w[j];
+        for (uint32_t j = at, stop = cut ? first : n; j < stop; j += step) to[j] = w[j];
 }
 
 __global__ __launch_bounds__(kShortThreads) void evict_short(EvictArgs a) {
@@ -333,8 +334,9 @@ __global__ __launch_bounds__(kSegThreads) void evict_bracket(EvictArgs a) {
     const int seg = static_cast<int>(blockIdx.x - bh * a.segments), b = static_cast<int>(bh) / a.Hkv, tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const EvictRequest q = evict_request(a, b);
-    const int begin = q.first + seg * kSegment, total = q.stop - q.first;
-    if (!q.cut || begin >= q.stop) return;
+    const int total = q.stop - q.first;
+    if (!q.cut || seg * kSegment >= total) return;          // (before anything is added to `first`: the table's segments from there on may pass 2^31)
+    const int begin = q.first + seg * kSegment;
     const float* w = a.weights + bh * a.ldw;
     const int count = min(kSegment, q.stop - begin), below = min(max(q.end - begin, 0), count);
     float v[kHold];
@@ -521,7 +523,7 @@ __global__ __launch_bounds__(kSegThreads) void evict_list(EvictArgs a) {
     const int seg = static_cast<int>(blockIdx.x - bh * a.segments), b = static_cast<int>(bh) / a.Hkv, tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const EvictRequest q = evict_request(a, b);
-    const int begin = q.first + seg * kSegment, count = q.cut ? min(kSegment, q.stop - begin) : 0;
+    const int count = q.cut ? min(kSegment, q.stop - q.first - seg * kSegment) : 0, begin = count > 0 ? q.first + seg * kSegment : 0;
     if (count > 0) load_keys<kSegThreads>(s_key, a.weights + bh * a.ldw, begin, count);
     const EvictHeader h = a.header[bh];
     fixed_positions(a, bh, h.cut, q.first, q.n, h.usable, seg * kSegThreads + tid, a.segments * kSegThreads);
