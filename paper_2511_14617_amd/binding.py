@@ -511,7 +511,8 @@ def seer_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, accepted_pat
     """(logprob, entropy, logsumexp, top_logprob, top_token) of tokens under softmax(logits / temperature).
     logits [B,T,V] or [N,V] float32 or bfloat16, rows at one distance; tokens int32 of the same leading shape, outside
     [0, V) = no entry; accepted_path [B,T] int32 (entry (b,i) is judged by the logits of slot accepted_path[b,i]) or None.
-    The first three are float32 of the tokens' shape, the last two [..., top_n] float32 and int32, None where top_n is 0."""
+    The first three are float32 of the tokens' shape, the last two [..., top_n] float32 and int32, None where top_n is 0.  `out`: such a tuple to write
+    to; its entropy and logsumexp may be None."""
     lib = load_library()
     p = logprob_params(logits, temperature, top_n)
     lead = tuple(logits.shape[:-1])
@@ -524,8 +525,11 @@ def seer_token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, accepted_pat
         out += (_empty((*lead, top_n), torch.float32, dev, stream) if top_n > 0 else None,
                 _empty((*lead, top_n), torch.int32, dev, stream) if top_n > 0 else None)
     else:
+        if out[0] is None or (top_n > 0 and (out[3] is None or out[4] is None)):
+            raise ValueError("out: want logprob, and the alternatives where top_n asks for them; entropy and logsumexp may be None")
         for t, name in zip(out[:3], ("logprob", "entropy", "logsumexp")):
-            _want(t, torch.float32, lead, name)
+            if t is not None:
+                _want(t, torch.float32, lead, name)
         if top_n > 0:
             _want(out[3], torch.float32, (*lead, top_n), "top_logprob")
             _want(out[4], torch.int32, (*lead, top_n), "top_token")
