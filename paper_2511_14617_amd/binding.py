@@ -620,6 +620,10 @@ def seer_kv_evict(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_
     lib = load_library()
     if k_pages.dim() != 4 or block_table.dim() != 2:
         raise ValueError("want k_pages [num_pages,Hkv,page,Dqk] and block_table [B,max_pages]")
+    per_request = isinstance(keep_first, torch.Tensor)
+    for value, name in ((limit, "limit"), (budget, "budget"), (0 if per_request else keep_first, "keep_first"), (keep_last, "keep_last")):
+        if not -2 ** 31 <= int(value) < 2 ** 31:            # (the struct's field would take its lowest 32 bits)
+            raise ValueError("%s: want a 32-bit number, got %s" % (name, value))
     num_pages, Hkv, P, Dqk = k_pages.shape
     B, max_pages = block_table.shape
     for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
@@ -628,7 +632,6 @@ def seer_kv_evict(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_
     _want(block_table, torch.int32, (B, max_pages), "block_table")
     _want(ctx_len, torch.int32, (B,), "ctx_len")
     _want(weights, torch.float32, (B, Hkv, max_pages * P), "weights")
-    per_request = isinstance(keep_first, torch.Tensor)
     if per_request:
         _want(keep_first, torch.int32, (B,), "keep_first")
     p = SeerAttnParams(B, 1, Hkv, Hkv, Dqk, v_pages.shape[3] if v_pages is not None else 0, P, num_pages, max_pages, 0,
