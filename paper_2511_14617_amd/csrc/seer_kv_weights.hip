@@ -217,6 +217,7 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
     constexpr int kTileLoads = K::kBytes / 1024, kLoads = (kTileLoads + NW - 1) / NW;      // direct-to-LDS loads of a tile, of a wave at most
     static_assert(kSwStages == 2 || kLoads * (kSwStages - 1) < 64, "");
     constexpr bool APART = NW == 8;
+    static_assert(APART || kTileLoads % NW == 0, "every wave has the same number of loads in flight");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[APART ? 1024 : kSwStages * K::kBytes];
     __shared__ __attribute__((aligned(1024))) unsigned char lds_even[APART ? K::kBytes : 1], lds_odd[APART ? K::kBytes : 1];
     __shared__ float s_sums[WEIGHTS ? kSwChunk * kSwTile : 1];
@@ -319,8 +320,7 @@ __global__ __launch_bounds__(NW * kWave) __attribute__((amdgpu_waves_per_eu(NW =
                 for (int t = t0; t < t1; ++t) {
                     // (this wave's loads of the tiles behind this one may be on their way; near the end none are waited for apart)
                     if (kSwStages == 2 || t + kSwStages - 1 > t1) wait_vmcnt<0>();
-                    else if (kTileLoads % NW == 0 || wave < kTileLoads % NW) wait_vmcnt<kLoads * (kSwStages - 2)>();
-                    else wait_vmcnt<(kLoads - 1) * (kSwStages - 2)>();
+                    else wait_vmcnt<kLoads * (kSwStages - 2)>();
                     if (NW > 1) {
                         __builtin_amdgcn_s_waitcnt(0xc07f); // (lgkmcnt: what `use` wrote)
                         bare_barrier();
