@@ -575,7 +575,9 @@ __global__ __launch_bounds__(kApplyThreads) void kv_apply(KvWeightsArgs a, int p
 // Short block tables: one workgroup per request and KV head keeps all scores in LDS, and the three launches become one.  Wave i takes tiles i, i + 4, .. (the keys
 // go from memory to the operand registers, the next tile's while this one is multiplied), then a wave each row for its denominator, then a
 // thread each position for its sum.  Against three launches: 4 requests of 64 .. 512 tokens, 8/2 heads, 20 rows at most 12.4 | 17.3 us, 64 of them with 32/8
-// heads 20.3 | 30.6; but 16 of up to 3000 tokens with 4 rows 40.4 | 26.3 and 16 of up to 400 with 36 rows 21.9 | 18.9.
+// heads 20.3 | 30.6; but 16 of up to 3000 tokens with 4 rows 40.4 | 26.3 and 16 of up to 400 with 36 rows 21.9 | 18.9.  Between 512 and 3000 positions they cross at 768 .. 1536 for few
+// requests (4 on 8/2 heads, one row: 768 positions 11.8 | 16.3, 1536 19.9 | 16.9; three rows: 1024 19.1 | 16.9), beyond 3000 for many (64 on 32/8, one
+// row: 84 | 94): the limit is safe for both.
 constexpr int kShortWaves = 4, kShortPositions = 512, kShortRows = 32, kShortScores = 16000;      // of the table, rows, scores in LDS at most
 inline bool weights_short(int rows, int Dqk, int64_t positions) {
     return Dqk <= 256 && positions <= kShortPositions && rows <= kShortRows && (positions + 36) * rows <= kShortScores;
@@ -689,7 +691,7 @@ inline KvWeightsLayout kv_weights_layout(const seer_attn_params& p) {
     w.kept = kept_rows(p, rows);
     // Waves of a workgroup.  Up to 256-wide keys: one per 32 rows that a request may have, at most two (of a step's slots only the accepted ones come, so
     // most requests have fewer: 64 requests of 72 rows at most, two waves 53 us, four 58, one 62).  Shared latent: eight, since every
-    // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 300, 278 with stage_scores).
+    // row block of a request reads its keys again (16 requests of 8192 .. 24 576 tokens, 640 rows at most: four waves 326 us, eight 300, 263 .. 280 with stage_scores).
     w.waves = p.Dqk > 256 ? (w.kept ? 1 : 8) : rows <= 32 ? 1 : 2;
     // what a CU holds at once, by LDS and by registers
     const int tile_bytes = kSwTile * p.Dqk * 2;
