@@ -20,7 +20,8 @@
  *   seer_accept           : target token per position from the logits, then the
  *                           longest accepted root path (once per step)
  * The others stand before and after it: drafting and histories, the commit of the accepted path, draft lengths and their
- * statistics, log probabilities of what was emitted (and their gradient), weights of cached positions and eviction by them.
+ * statistics, log probabilities of what was emitted (and their gradient), weights of cached positions and eviction by them; and
+ * in front of a request's first step pages, the rows of new tokens in them, and attention over whole prompts.
  *
  * Common rules
  *  - Calls are asynchronous on `hip_stream` (a hipStream_t passed as void*,
@@ -568,6 +569,99 @@ SEER_API int seer_kv_evict(const seer_attn_params* p, const seer_evict_params* e
                   const int32_t* block_table, const int32_t* ctx_len, const int32_t* keep_first, const float* weights,
                   int32_t* new_ctx_len, float* new_weights, int32_t* kept, int32_t* status, void* workspace,
                   size_t workspace_bytes, void* hip_stream);
+
+/*
+ * In front of the first verification step: pages for requests, the rows of new tokens in them, attention over whole prompts.
+ * One step of a server that takes new requests beside those that are being verified:
+ *   seer_kv_reserve       pages, slots and positions of every request's next tokens (a prompt, a piece of one, T draft
+ *                         slots, one token), pages of finished and cut requests back into the pool
+ *   seer_kv_append        per layer: the tokens' queries and keys rotated, keys and values into their slots
+ *   seer_prompt_attention per layer: causal attention of the tokens, request behind request in one packed array
+ * and for the requests that verify, whose tokens are B*T packed ones, seer_verify_attention, seer_accept and seer_kv_commit
+ * on the lengths that seer_kv_reserve wrote.
+ *
+ * Packed tokens: request b's are first_token[b] .. first_token[b + 1] - 1 of n_tokens rows; rows behind the last request's are padding.
+ */
+typedef struct seer_reserve_params {
+    int32_t B;                  /* rows, up to 16384                                                       */
+    int32_t page_size;          /* tokens per page, any; num_pages * page_size below 2^31                  */
+    int32_t num_pages;          /* pages in the pool, up to 2^30                                           */
+    int32_t max_pages_per_seq;  /* row stride of block_table                                               */
+    int32_t n_tokens;           /* entries of slot and position: room for all new tokens of the call       */
+} seer_reserve_params;
+
+/* Bytes of device scratch seer_kv_reserve needs; 0 on invalid params.  Host-only. */
+SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
+
+/*
+ * Room for n_new[b] tokens behind the ctx_len[b] positions of every request: afterwards row b holds exactly the
+ * ceil((ctx_len[b] + n_new[b]) / page_size) pages of those positions.  The pages that it holds beyond them (after an eviction, or a
+ * step that accepted little) go back; n_new[b] = -1 gives back all pages of a finished request (its ctx_len is not looked at).
+ *
+ * page_refs[p] counts the rows that hold page p, and the caller if it has a use of its own for it: 0 = free.  A request that starts (pages_held[b] = 0) may take over the leading pages of row r = share_from[b] that hold its first
+ * ctx_len[b] positions, a multiple of page_size and no more than row r holds before the call: the
+ * whole pages of a prompt that a group has in common (the rest of the prompt is among its new tokens).
+ *
+ * All rows are judged by the state before the call.  Shared pages are counted up, then pages counted down, then the free pages, the lowest
+ * ids first, go to the rows in ascending order; a row that needs pages gets them if those before it that need any and it itself
+ * need no more than there are free, and is left as it was otherwise.  The result depends on nothing else.
+ *
+ *  ctx_len       device [B] int32: positions that hold keys and values
+ *  n_new         device [B] int32: -1, 0 or more
+ *  share_from    device [B] int32 or NULL; below 0 = none
+ *  tree_mask     device [n_tokens] uint64 or NULL: where a token's word is not 0, its position is ctx_len[b] plus the number
+ *                of its ancestors, the word's bits without its own (seer_draft's tree_mask, for draft trees:
+ *                siblings have one position and slots of their own)
+ *  block_table   device [B,max_pages_per_seq] int32, entries of new and taken over pages written
+ *  pages_held    device [B] int32, read and written; zeros at first
+ *  page_refs     device [num_pages] int32, 16-byte aligned, read and written; zeros at first
+ *  step_len      device [B] int32, written: ctx_len[b] + n_new[b] (what seer_verify_attention and seer_prompt_attention take as
+ *                ctx_len); 0 for requests that are over or were left as they were.  Not ctx_len itself
+ *  first_token   device [B+1] int32, written: sums of the n_new above 0 of the rows before (2^31 - 1 at most)
+ *  slot          device [n_tokens] int32, written: page * page_size + offset, -1 for padding and for rows that were left as they were
+ *  position      device [n_tokens] int32, written: ctx_len[b] + i for the row's i-th token (but see tree_mask); -1 as for slot
+ *  status        device [1] int32 or NULL; bits are OR-ed in: 1 = numbers out of range (n_new, ctx_len beyond the table or the pages
+ *                held, share_from), 4 = tokens beyond n_tokens, 8 = no pages left: such rows are left as they were.  2 = a page id
+ *                outside the pool, 16 = a page given back more often than taken (its count is below 0: it is not given out again).  The caller clears it.
+ *  workspace     device, >= seer_kv_reserve_workspace(p) bytes, 16-byte aligned
+ * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_len, const int32_t* n_new, const int32_t* share_from,
+                    const uint64_t* tree_mask, int32_t* block_table, int32_t* pages_held, int32_t* page_refs, int32_t* step_len,
+                    int32_t* first_token, int32_t* slot, int32_t* position, int32_t* status, void* workspace,
+                    size_t workspace_bytes, void* hip_stream);
+
+typedef struct seer_append_params {
+    int32_t n_tokens;
+    int32_t Hq, Hkv;            /* Hq = 0: keys and values only                                            */
+    int32_t Dqk, Dv;            /* multiples of 8, up to 4096; a token's components below 2^19             */
+    int32_t page_size, num_pages;  /* num_pages * page_size below 2^31                                     */
+    int32_t kv_shared_latent;   /* 1: no values of their own (Dv is not looked at)                         */
+    int32_t rotary_at;          /* first rotated component of every head of q and k, a multiple of 8       */
+    int32_t rotary_dim;         /* rotated components R, 0 .. 512, a multiple of 16 (interleaved: of 8)    */
+    int32_t interleaved;        /* pairs of components: 0 = (i, i + R/2), 1 = (2i, 2i + 1)                 */
+    int64_t q_stride, k_stride, v_stride, q_out_stride;   /* elements from a token to the next, multiples of 8 */
+} seer_append_params;
+
+/*
+ * The rows of new tokens into the paged cache.  For token i with slot[i] >= 0: its key and value heads go to page
+ * slot[i] / page_size, offset slot[i] % page_size of the pools; the R components of every query and key head from rotary_at on are rotated
+ * on the way, pair j by the angle position[i] * inv_freq[j] (product and reduction in 64 bits, sine, cosine and rotation in fp32,
+ * rounded once), the others and the values copied.  Tokens without a slot are not looked at and leave q_out's row as it is.
+ *
+ *  q             device, n_tokens rows of [Hq,Dqk] bf16, q_stride apart (a slice of a fused projection, for instance); NULL iff Hq = 0
+ *  k, v          device, rows of [Hkv,Dqk] and [Hkv,Dv] bf16; v and v_pages NULL iff kv_shared_latent
+ *  slot          device [n_tokens] int32, as written by seer_kv_reserve; no two tokens with the same slot
+ *  position      device [n_tokens] int32;  inv_freq device [R/2] fp32; both may be NULL if R = 0
+ *  q_out         device, rows of [Hq,Dqk] bf16, q_out_stride apart; may be q itself (with the same stride), no other overlap
+ *  k_pages, v_pages  device, as for seer_verify_attention, written
+ *  status        device [1] int32 or NULL; bit 0 is OR-ed in for a slot below -1 or beyond the pool (the token is left out).  The
+ *                caller clears it.
+ * Asynchronous on hip_stream; no workspace.  Returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_kv_append(const seer_append_params* p, const void* q, const void* k, const void* v, const int32_t* slot,
+                   const int32_t* position, const float* inv_freq, void* q_out, void* k_pages, void* v_pages, int32_t* status,
+                   void* hip_stream);
 
 /* Static text for a return code of either call (negative SEER_E*, or a
  * positive hipError_t). */

@@ -24,7 +24,8 @@ EXPORTS = ("seer_verify_attention_workspace", "seer_verify_attention_status_offs
            "seer_accept_workspace", "seer_accept", "seer_accept_static", "seer_accept_sampled",
            "seer_kv_commit", "seer_mba_draft_lengths", "seer_acceptance_stats", "seer_acceptance_beta", "seer_draft_workspace", "seer_draft", "seer_history_append",
            "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad",
-           "seer_kv_weights_workspace", "seer_kv_weights", "seer_kv_evict_workspace", "seer_kv_evict", "seer_strerror")
+           "seer_kv_weights_workspace", "seer_kv_weights", "seer_kv_evict_workspace", "seer_kv_evict",
+           "seer_kv_reserve_workspace", "seer_kv_reserve", "seer_kv_append", "seer_strerror")
 
 
 class SeerAttnParams(ctypes.Structure):
@@ -48,6 +49,18 @@ class SeerLogprobParams(ctypes.Structure):
 
 class SeerEvictParams(ctypes.Structure):
     _fields_ = [("limit", ctypes.c_int32), ("budget", ctypes.c_int32), ("keep_first", ctypes.c_int32), ("keep_last", ctypes.c_int32)]
+
+
+class SeerReserveParams(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+                ("n_tokens", ctypes.c_int32)]
+
+
+class SeerAppendParams(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("Dqk", ctypes.c_int32), ("Dv", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("kv_shared_latent", ctypes.c_int32),
+                ("rotary_at", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64)]
 
 
 SEER_F32, SEER_BF16 = 0, 1
@@ -125,6 +138,12 @@ def load_library() -> ctypes.CDLL:
         lib.seer_kv_evict_workspace.restype = sz
         lib.seer_kv_evict.argtypes = [ctypes.POINTER(SeerAttnParams), ctypes.POINTER(SeerEvictParams)] + [vp] * 11 + [sz, vp]
         lib.seer_kv_evict.restype = ctypes.c_int
+        lib.seer_kv_reserve_workspace.argtypes = [ctypes.POINTER(SeerReserveParams)]
+        lib.seer_kv_reserve_workspace.restype = sz
+        lib.seer_kv_reserve.argtypes = [ctypes.POINTER(SeerReserveParams)] + [vp] * 13 + [sz, vp]
+        lib.seer_kv_reserve.restype = ctypes.c_int
+        lib.seer_kv_append.argtypes = [ctypes.POINTER(SeerAppendParams)] + [vp] * 11
+        lib.seer_kv_append.restype = ctypes.c_int
         lib.seer_strerror.argtypes = [ctypes.c_int]
         lib.seer_strerror.restype = ctypes.c_char_p
         _lib = lib
@@ -658,3 +677,113 @@ def seer_kv_evict(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_
                              _ptr(keep_first) if per_request else None, _ptr(weights), _ptr(new_ctx_len), _ptr(new_weights), _ptr(kept),
                              _ptr(status), _ptr(workspace), workspace.numel(), _stream_handle(stream)))
     return new_ctx_len, kept
+
+
+def seer_kv_reserve_workspace(params: SeerReserveParams) -> int:
+    return int(load_library().seer_kv_reserve_workspace(ctypes.byref(params)))
+
+
+def seer_kv_reserve(block_table: torch.Tensor, pages_held: torch.Tensor, page_refs: torch.Tensor, ctx_len: torch.Tensor, n_new: torch.Tensor,
+                    n_tokens: int, page_size: int, *, share_from: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                    out: Optional[Tuple[torch.Tensor, ...]] = None, status: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Pages for n_new [B] tokens (-1: the request is over) behind the ctx_len [B] positions of every request, in place in block_table
+    [B,max_pages], pages_held [B] and page_refs [num_pages]; share_from [B]: row whose leading pages a starting request takes over.  All int32 on
+    the device; tree_mask [n_tokens] int64 (the uint64 ancestor bits).  Returns (step_len [B], first_token [B+1], slot [n_tokens],
+    position [n_tokens]), all int32; `out`: such a tuple to write to."""
+    lib = load_library()
+    for value, name in ((n_tokens, "n_tokens"), (page_size, "page_size")):
+        if not 0 <= int(value) < 2 ** 31:                   # (the struct's field would take its lowest 32 bits)
+            raise ValueError("%s: want a number from 0 to 2^31 - 1, got %s" % (name, value))
+    if block_table.dim() != 2 or page_refs.dim() != 1:
+        raise ValueError("want block_table [B,max_pages] and page_refs [num_pages]")
+    B, max_pages = block_table.shape
+    p = SeerReserveParams(B, int(page_size), page_refs.shape[0], max_pages, int(n_tokens))
+    _want(block_table, torch.int32, (B, max_pages), "block_table")
+    _want(pages_held, torch.int32, (B,), "pages_held")
+    _want(page_refs, torch.int32, (p.num_pages,), "page_refs")
+    _want(ctx_len, torch.int32, (B,), "ctx_len")
+    _want(n_new, torch.int32, (B,), "n_new")
+    if share_from is not None:
+        _want(share_from, torch.int32, (B,), "share_from")
+    if tree_mask is not None:
+        _want(tree_mask, torch.int64, (p.n_tokens,), "tree_mask")
+    if status is not None:
+        _want(status, torch.int32, (1,), "status")
+    dev = block_table.device
+    if out is None:                                         # (one allocation: short calls are bound by the host)
+        out = _empty(2 * B + 1 + 2 * p.n_tokens, torch.int32, dev, stream).split((B, B + 1, p.n_tokens, p.n_tokens))
+    else:
+        for t, shape, name in zip(out, ((B,), (B + 1,), (p.n_tokens,), (p.n_tokens,)), ("step_len", "first_token", "slot", "position")):
+            _want(t, torch.int32, shape, name)
+    if workspace is None:
+        need = int(lib.seer_kv_reserve_workspace(ctypes.byref(p)))
+        workspace = _empty(max(need, 256), torch.uint8, dev, stream)
+    _here(stream, block_table=block_table, pages_held=pages_held, page_refs=page_refs, ctx_len=ctx_len, n_new=n_new, share_from=share_from,
+          tree_mask=tree_mask, step_len=out[0], first_token=out[1], slot=out[2], position=out[3], status=status, workspace=workspace)
+    _check(lib.seer_kv_reserve(ctypes.byref(p), _ptr(ctx_len), _ptr(n_new), _ptr(share_from), _ptr(tree_mask), _ptr(block_table),
+                               _ptr(pages_held), _ptr(page_refs), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(status),
+                               _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+    return tuple(out)
+
+
+def _token_rows(t: torch.Tensor, N: int, name: str) -> int:
+    """Elements from one token to the next of rows [N,H,D] (tokens may be apart, their heads not)."""
+    if (t.dim() != 3 or t.shape[0] != N or t.dtype != torch.bfloat16 or not t.is_cuda or (t.shape[2] > 1 and t.stride(2) != 1)
+            or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
+        raise ValueError("%s: want device bfloat16 [%d,H,D], the heads of a token behind one another, got %s%s with strides %s on %s" %
+                         (name, N, t.dtype, tuple(t.shape), t.stride(), t.device))
+    return t.stride(0) if N > 1 else max(t.stride(0), t.shape[1] * t.shape[2]) // 8 * 8
+
+
+def seer_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], slot: torch.Tensor, position: Optional[torch.Tensor],
+                   k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], *, inv_freq: Optional[torch.Tensor] = None, rotary_at: int = 0,
+                   interleaved: bool = False, q_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                   stream: Optional[torch.cuda.Stream] = None) -> Optional[torch.Tensor]:
+    """Rotates q [N,Hq,Dqk] (or None) and k [N,Hkv,Dqk] bf16 by position [N] int32 and inv_freq [R/2] float32 (None: no rotation), from component
+    rotary_at on, and writes k and v [N,Hkv,Dv] (None: shared latent) to slot [N] int32 of the pools.  Tokens may be apart in q, k, v and q_out.
+    Returns q_out (rows of tokens without a slot are left as they are; may be q itself)."""
+    lib = load_library()
+    if k.dim() != 3 or k_pages.dim() != 4:
+        raise ValueError("want k [N,Hkv,Dqk] and k_pages [num_pages,Hkv,page,Dqk]")
+    N, Hkv, Dqk = k.shape
+    num_pages, P = k_pages.shape[0], k_pages.shape[2]
+    k_stride, v_stride, q_stride, out_stride, Hq, Dv = _token_rows(k, N, "k"), 0, 0, 0, 0, 0
+    _want(k_pages, torch.bfloat16, (num_pages, Hkv, P, Dqk), "k_pages")
+    if (v is None) != (v_pages is None):
+        raise ValueError("v, v_pages: want both or neither")
+    if v is not None:
+        v_stride, Dv = _token_rows(v, N, "v"), v.shape[2]
+        _want(v_pages, torch.bfloat16, (num_pages, Hkv, P, Dv), "v_pages")
+        if v.shape[1] != Hkv:
+            raise ValueError("v: want [N,%d,Dv], got %s" % (Hkv, tuple(v.shape)))
+    _want(slot, torch.int32, (N,), "slot")
+    R = 0
+    if inv_freq is not None:
+        R = 2 * inv_freq.numel()
+        _want(inv_freq, torch.float32, (R // 2,), "inv_freq")
+        if position is None:
+            raise ValueError("position: needed for a rotation")
+    if position is not None:
+        _want(position, torch.int32, (N,), "position")
+    if status is not None:
+        _want(status, torch.int32, (1,), "status")
+    if not 0 <= int(rotary_at) < 2 ** 31:
+        raise ValueError("rotary_at: want a number from 0 to 2^31 - 1, got %s" % (rotary_at,))
+    if q is not None:
+        q_stride, Hq = _token_rows(q, N, "q"), q.shape[1]
+        if q.shape[2] != Dqk:
+            raise ValueError("q: want [N,Hq,%d], got %s" % (Dqk, tuple(q.shape)))
+        if q_out is None:
+            q_out = _empty((N, Hq, Dqk), torch.bfloat16, q.device, stream)
+        out_stride = _token_rows(q_out, N, "q_out")
+        if q_out.shape != q.shape:
+            raise ValueError("q_out: want %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
+    elif q_out is not None:
+        raise ValueError("q_out: there is no q")
+    _here(stream, q=q, k=k, v=v, slot=slot, position=position, k_pages=k_pages, v_pages=v_pages, inv_freq=inv_freq, q_out=q_out, status=status)
+    p = SeerAppendParams(N, Hq, Hkv, Dqk, Dv, P, num_pages, 1 if v is None else 0, int(rotary_at), R, 1 if interleaved else 0,
+                         q_stride, k_stride, v_stride, out_stride)
+    _check(lib.seer_kv_append(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(slot), _ptr(position), _ptr(inv_freq), _ptr(q_out), _ptr(k_pages),
+                              _ptr(v_pages), _ptr(status), _stream_handle(stream)))
+    return q_out

@@ -1,0 +1,462 @@
+// Pages, slots and positions of a step's new tokens: block tables kept on the device from request lengths alone.
+//
+// The state is page_refs (rows that hold a page, 0 = free) and each row's pages.  With need_b = ceil((ctx_b + n_b) / P), base_b =
+// pages the row holds or takes over from another row, grow_b = max(0, need_b - base_b) and the free pages in ascending order
+// f_0 < f_1 < .., row b gets f_(g_b) .. f_(g_b + grow_b - 1), g_b = sum of grow before b: two sums over rows, one list of the
+// free pages, and no list that would have to be kept from call to call.
+//
+// What bounds it: latency.  A step moves a few KB beside the 4 bytes a page of page_refs.  Three phases depend on one another:
+//   rows    records, shared pages counted up and released ones down
+//   pages   the free pages of every piece of the pool, in order (and the sums over the rows)
+//   give    a thread per new token finds its row, its page, its slot; the thread of a page's first position writes the page's
+//           entries, so tables and references cost no pass of their own
+// Pools of up to kSmallPages pages take one workgroup and one launch, in which a barrier separates the phases; beyond that they are three
+// launches.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/seer_verify.h"
+#include "seer_device.h"
+
+namespace seer {
+
+constexpr int kReserveMaxB = 16384;
+// one workgroup takes the call up to these sizes
+constexpr int kSmallThreads = 1024, kSmallPages = 32 * kSmallThreads, kSmallRows = kSmallThreads, kSmallTokens = 8192;
+constexpr int kThreads = 256;
+constexpr int kPieceStep = kThreads * 16;            // pages that a workgroup looks at together
+constexpr int kMaxPieces = 2048;
+constexpr int kTokensPerBlock = kThreads * 4;
+
+// A row of the call: positions and pages before it, pages it needs beside them (-1: refused, left as it is), new tokens (-1: over).
+struct ReserveRow {
+    int32_t ctx, base, grow, n;
+};
+
+struct ReserveArgs {
+    const int32_t* ctx_len;
+    const int32_t* n_new;
+    const int32_t* share_from;
+    const uint64_t* tree_mask;
+    int32_t* block_table;
+    int32_t* held;
+    int32_t* refs;
+    int32_t* step_len;
+    int32_t* first;
+    int32_t* slot;
+    int32_t* position;
+    int32_t* status;
+    ReserveRow* rows;        // [B]
+    int32_t* start;          // [B] sum of grow before the row
+    int32_t* counts;         // [pieces] free pages of a piece
+    int32_t* list;           // [pieces][piece] the free pages of a piece
+    int B, P, num_pages, max_pages, n_tokens, piece, pieces;
+};
+
+__device__ __forceinline__ void raise(const ReserveArgs& a, int bits) {
+    if (bits && a.status) atomicOr(a.status, bits);
+}
+
+// The record of row b, from the arrays as they are before the call; `before`: new tokens of the rows before it.  error: status bits.
+__device__ __forceinline__ ReserveRow reserve_row(const ReserveArgs& a, int b, int64_t before, int& error) {
+    ReserveRow r;
+    r.n = a.n_new[b], r.ctx = a.ctx_len[b], r.base = a.held[b], r.grow = -1;
+    const int share = a.share_from ? a.share_from[b] : -1;
+    error = 1;
+    if (r.n < -1 || r.base < 0 || r.base > a.max_pages) return r;
+    if (r.n < 0) {
+        r.ctx = 0, r.grow = 0, error = 0;
+        return r;
+    }
+    const int64_t end = static_cast<int64_t>(r.ctx) + r.n;
+    if (r.ctx < 0 || end > static_cast<int64_t>(a.max_pages) * a.P) return r;
+    if (share >= 0) {
+        if (share >= a.B || share == b || r.base != 0 || r.ctx % a.P != 0) return r;
+        const int theirs = a.held[share];
+        r.base = r.ctx / a.P;
+        if (theirs < 0 || theirs > a.max_pages || r.base > theirs) {
+            r.base = 0;
+            return r;
+        }
+    } else if (r.ctx > static_cast<int64_t>(r.base) * a.P) {
+        return r;
+    }
+    if (before + r.n > a.n_tokens) {
+        if (share >= 0) r.base = 0;
+        error = 4;
+        return r;
+    }
+    const int need = static_cast<int>((end + a.P - 1) / a.P);
+    r.grow = max(0, need - r.base), error = 0;
+    return r;
+}
+__device__ __forceinline__ int reserve_need(const ReserveArgs& a, const ReserveRow& r) {
+    return r.n < 0 ? 0 : static_cast<int>((static_cast<int64_t>(r.ctx) + r.n + a.P - 1) / a.P);
+}
+
+// Counts of the pages in row[from .. to) up or down, one wave (by = 0: looks whether one was given back more often than taken).
+__device__ __forceinline__ int count_pages(const ReserveArgs& a, const int32_t* row, int from, int to, int by, int lane) {
+    int error = 0;
+    for (int j = from + lane; j < to; j += kWave) {
+        const int page = row[j];
+        if (page < 0 || page >= a.num_pages) error |= 2;
+        else if (by != 0) atomicAdd(a.refs + page, by);
+        else if (__hip_atomic_load(a.refs + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0) error |= 16;
+    }
+    return error;
+}
+// Row b's shared pages up, or those that it no longer needs down.
+__device__ __forceinline__ int count_row(const ReserveArgs& a, int b, const ReserveRow& r, int lane) {
+    if (r.grow < 0) return 0;
+    const int share = a.share_from && r.n >= 0 ? a.share_from[b] : -1;
+    if (share >= 0) return count_pages(a, a.block_table + static_cast<size_t>(share) * a.max_pages, 0, r.base, 1, lane);
+    return count_pages(a, a.block_table + static_cast<size_t>(b) * a.max_pages, reserve_need(a, r), r.base, -1, lane);
+}
+// What a row holds from now on; `granted`: it got its pages.
+__device__ __forceinline__ int finish_row(const ReserveArgs& a, int b, const ReserveRow& r, bool granted, int lane) {
+    int error = 0;
+    const int share = a.share_from && r.grow >= 0 && r.n >= 0 ? a.share_from[b] : -1;
+    if (share >= 0) {
+        const int32_t* from = a.block_table + static_cast<size_t>(share) * a.max_pages;
+        if (granted) {
+            int32_t* to = a.block_table + static_cast<size_t>(b) * a.max_pages;
+            for (int j = lane; j < r.base; j += kWave) to[j] = from[j];
+        } else {
+            error = count_pages(a, from, 0, r.base, -1, lane);
+        }
+    } else if (r.grow >= 0) {
+        error = count_pages(a, a.block_table + static_cast<size_t>(b) * a.max_pages, reserve_need(a, r), r.base, 0, lane);
+    }
+    if (lane == 0) {
+        if (granted) a.held[b] = reserve_need(a, r);
+        a.step_len[b] = granted && r.n >= 0 ? r.ctx + r.n : 0;
+        if (r.grow >= 0 && !granted) error |= 8;
+    }
+    return error;
+}
+
+// Slot and position of new token i, of row b whose tokens begin at `begin`; page_at(rank): the rank-th free page.
+template <class PageAt>
+__device__ __forceinline__ int place_token(const ReserveArgs& a, int i, int b, int begin, const ReserveRow& r, int start, bool granted, PageAt&& page_at) {
+    int slot = -1, position = -1, error = 0;
+    if (granted) {
+        const int at = r.ctx + (i - begin), lp = at / a.P, inside = at - lp * a.P;
+        int32_t* entry = a.block_table + static_cast<size_t>(b) * a.max_pages + lp;
+        int page;
+        if (lp < r.base) {
+            page = *entry;
+        } else {
+            page = page_at(start + lp - r.base);
+            if (inside == 0) *entry = page, a.refs[page] = 1;       // (every position of a new page is a new token's, its first one too)
+        }
+        position = at;
+        if (page >= 0 && page < a.num_pages) slot = page * a.P + inside;
+        else error = 2;
+        if (a.tree_mask) {
+            const uint64_t word = a.tree_mask[i];
+            if (word) position = r.ctx + __popcll(word) - 1;
+        }
+    }
+    a.slot[i] = slot;
+    a.position[i] = position;
+    return error;
+}
+
+// The row of token i: the last one whose tokens begin at or before it (first[0 .. B], ascending; rows without tokens come before).
+__device__ __forceinline__ int row_of_token(const int32_t* first, int B, int i) {
+    int lo = 0, hi = B;                              // first[lo] <= i; first[hi] > i or hi == B
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+    return v;
+}
+// Sum of v over the threads before this one; total: over all.  Ends behind a barrier.
+template <int THREADS>
+__device__ __forceinline__ int64_t block_before(int64_t v, int64_t* s_sums, int64_t& total) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    int64_t up = v;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int64_t x = __shfl_up(up, o, kWave);
+        if (lane >= o) up += x;
+    }
+    if (lane == kWave - 1) s_sums[wave] = up;
+    __syncthreads();
+    int64_t before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / kWave; ++w) {
+        if (w < wave) before += s_sums[w];
+        total += s_sums[w];
+    }
+    __syncthreads();
+    return before + up - v;
+}
+__device__ __forceinline__ int32_t saturate(int64_t x) { return x > 0x7fffffff ? 0x7fffffff : static_cast<int32_t>(x); }
+
+// Which of ROWS * 64 pages from page0 on are free: lane x < ROWS gets the bits of pages page0 + 64 x ...  (Read past the vector cache: another
+// workgroup, or this one, may have counted them a moment ago.)
+template <int ROWS>
+__device__ __forceinline__ uint64_t free_pages(const ReserveArgs& a, int64_t page0, int64_t end) {
+    const int lane = threadIdx.x & (kWave - 1);
+    int refs[ROWS];
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x)
+        refs[x] = __hip_atomic_load(a.refs + min(page0 + x * kWave + lane, static_cast<int64_t>(a.num_pages) - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    uint64_t mine = 0;
+#pragma unroll
+    for (int x = 0; x < ROWS; ++x) {
+        const uint64_t bits = __ballot(refs[x] == 0 && page0 + x * kWave + lane < end);
+        if (lane == x) mine = bits;
+    }
+    return mine;
+}
+// Writes those pages behind one another, lane x's at `at` and on, as far as `limit`.
+template <int ROWS>
+__device__ __forceinline__ void write_pages(int32_t* list, int limit, int page0, uint64_t mine, int at) {
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int x = 0; x < ROWS; ++x) {
+        const uint64_t bits = static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(mine >> 32), x))) << 32 |
+                              static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(mine), x));
+        const int to = __builtin_amdgcn_readlane(at, x) + __popcll(bits & ((1ull << lane) - 1));
+        if (((bits >> lane) & 1) && to < limit) list[to] = page0 + x * kWave + lane;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// one workgroup
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kSmallThreads) void reserve_small(ReserveArgs a) {
+    __shared__ ReserveRow s_row[kSmallRows];
+    __shared__ int32_t s_first[kSmallRows + 1], s_start[kSmallRows];
+    __shared__ int32_t s_list[kSmallTokens];
+    __shared__ int64_t s_sums[kSmallThreads / kWave];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    int error = 0;
+    int64_t total;
+    {
+        const int64_t mine = tid < a.B ? max(a.n_new[tid], 0) : 0;
+        const int64_t before = block_before<kSmallThreads>(mine, s_sums, total);
+        int64_t grow = 0;
+        if (tid < a.B) {
+            const ReserveRow r = reserve_row(a, tid, before, error);
+            s_row[tid] = r, s_first[tid] = saturate(before), a.first[tid] = saturate(before);
+            grow = max(r.grow, 0);
+            if (tid == a.B - 1) s_first[a.B] = saturate(total), a.first[a.B] = saturate(total);
+        }
+        const int64_t start = block_before<kSmallThreads>(grow, s_sums, total);
+        if (tid < a.B) s_start[tid] = saturate(start);
+    }
+    __syncthreads();
+    for (int b = wave; b < a.B; b += kSmallThreads / kWave) error |= count_row(a, b, s_row[b], lane);
+    __threadfence();
+    __syncthreads();                                 // the counts are what they are before pages are given
+    const int wanted = saturate(total);
+    int64_t free_total;
+    {
+        constexpr int kRows = kSmallPages / kSmallThreads;                     // (of 64 pages, a wave)
+        const int page0 = wave * kRows * kWave;
+        uint64_t mine = 0;
+        if (wanted > 0 && page0 < a.num_pages) mine = free_pages<kRows>(a, page0, a.num_pages);
+        const int at = static_cast<int>(block_before<kSmallThreads>(__popcll(mine), s_sums, free_total));
+        if (__any(mine != 0)) write_pages<kRows>(s_list, min(wanted, kSmallTokens), page0, mine, at);
+    }
+    __syncthreads();
+    auto granted = [&](int b) { return s_row[b].grow == 0 || (s_row[b].grow > 0 && static_cast<int64_t>(s_start[b]) + s_row[b].grow <= free_total); };
+    for (int b = wave; b < a.B; b += kSmallThreads / kWave) error |= finish_row(a, b, s_row[b], granted(b), lane);
+    for (int i = tid; i < a.n_tokens; i += kSmallThreads) {
+        const bool real = i < s_first[a.B];
+        const int b = row_of_token(s_first, a.B, i);
+        error |= place_token(a, i, b, s_first[b], s_row[b], s_start[b], real && granted(b), [&](int rank) { return s_list[rank]; });
+    }
+    raise(a, error);
+}
+
+// ---------------------------------------------------------------------------
+// three launches
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads) void reserve_rows(ReserveArgs a) {
+    const int lane = threadIdx.x & (kWave - 1), b = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
+    if (b >= a.B) return;
+    int64_t before = 0;
+    for (int i = lane; i < b; i += kWave) before += max(a.n_new[i], 0);
+    before = wave_sum64(before);
+    int error;
+    const ReserveRow r = reserve_row(a, b, before, error);
+    if (lane == 0) {
+        a.rows[b] = r;
+        a.first[b] = saturate(before);
+        if (b == a.B - 1) a.first[a.B] = saturate(before + max(r.n, 0));
+    }
+    error |= count_row(a, b, r, lane);
+    raise(a, error);
+}
+
+// Workgroup 0: the sums of grow.  The others: the free pages of a piece of the pool, in order.
+__global__ __launch_bounds__(kThreads) void reserve_pages(ReserveArgs a) {
+    __shared__ int64_t s_sums[kThreads / kWave];
+    const int tid = threadIdx.x;
+    int64_t total;
+    if (blockIdx.x == 0) {
+        int64_t sum = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+            const int b = b0 + tid;
+            const int64_t before = block_before<kThreads>(b < a.B ? max(a.rows[b].grow, 0) : 0, s_sums, total);
+            if (b < a.B) a.start[b] = saturate(sum + before);
+            sum += total;
+        }
+        return;
+    }
+    const int piece = blockIdx.x - 1, first = piece * a.piece, end = min(first + a.piece, a.num_pages);
+    int32_t* list = a.list + first;
+    int count = 0;
+    for (int page0 = first; page0 < end; page0 += kPieceStep) {
+        constexpr int kRows = kPieceStep / kThreads;
+        const int wave0 = page0 + tid / kWave * kRows * kWave;
+        const uint64_t mine = free_pages<kRows>(a, wave0, end);
+        const int at = count + static_cast<int>(block_before<kThreads>(__popcll(mine), s_sums, total));
+        write_pages<kRows>(list, a.piece, wave0, mine, at);
+        count += static_cast<int>(total);
+    }
+    if (tid == 0) a.counts[piece] = count;
+}
+
+constexpr int kFirstInLds = 4096;
+
+__global__ __launch_bounds__(kThreads) void reserve_give(ReserveArgs a, int token_blocks) {
+    __shared__ int32_t s_before[kMaxPieces + 1];      // free pages of the pieces before
+    __shared__ int32_t s_first[kFirstInLds + 1];
+    __shared__ int64_t s_sums[kThreads / kWave];
+    const int tid = threadIdx.x;
+    int64_t sum = 0, total;
+    for (int p0 = 0; p0 < a.pieces; p0 += kThreads) {
+        const int64_t before = block_before<kThreads>(p0 + tid < a.pieces ? a.counts[p0 + tid] : 0, s_sums, total);
+        if (p0 + tid < a.pieces) s_before[p0 + tid] = static_cast<int32_t>(sum + before);
+        sum += total;
+    }
+    const int64_t free_total = sum;
+    auto granted = [&](const ReserveRow& r, int start) { return r.grow == 0 || (r.grow > 0 && static_cast<int64_t>(start) + r.grow <= free_total); };
+    int error = 0;
+    if (static_cast<int>(blockIdx.x) >= token_blocks) {
+        const int lane = tid & (kWave - 1), b = (blockIdx.x - token_blocks) * (kThreads / kWave) + tid / kWave;
+        if (b < a.B) {
+            const ReserveRow r = a.rows[b];
+            error = finish_row(a, b, r, granted(r, a.start[b]), lane);
+        }
+        raise(a, error);
+        return;
+    }
+    const bool in_lds = a.B <= kFirstInLds;
+    if (in_lds)
+        for (int b = tid; b <= a.B; b += kThreads) s_first[b] = a.first[b];
+    __syncthreads();
+    const int32_t* first = in_lds ? s_first : a.first;
+    auto page_at = [&](int rank) {
+        int lo = 0, hi = a.pieces;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (s_before[mid] <= rank) lo = mid;
+            else hi = mid;
+        }
+        return a.list[static_cast<size_t>(lo) * a.piece + (rank - s_before[lo])];
+    };
+#pragma unroll
+    for (int x = 0; x < kTokensPerBlock / kThreads; ++x) {
+        const int64_t i = static_cast<int64_t>(blockIdx.x) * kTokensPerBlock + x * kThreads + tid;
+        if (i >= a.n_tokens) break;
+        const bool real = i < first[a.B];
+        const int b = row_of_token(first, a.B, static_cast<int>(i));
+        const ReserveRow r = a.rows[b];
+        const int start = a.start[b];
+        error |= place_token(a, static_cast<int>(i), b, first[b], r, start, real && granted(r, start), page_at);
+    }
+    raise(a, error);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+static int check_reserve_params(const seer_reserve_params* p) {
+    if (!p) return SEER_EINVAL;
+    if (p->B < 0 || p->page_size < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1 || p->n_tokens < 0) return SEER_EINVAL;
+    if (p->B > kReserveMaxB || p->num_pages > 1 << 30 || static_cast<int64_t>(p->num_pages) * p->page_size > 0x7fffffffLL || p->n_tokens > 0x7fffffff - (1 << 20)) return SEER_ESHAPE;
+    if (static_cast<int64_t>(p->max_pages_per_seq) * p->page_size > 0x7fffffffLL) return SEER_ESHAPE;
+    return SEER_OK;
+}
+inline bool reserve_is_small(const seer_reserve_params& p) { return p.num_pages <= kSmallPages && p.B <= kSmallRows && p.n_tokens <= kSmallTokens; }
+struct ReserveLayout {
+    int piece, pieces;
+    size_t off_start, off_counts, off_list, total;
+};
+inline ReserveLayout reserve_layout(const seer_reserve_params& p) {
+    ReserveLayout w{};
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    const int64_t share = (static_cast<int64_t>(p.num_pages) + kMaxPieces - 1) / kMaxPieces;
+    w.piece = static_cast<int>((share + kPieceStep - 1) / kPieceStep) * kPieceStep;
+    w.pieces = static_cast<int>((static_cast<int64_t>(p.num_pages) + w.piece - 1) / w.piece);
+    w.off_start = up(sizeof(ReserveRow) * p.B);
+    w.off_counts = w.off_start + up(sizeof(int32_t) * p.B);
+    w.off_list = w.off_counts + up(sizeof(int32_t) * w.pieces);
+    w.total = reserve_is_small(p) ? 256 : w.off_list + up(sizeof(int32_t) * p.num_pages);
+    return w;
+}
+
+}  // namespace seer
+
+extern "C" size_t seer_kv_reserve_workspace(const seer_reserve_params* p) {
+    if (seer::check_reserve_params(p) != SEER_OK || p->B == 0) return 0;
+    return seer::reserve_layout(*p).total;
+}
+
+extern "C" int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_len, const int32_t* n_new, const int32_t* share_from,
+                               const uint64_t* tree_mask, int32_t* block_table, int32_t* pages_held, int32_t* page_refs, int32_t* step_len,
+                               int32_t* first_token, int32_t* slot, int32_t* position, int32_t* status, void* workspace,
+                               size_t workspace_bytes, void* hip_stream) {
+    const int rc = seer::check_reserve_params(p);
+    if (rc != SEER_OK) return rc;
+    if (p->B == 0) return SEER_OK;
+    if (!ctx_len || !n_new || !block_table || !pages_held || !page_refs || !step_len || !first_token || (p->n_tokens > 0 && (!slot || !position)))
+        return SEER_EINVAL;
+    if (step_len == ctx_len || step_len == n_new) return SEER_EINVAL;
+    const seer::ReserveLayout layout = seer::reserve_layout(*p);
+    if (!workspace || workspace_bytes < layout.total) return SEER_EWORKSPACE;
+    auto misaligned = [](const void* ptr, uintptr_t a) { return reinterpret_cast<uintptr_t>(ptr) % a != 0; };
+    if (misaligned(page_refs, 16) || misaligned(workspace, 16) || misaligned(tree_mask, 8) || misaligned(ctx_len, 4) || misaligned(n_new, 4) ||
+        misaligned(share_from, 4) || misaligned(block_table, 4) || misaligned(pages_held, 4) || misaligned(step_len, 4) || misaligned(first_token, 4) ||
+        misaligned(slot, 4) || misaligned(position, 4) || misaligned(status, 4))
+        return SEER_EALIGN;
+    seer::ReserveArgs a{};
+    a.ctx_len = ctx_len, a.n_new = n_new, a.share_from = share_from, a.tree_mask = tree_mask;
+    a.block_table = block_table, a.held = pages_held, a.refs = page_refs, a.step_len = step_len, a.first = first_token;
+    a.slot = slot, a.position = position, a.status = status;
+    a.B = p->B, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq, a.n_tokens = p->n_tokens;
+    a.piece = layout.piece, a.pieces = layout.pieces;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (seer::reserve_is_small(*p)) {
+        hipLaunchKernelGGL(seer::reserve_small, dim3(1), dim3(seer::kSmallThreads), 0, stream, a);
+        const hipError_t err = hipGetLastError();
+        return err == hipSuccess ? SEER_OK : static_cast<int>(err);
+    }
+    char* ws = static_cast<char*>(workspace);
+    a.rows = reinterpret_cast<seer::ReserveRow*>(ws);
+    a.start = reinterpret_cast<int32_t*>(ws + layout.off_start);
+    a.counts = reinterpret_cast<int32_t*>(ws + layout.off_counts);
+    a.list = reinterpret_cast<int32_t*>(ws + layout.off_list);
+    const unsigned row_blocks = (p->B + seer::kThreads / seer::kWave - 1) / (seer::kThreads / seer::kWave);
+    const int token_blocks = (p->n_tokens + seer::kTokensPerBlock - 1) / seer::kTokensPerBlock;
+    hipLaunchKernelGGL(seer::reserve_rows, dim3(row_blocks), dim3(seer::kThreads), 0, stream, a);
+    hipLaunchKernelGGL(seer::reserve_pages, dim3(1u + layout.pieces), dim3(seer::kThreads), 0, stream, a);
+    hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return static_cast<int>(err);
+    hipLaunchKernelGGL(seer::reserve_give, dim3(token_blocks + row_blocks), dim3(seer::kThreads), 0, stream, a, token_blocks);
+    err = hipGetLastError();
+    return err == hipSuccess ? SEER_OK : static_cast<int>(err);
+}

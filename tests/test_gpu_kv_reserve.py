@@ -1,0 +1,212 @@
+"""seer_kv_reserve against the plain implementation, exactly: random steps of a server that starts, continues, cuts and ends requests, on
+pools of one workgroup and of several, and every case in which a row is left as it was."""
+import random
+
+import pytest
+import torch
+
+from reserve_reference import reserve
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(x, dtype=torch.int32):
+    return None if x is None else torch.tensor(x, dtype=dtype, device="cuda")
+
+
+def signed(words):
+    return None if words is None else [w - 2 ** 64 if w >= 2 ** 63 else w for w in words]
+
+
+def check(table, held, refs, ctx, new, share, mask, n_tokens, page, **kw):
+    """Runs the call and the plain implementation on copies of the state; returns the plain one's results."""
+    from paper_2511_14617_amd import binding as b
+    want = reserve(table, held, refs, ctx, new, share, mask, n_tokens, page)
+    t, h, r, status = dev(table), dev(held), dev(refs), dev([0])
+    got = b.seer_kv_reserve(t, h, r, dev(ctx), dev(new), n_tokens, page, share_from=dev(share), tree_mask=dev(signed(mask), torch.int64),
+                            status=status, **kw)
+    torch.cuda.synchronize()
+    for name, x, y in zip(("pages_held", "page_refs", "step_len", "first_token", "slot", "position", "status", "block_table"),
+                          (h, r, *got, status, t), (want[1], want[2], want[3], want[4], want[5], want[6], [want[7]], want[0])):
+        assert x.cpu().tolist() == y, name
+    return want
+
+
+class Server:
+    """A pool and its rows, with random requests."""
+
+    def __init__(self, seed, B, pages, width, page):
+        self.rng, self.page, self.width = random.Random(seed), page, width
+        self.table, self.held, self.refs = [[0] * width for _ in range(B)], [0] * B, [0] * pages
+        self.len = [0] * B
+
+    def ask(self, longest, pad=0):
+        rng, B = self.rng, len(self.held)
+        ctx, new, share = self.len[:], [0] * B, [-1] * B
+        for b in range(B):
+            x = rng.random()
+            if self.held[b] == 0:
+                if x < 0.5:
+                    donor = rng.randrange(B)
+                    if donor != b and self.held[donor] and rng.random() < 0.6:
+                        ctx[b] = rng.randint(0, self.len[donor] // self.page) * self.page
+                        share[b] = donor
+                    new[b] = rng.randint(0, longest)
+            elif x < 0.15:
+                new[b] = -1
+            elif x < 0.3:
+                ctx[b] = rng.randint(0, self.len[b])                 # (cut, or a step that accepted little)
+                new[b] = rng.randint(0, 3)
+            elif x < 0.9:
+                new[b] = rng.randint(0, 20)
+            if new[b] > 0:
+                new[b] = min(new[b], self.width * self.page - ctx[b])
+        tokens = sum(max(n, 0) for n in new) + pad
+        mask = None
+        if rng.random() < 0.5:
+            mask = [0 if rng.random() < 0.5 else rng.getrandbits(64) | 1 for _ in range(tokens)]
+        return ctx, new, share, mask, tokens
+
+    def step(self, longest, pad=0, **kw):
+        ctx, new, share, mask, tokens = self.ask(longest, pad)
+        self.table, self.held, self.refs, step, *_ , status = check(self.table, self.held, self.refs, ctx, new, share, mask, tokens, self.page, **kw)
+        assert status in (0, 8)
+        assert sum(self.refs) == sum(self.held)                      # (every held page is counted)
+        for b in range(len(new)):
+            if new[b] == -1:
+                self.len[b] = 0
+            elif step[b] or (self.held[b] * self.page >= ctx[b] and ctx[b] + max(new[b], 0) == 0):
+                self.len[b] = step[b]
+
+
+# (pools of up to 32 768 pages, 1024 rows and 8192 tokens take one workgroup)
+@pytest.mark.parametrize("seed,B,pages,width,page,longest", [
+    (1, 1, 3, 3, 16, 40), (2, 7, 40, 9, 16, 100), (3, 33, 200, 12, 1, 12), (4, 64, 5000, 60, 16, 700), (5, 5, 64, 30, 7, 150),
+    (6, 130, 32768, 100, 4, 60), (7, 65, 32769, 40, 16, 300), (8, 40, 70000, 300, 3, 700), (9, 1025, 4000, 8, 16, 10), (10, 300, 2500, 50, 20, 900)])
+def test_steps_of_a_server(seed, B, pages, width, page, longest):
+    server = Server(seed, B, pages, width, page)
+    for k in range(6):
+        server.step(longest, pad=(0, 5, 0, 300, 1, 0)[k])
+
+
+@pytest.mark.parametrize("pages", [64, 40000])
+def test_rows_that_are_left_as_they_were(pages):
+    page, width = 4, 6
+    table = [[10, 11, 12, 0, 0, 0], [13, 14, 0, 0, 0, 0], [0] * 6, [0] * 6, [15, 0, 0, 0, 0, 0], [0] * 6, [16, 17, 0, 0, 0, 0], [0] * 6]
+    held = [3, 2, 0, 0, 1, 0, 2, 0]
+    refs = [0] * pages
+    for row, h in zip(table, held):
+        for p in row[:h]:
+            refs[p] += 1
+    good = [12, 6, 0, 0, 3, 0, 8, 0]
+
+    def run(status, **change):
+        ctx, new, share = good[:], [2, 1, 5, 1, 4, 1, 0, 0], [-1] * 8
+        for b, (c, n, s) in change.items():
+            ctx[int(b[1:])], new[int(b[1:])], share[int(b[1:])] = c, n, s
+        out = check(table, held, refs, ctx, new, share, None, sum(max(n, 0) for n in new), page)
+        assert out[7] == status, change
+
+    run(0)
+    run(1, r0=(13, 2, -1))                 # more positions than the pages that it holds
+    run(1, r0=(-1, 2, -1))
+    run(1, r0=(12, 13, -1))                # beyond the table
+    run(1, r1=(6, -2, -1))
+    run(1, r2=(4, 5, 8))                   # no such row
+    run(1, r2=(4, 5, 2))                   # itself
+    run(1, r2=(5, 5, 0))                   # not a whole page
+    run(1, r2=(16, 5, 0))                  # more than that row holds
+    run(1, r0=(8, 2, 1))                   # holds pages of its own
+    run(0, r2=(12, 5, 0), r3=(8, 1, 0), r0=(0, -1, 0))       # two rows take over from one that is over
+    run(0, r2=(0, 5, 0))
+    run(1, r2=(4, 0, 3))                   # from a row without pages
+
+
+@pytest.mark.parametrize("pages", [12, 33000])
+def test_pool_runs_out(pages):
+    """Rows are served in order; a shared prompt of a row that gets nothing is counted down again; what is over is free at once."""
+    page, width = 2, 10
+    B = 7
+    used = pages - 6
+    table, held, refs = [[0] * width for _ in range(B)], [0] * B, [1] * used + [0] * 6
+    table[0][:2], held[0] = [0, 1], 2
+    table[6][:3], held[6] = [2, 3, 4], 3
+    out = check(table, held, refs, [4, 0, 2, 0, 0, 0, 6], [1, 7, 9, 2, 1, 1, -1], [-1, -1, 0, -1, -1, -1, -1], None, 40, page)
+    assert out[7] == 8 and out[3] == [5, 7, 0, 0, 0, 0, 0] and out[1] == [3, 4, 0, 0, 0, 0, 0]
+    # (rows 3 to 5 would fit, but rows are served in order)
+    out = check(table, held, refs, [4, 0, 2, 0, 0, 0, 6], [1, 7, 4, 2, 1, 1, -1], [-1, -1, 0, -1, -1, -1, -1], None, 40, page)
+    assert out[3] == [5, 7, 6, 2, 1, 0, 0] and out[7] == 8
+    check(table, held, refs, [4, 0, 2, 0, 0, 0, 6], [0, 20, 4, 2, 1, 1, 0], [-1, -1, 0, -1, -1, -1, -1], None, 40, page)
+
+
+@pytest.mark.parametrize("pages", [20, 33000])
+def test_pages_of_the_caller_and_wrong_tables(pages):
+    page, width = 2, 6
+    refs = [5] + [1] * 9 + [0] * (pages - 10)
+    table = [[0, 1, 2, 0, 0, 0], [3, 99999999, -7, 4, 0, 0], [5, 5, 0, 0, 0, 0], [0] * 6, [0] * 6]
+    held = [3, 4, 2, 0, 0]
+    out = check(table, held, refs, [0, 0, 0, 6, 4], [-1, -1, -1, 1, 3], [-1, -1, -1, 0, 1], None, 9, page)
+    assert out[7] == 2 | 16 and out[2][0] == 5 and out[2][5] == -1
+    out = check(table, held, refs, [5, 7, 4, 0, 4], [1, 1, 0, 0, 0], [-1, -1, -1, -1, 1], None, 3, page)
+    assert out[7] == 2 and out[5] == [2 * 2 + 1, 4 * 2 + 1, -1]
+    out = check(table, held, refs, [5, 4, 4, 0, 0], [1, 2, 0, 0, 0], None, None, 3, page)
+    assert out[5] == [5, -1, -1] and out[6] == [5, 4, 5] and out[7] & 2
+
+
+@pytest.mark.parametrize("pages", [30, 40000])
+def test_more_tokens_than_room(pages):
+    table, held, refs = [[0] * 8 for _ in range(4)], [0] * 4, [0] * pages
+    out = check(table, held, refs, [0] * 4, [3, 4, 5, 0], None, None, 9, 4)
+    assert out[7] == 4 and out[3] == [3, 4, 0, 0] and out[4] == [0, 3, 7, 12, 12]
+    out = check(table, held, refs, [0] * 4, [3, 2 ** 31 - 1, 2 ** 31 - 1, 2], None, None, 9, 4)
+    assert out[7] == 1 | 4 and out[4] == [0, 3, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1]
+    check(table, held, refs, [0] * 4, [0, 0, 0, 0], None, None, 0, 4)
+    check(table, held, refs, [0] * 4, [-1, -1, -1, -1], None, None, 5, 4)
+
+
+def test_tables_behind_what_a_row_holds_stay(page=4):
+    table, held, refs = [[7, 8, 9, 77, 78, 79], [5] * 6], [3, 0], [0] * 7 + [1] * 3 + [0] * 10
+    out = check(table, held, refs, [4, 0], [0, 0], None, None, 2, page)
+    assert out[0] == table and out[1] == [1, 0]
+
+
+@pytest.mark.parametrize("pages,tokens", [(20000, 3000), (200000, 3000), (20000, 9000)])
+def test_captured_and_replayed(pages, tokens):
+    """A captured step on buffers that change from replay to replay, against eager calls; another stream beside it."""
+    from paper_2511_14617_amd import binding as b
+    server = Server(20, 40, pages, 100, 16)
+    state = [dev(server.table), dev(server.held), dev(server.refs)]
+    ctx, new, share, mask, status = dev([0] * 40), dev([0] * 40), dev([-1] * 40), dev([0] * tokens, torch.int64), dev([0])
+    out = (dev([0] * 40), dev([0] * 41), dev([0] * tokens), dev([0] * tokens))
+    ws = torch.empty(max(256, b.seer_kv_reserve_workspace(b.SeerReserveParams(40, 16, pages, 100, tokens))), dtype=torch.uint8, device="cuda")
+    call = lambda: b.seer_kv_reserve(*state, ctx, new, tokens, 16, share_from=share, tree_mask=mask, out=out, status=status, workspace=ws)
+    call()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            call()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        c, n, s, m, t = server.ask(tokens // 60)
+        m = (m or [0] * t) + [0] * (tokens - t)
+        want = reserve(server.table, server.held, server.refs, c, n, s, m, tokens, 16)
+        ctx.copy_(dev(c)), new.copy_(dev(n)), share.copy_(dev(s)), mask.copy_(dev(signed(m), torch.int64))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert [x.tolist() for x in (*state, *out)] == list(want[:7])
+        server.table, server.held, server.refs = want[:3]
+        server.len = [0 if n[b] == -1 else max(want[3][b], 0) if want[3][b] else min(server.len[b], want[1][b] * 16) for b in range(40)]
+
+
+def test_own_stream():
+    from paper_2511_14617_amd import binding as b
+    stream = torch.cuda.Stream()
+    for pages in (1000, 50000):
+        table, held, refs = [[0] * 70 for _ in range(9)], [0] * 9, [0] * pages
+        want = reserve(table, held, refs, [0] * 9, [100 * b for b in range(9)], None, None, 3601, 16)
+        t, h, r, c, n = dev(table), dev(held), dev(refs), dev([0] * 9), dev([100 * b for b in range(9)])
+        torch.cuda.synchronize()
+        got = b.seer_kv_reserve(t, h, r, c, n, 3601, 16, stream=stream)
+        stream.synchronize()
+        assert [x.tolist() for x in (t, h, r, *got)] == list(want[:7])
