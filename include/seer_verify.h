@@ -663,6 +663,35 @@ SEER_API int seer_kv_append(const seer_append_params* p, const void* q, const vo
                    const int32_t* position, const float* inv_freq, void* q_out, void* k_pages, void* v_pages, int32_t* status,
                    void* hip_stream);
 
+/* Bytes of device scratch seer_prompt_attention needs; 0 on invalid params.  Host-only. */
+SEER_API size_t seer_prompt_attention_workspace(const seer_attn_params* p, int32_t n_tokens);
+
+/*
+ * Causal attention of packed tokens over the paged cache.  Request b's tokens are its last n_b = first_token[b + 1] -
+ * first_token[b] positions, their keys and values already in the cache; its i-th token sees positions 0 .. ctx_len[b] - n_b + i:
+ *   out[first_token[b] + i, h, :] = softmax_j(scale * q[.., h, :] . K[j, h/G, :]) . V[j, h/G, :],
+ * with scores, sums and outputs in fp32, rounded to bf16 once (nearest even); probabilities enter the product with V as bf16.
+ * Any mix of lengths: whole prompts, pieces of prompts behind a cached beginning, single tokens, requests without a token.
+ * The result depends on the arguments only.  A key or value with a NaN or an infinity in a position that a token does not see does
+ * not reach it; rows behind the last request's are left as they are.
+ *
+ *  out           device [n_tokens,Hq,Dv]  bf16, written
+ *  q             device [n_tokens,Hq,Dqk] bf16
+ *  k_pages, v_pages, block_table  as for seer_verify_attention
+ *  ctx_len       device [B] int32, INCLUDING the new tokens (seer_kv_reserve's step_len)
+ *  first_token   device [B+1] int32, ascending from 0 or more to at most n_tokens
+ *  p             host; T, max_splits and flags are not looked at.  (Dqk, Dv) in {(64,64), (128,128), (192,128), (256,256)}, any
+ *                page_size
+ *  status        device [1] int32 or NULL; bits are OR-ed in: 1 = a ctx_len below n_b or beyond the block table (the request's rows
+ *                are zeros), 2 = a page id outside the pool (it is clamped into the pool), 4 = first_token not ascending or
+ *                beyond n_tokens (the request's rows are left as they are).  The caller clears it.
+ *  workspace     device, >= seer_prompt_attention_workspace(p, n_tokens) bytes, 256-byte aligned
+ * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
+ */
+SEER_API int seer_prompt_attention(void* out, const void* q, const void* k_pages, const void* v_pages, const int32_t* block_table,
+                          const int32_t* ctx_len, const int32_t* first_token, const seer_attn_params* p, int32_t n_tokens,
+                          int32_t* status, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static text for a return code of either call (negative SEER_E*, or a
  * positive hipError_t). */
 SEER_API const char* seer_strerror(int code);

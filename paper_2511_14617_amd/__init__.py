@@ -13,7 +13,7 @@ def __getattr__(name):
                 "seer_accept_sampled", "seer_kv_commit", "seer_mba_draft_lengths", "seer_draft", "seer_draft_workspace", "seer_history_append",
                 "seer_token_logprobs", "seer_token_logprobs_workspace", "seer_token_logprobs_grad", "SeerLogprobParams",
                 "seer_kv_weights", "seer_kv_weights_workspace", "seer_kv_evict", "seer_kv_evict_workspace", "SeerEvictParams",
-                "seer_kv_reserve", "seer_kv_reserve_workspace", "seer_kv_append", "SeerReserveParams", "SeerAppendParams",
+                "seer_kv_reserve", "seer_kv_reserve_workspace", "seer_kv_append", "seer_prompt_attention", "seer_prompt_attention_workspace", "SeerReserveParams", "SeerAppendParams",
                 "SeerDraftParams",
                 "SeerAttnParams", "SeerError", "attn_params"):
         from . import binding

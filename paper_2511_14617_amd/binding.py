@@ -25,7 +25,8 @@ EXPORTS = ("seer_verify_attention_workspace", "seer_verify_attention_status_offs
            "seer_kv_commit", "seer_mba_draft_lengths", "seer_acceptance_stats", "seer_acceptance_beta", "seer_draft_workspace", "seer_draft", "seer_history_append",
            "seer_token_logprobs_workspace", "seer_token_logprobs", "seer_token_logprobs_grad",
            "seer_kv_weights_workspace", "seer_kv_weights", "seer_kv_evict_workspace", "seer_kv_evict",
-           "seer_kv_reserve_workspace", "seer_kv_reserve", "seer_kv_append", "seer_strerror")
+           "seer_kv_reserve_workspace", "seer_kv_reserve", "seer_kv_append",
+           "seer_prompt_attention_workspace", "seer_prompt_attention", "seer_strerror")
 
 
 class SeerAttnParams(ctypes.Structure):
@@ -144,6 +145,10 @@ def load_library() -> ctypes.CDLL:
         lib.seer_kv_reserve.restype = ctypes.c_int
         lib.seer_kv_append.argtypes = [ctypes.POINTER(SeerAppendParams)] + [vp] * 11
         lib.seer_kv_append.restype = ctypes.c_int
+        lib.seer_prompt_attention_workspace.argtypes = [ctypes.POINTER(SeerAttnParams), i32]
+        lib.seer_prompt_attention_workspace.restype = sz
+        lib.seer_prompt_attention.argtypes = [vp] * 7 + [ctypes.POINTER(SeerAttnParams), i32, vp, vp, sz, vp]
+        lib.seer_prompt_attention.restype = ctypes.c_int
         lib.seer_strerror.argtypes = [ctypes.c_int]
         lib.seer_strerror.restype = ctypes.c_char_p
         _lib = lib
@@ -787,3 +792,45 @@ def seer_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch
     _check(lib.seer_kv_append(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(slot), _ptr(position), _ptr(inv_freq), _ptr(q_out), _ptr(k_pages),
                               _ptr(v_pages), _ptr(status), _stream_handle(stream)))
     return q_out
+
+
+def seer_prompt_attention_workspace(params: SeerAttnParams, n_tokens: int) -> int:
+    return int(load_library().seer_prompt_attention_workspace(ctypes.byref(params), n_tokens))
+
+
+def seer_prompt_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], block_table: torch.Tensor,
+                          ctx_len: torch.Tensor, first_token: torch.Tensor, scale: float, *, Dv: Optional[int] = None,
+                          out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Causal attention of packed tokens q [n_tokens,Hq,Dqk] bf16 over the paged cache: out [n_tokens,Hq,Dv] bf16.  Request b's tokens are
+    first_token[b] .. first_token[b+1]-1 ([B+1] int32) and the last positions of its ctx_len[b] ([B] int32, e.g. the step_len of
+    seer_kv_reserve); rows behind the last request's are left as they are.  k_pages, v_pages (None: shared latent) and block_table as for
+    seer_verify_attention."""
+    lib = load_library()
+    if q.dim() != 3 or k_pages.dim() != 4 or block_table.dim() != 2:
+        raise ValueError("want q [n_tokens,Hq,Dqk], k_pages [num_pages,Hkv,page,Dqk] and block_table [B,max_pages]")
+    N, Hq, Dqk = q.shape
+    B = block_table.shape[0]
+    p = attn_params(q.unsqueeze(1), k_pages, v_pages, block_table, scale, Dv)
+    p.B = B
+    _want(q, torch.bfloat16, (N, Hq, Dqk), "q")
+    _want(k_pages, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size, Dqk), "k_pages")
+    if v_pages is not None:
+        _want(v_pages, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size, p.Dv), "v_pages")
+    _want(block_table, torch.int32, (B, p.max_pages_per_seq), "block_table")
+    _want(ctx_len, torch.int32, (B,), "ctx_len")
+    _want(first_token, torch.int32, (B + 1,), "first_token")
+    if out is None:
+        out = _empty((N, Hq, p.Dv), torch.bfloat16, q.device, stream)
+    else:
+        _want(out, torch.bfloat16, (N, Hq, p.Dv), "out")
+    if status is not None:
+        _want(status, torch.int32, (1,), "status")
+    if workspace is None:
+        need = int(lib.seer_prompt_attention_workspace(ctypes.byref(p), N))
+        workspace = _empty(max(need, 256), torch.uint8, q.device, stream)
+    _here(stream, q=q, k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, first_token=first_token, out=out, status=status,
+          workspace=workspace)
+    _check(lib.seer_prompt_attention(_ptr(out), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(ctx_len), _ptr(first_token),
+                                     ctypes.byref(p), N, _ptr(status), _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+    return out

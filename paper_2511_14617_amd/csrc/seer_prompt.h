@@ -1,0 +1,217 @@
+// Work of the prompt attention kernels: how packed tokens of requests of any length are cut into equal shares, on the device.
+//
+// Rows: a request's n tokens times the G heads that share a KV head are n G consecutive query rows (row r = token r / G, head r % G), cut into
+// row tiles of kRowTile.  A row tile reads the positions that its last row sees, so its cost grows along a prompt: with past = ctx - n
+// cached positions before the new ones, row tile i of a request costs (in units of a position times a head of the group)
+//     c_i = G past + kRowTile (i + 1) + kTileCost,     i < R = ceil(n G / kRowTile).
+// All row tiles -- requests in order, their KV heads in order, their row tiles in order -- lie end to end on one line, whose
+// prefix sums have closed forms in i and in the KV head, and whose sums over requests are one scan.  Workgroup w of W takes the stretch from
+// x_w = total w / W to x_(w+1): equal work whatever the mix of lengths, one launch, no queue.
+// A cut inside a row tile costs two partial results and their joining; a cut that comes within `snap` of a row tile's end is moved
+// there.  Stretches are at least 2 `snap` long, so short row tiles are never cut, and calls with little to do use fewer workgroups.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/seer_verify.h"
+#include "seer_device.h"
+
+namespace seer {
+
+constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves
+constexpr int kPromptThreads = 256;
+constexpr int kTileCost = 64;          // of a row tile beside its positions (queries, output), per head of the group
+constexpr int kMinStretch = 256;       // positions per head of the group
+
+// The pieces that end a stretch inside a row tile: the row tile, and in how many stretches it lies (0: none begins here and goes on).
+struct PromptCut {
+    int32_t b, kvh, tile, pieces;
+};
+
+struct PromptArgs {
+    uint16_t* out;
+    const uint16_t* q;
+    const unsigned char* k_pages;
+    const unsigned char* v_pages;
+    const int32_t* block_table;
+    const int32_t* ctx_len;
+    const int32_t* first;
+    int32_t* status;
+    PromptCut* cuts;       // [W]
+    float* part_ml;        // [2 W][kRowTile][2]: reference exponent (in units of log2 e), sum
+    float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
+    int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
+    int W;
+    int page_shift;        // -1: pages are no power of two
+    float scale_log2;
+    int64_t max_ctx;
+};
+
+// A request as the line counts it.
+struct PromptRequest {
+    int64_t past;          // positions before the new tokens
+    int n, tiles, first;   // new tokens, row tiles per KV head (0: nothing to do), first packed token
+    bool bad;              // a ctx_len that cannot be: rows of zeros
+};
+
+__device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int b, int64_t before, int& error) {
+    PromptRequest r{0, 0, 0, 0, false};
+    const int lo = a.first[b], hi = a.first[b + 1], ctx = a.ctx_len[b];
+    if (lo < 0 || hi < lo || hi > a.n_tokens || before + (hi - lo) > a.n_tokens) {      // (the sum keeps the whole line finite whatever the array holds)
+        error |= 4;
+        return r;
+    }
+    r.n = hi - lo, r.first = lo;
+    if (r.n == 0) return r;
+    r.bad = ctx < r.n || ctx > a.max_ctx;
+    if (r.bad) error |= 1;
+    r.past = r.bad ? 0 : ctx - r.n;
+    r.tiles = static_cast<int>((static_cast<int64_t>(r.n) * a.G + kRowTile - 1) / kRowTile);
+    return r;
+}
+// Cost of the first i row tiles of a KV head, and of row tile i.
+__device__ __forceinline__ int64_t tiles_before(const PromptArgs& a, int64_t past, int64_t i) {
+    return i * (a.G * (past + kTileCost)) + kRowTile / 2 * (i * (i + 1));
+}
+__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + kTileCost) + kRowTile * (i + 1); }
+
+struct PromptLds {
+    int64_t sums[2][kPromptThreads / kWave];
+    int64_t base[2];
+    int found[2];
+};
+
+// A row tile on the line: begins at `begin`, costs `cost`.
+struct PromptTile {
+    int b, kvh, i;
+    int64_t begin, cost;
+    PromptRequest r;
+};
+
+struct PromptPlan {
+    int64_t total, mine, mine_n;       // of the line; before this thread's requests: cost, new tokens
+    int64_t mine_cost;
+    int64_t snap;
+    int W;                             // stretches in use
+};
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+    return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32)))) << 32 |
+                                static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(x))));
+}
+
+// Sum of v over the threads before this one, and over all; two barriers.
+__device__ __forceinline__ int64_t prompt_before(int64_t v, int64_t* s, int64_t& total) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+    int64_t up = v;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+        const int64_t x = __shfl_up(up, o, kWave);
+        if (lane >= o) up += x;
+    }
+    if (lane == kWave - 1) s[wave] = up;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kPromptThreads / kWave; ++w) {
+        if (w < wave) before += s[w];
+        all += s[w];
+    }
+    total = uniform64(all);
+    return before + up - v;
+}
+
+// The line, by all threads of a workgroup: each looks at ceil(B / threads) requests behind one another.
+__device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs& a, PromptLds& s, int& error) {
+    PromptPlan p;
+    const int per = (a.B + kPromptThreads - 1) / kPromptThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
+    int64_t n = 0, all;
+    for (int b = b0; b < b1; ++b) {
+        const int lo = a.first[b], hi = a.first[b + 1];
+        if (lo >= 0 && hi >= lo && hi <= a.n_tokens) n += hi - lo;
+    }
+    p.mine_n = prompt_before(n, s.sums[0], all);
+    int64_t cost = 0, before = p.mine_n;
+    for (int b = b0; b < b1; ++b) {
+        const PromptRequest r = prompt_request(a, b, before, error);
+        before += r.n;
+        cost += a.Hkv * tiles_before(a, r.past, r.tiles);
+    }
+    p.mine = prompt_before(cost, s.sums[1], p.total);
+    p.mine_cost = cost;
+    const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
+    const int64_t most = (p.total + least - 1) / least;
+    p.W = static_cast<int>(most < a.W ? most : a.W);
+    p.snap = least / 2;
+    if (p.W > 0 && p.total / p.W / 16 > p.snap) p.snap = p.total / p.W / 16;
+    return p;
+}
+// Where stretch w begins on the line, before cuts are moved.
+__device__ __forceinline__ int64_t stretch_begin(const PromptPlan& p, int w) {
+    const int64_t each = p.total / p.W, rest = p.total - each * p.W;
+    return each * w + rest * w / p.W;
+}
+
+// Which row tiles hold x[0] and x[1] (a place at the line's end or behind it: the last row tile); all threads, ends behind a barrier.
+__device__ __forceinline__ void prompt_find(const PromptArgs& a, const PromptPlan& p, PromptLds& s, const int64_t (&at)[2], PromptTile (&t)[2]) {
+    const int per = (a.B + kPromptThreads - 1) / kPromptThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
+    __syncthreads();                                   // (the words of the search before have been read)
+    int ignored = 0;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int64_t x = at[e] < p.total ? at[e] : p.total - 1;
+        if (x < p.mine || x >= p.mine + p.mine_cost) continue;
+        int64_t begin = p.mine, before = p.mine_n;
+        for (int b = b0; b < b1; ++b) {
+            const PromptRequest r = prompt_request(a, b, before, ignored);
+            before += r.n;
+            const int64_t cost = a.Hkv * tiles_before(a, r.past, r.tiles);
+            if (x < begin + cost) {
+                s.found[e] = b, s.base[e] = begin;
+                break;
+            }
+            begin += cost;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const int64_t x = at[e] < p.total ? at[e] : p.total - 1;
+        PromptTile& o = t[e];
+        o.b = __builtin_amdgcn_readfirstlane(s.found[e]);
+        o.r = prompt_request(a, o.b, 0, ignored);      // (valid: the search passes over the others)
+        int64_t begin = uniform64(s.base[e]);
+        const int64_t head = tiles_before(a, o.r.past, o.r.tiles), d = x - begin;
+        o.kvh = static_cast<int>(d / head);
+        const int64_t inside = d - o.kvh * head;
+        // the largest i with tiles_before(i) <= inside
+        const double A = static_cast<double>(a.G * (o.r.past + kTileCost) + kRowTile / 2);
+        int64_t i = static_cast<int64_t>((sqrt(A * A + 2.0 * kRowTile * static_cast<double>(inside)) - A) / kRowTile);
+        i = i < 0 ? 0 : (i >= o.r.tiles ? o.r.tiles - 1 : i);
+        while (i > 0 && tiles_before(a, o.r.past, i) > inside) --i;
+        while (i + 1 < o.r.tiles && tiles_before(a, o.r.past, i + 1) <= inside) ++i;
+        o.i = static_cast<int>(i);
+        o.begin = begin + o.kvh * head + tiles_before(a, o.r.past, i);
+        o.cost = tile_cost(a, o.r.past, i);
+    }
+}
+// A cut at x inside row tile t, moved to the row tile's end if that is near.
+__device__ __forceinline__ int64_t moved_cut(const PromptPlan& p, const PromptTile& t, int64_t x) {
+    if (x >= t.begin + t.cost) return t.begin + t.cost;        // (the line's end)
+    if (x - t.begin <= p.snap) return t.begin;
+    if (t.begin + t.cost - x <= p.snap) return t.begin + t.cost;
+    return x;
+}
+// How many stretches the row tile lies in that begins in stretch w and is cut behind it.
+__device__ __forceinline__ int pieces_of(const PromptPlan& p, const PromptTile& t, int w) {
+    const int64_t last = t.begin + t.cost - p.snap;            // the first cut from here on is moved to the row tile's end
+    int e = w + 1;
+    const int64_t each = p.total / p.W > 0 ? p.total / p.W : 1;
+    const int64_t guess = last / (each + 1);
+    if (guess > e) e = static_cast<int>(guess < p.W ? guess : p.W);
+    while (e > w + 1 && stretch_begin(p, e - 1) >= last) --e;
+    while (e < p.W && stretch_begin(p, e) < last) ++e;
+    return e - w;
+}
+
+}  // namespace seer

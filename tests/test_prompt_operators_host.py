@@ -116,3 +116,76 @@ def test_append_argument_errors_before_any_launch(lib):
     assert run(ap(kv_shared_latent=1)) == b.SEER_EINVAL and run(ap(kv_shared_latent=1), null=("v",)) == b.SEER_EINVAL
     assert run(ap(n_tokens=0)) == b.SEER_OK
     assert run(ap(Dqk=8, Dv=8, Hq=1, Hkv=1, rotary_dim=0, q_stride=8, k_stride=8, v_stride=8, q_out_stride=8, n_tokens=0)) == b.SEER_OK
+
+
+def pp(**kw):
+    from paper_2511_14617_amd.binding import SeerAttnParams
+    base = dict(B=4, T=0, Hq=8, Hkv=2, Dqk=128, Dv=128, page_size=16, num_pages=100, max_pages_per_seq=32, max_splits=-7, kv_shared_latent=0, flags=-1, scale=0.088)
+    base.update(kw)
+    return SeerAttnParams(**base)
+
+
+def test_prompt_attention_workspace(lib):
+    from paper_2511_14617_amd import binding as b
+    size = b.seer_prompt_attention_workspace
+    assert 0 < size(pp(), 1) <= size(pp(), 100000) <= size(pp(max_pages_per_seq=8192), 100000) < 1 << 28
+    for Dqk, Dv in ((64, 64), (192, 128), (256, 256)):
+        assert size(pp(Dqk=Dqk, Dv=Dv), 1000) > 0
+    for bad in (pp(B=0), pp(B=-1), pp(Hq=0), pp(Hkv=3), pp(Dqk=96), pp(Dv=64), pp(page_size=0), pp(num_pages=0), pp(max_pages_per_seq=0), pp(scale=0.0), pp(scale=float("nan"))):
+        assert size(bad, 10) == 0
+    assert size(pp(), 0) == 0 and size(pp(), -1) == 0 and lib.seer_prompt_attention_workspace(None, 5) == 0
+
+
+def test_prompt_attention_argument_errors_before_any_launch(lib):
+    from paper_2511_14617_amd import binding as b
+
+    def run(p, n=50, null=(), off=None, ws=0x10000, ws_bytes=1 << 40):
+        names = ["out", "q", "kp", "vp", "table", "ctx", "first"]
+        args = [None if k in null else FAKE * (i + 1) + (off[1] if off and off[0] == k else 0) for i, k in enumerate(names)]
+        return lib.seer_prompt_attention(*args, None if p is None else ctypes.byref(p), n, off[1] if off and off[0] == "status" else None, ws, ws_bytes, None)
+
+    assert run(None) == b.SEER_EINVAL and run(pp(), n=-1) == b.SEER_EINVAL
+    for bad in (dict(B=-1), dict(Hq=0), dict(Hkv=0), dict(page_size=0), dict(num_pages=0), dict(max_pages_per_seq=0), dict(scale=0.0), dict(scale=-1.0),
+                dict(scale=float("inf")), dict(scale=float("nan"))):
+        assert run(pp(**bad)) == b.SEER_EINVAL, bad
+    for bad in (dict(Hkv=3), dict(max_pages_per_seq=1 << 27), dict(num_pages=1 << 30, page_size=16)):
+        assert run(pp(**bad)) == b.SEER_ESHAPE, bad
+    assert run(pp(max_pages_per_seq=1 << 26, Hq=1 << 14, Hkv=1), n=1 << 30) == b.SEER_ESHAPE
+    for bad in (dict(Dqk=96, Dv=96), dict(Dqk=128, Dv=64), dict(Dqk=576, Dv=512), dict(Dqk=128, kv_shared_latent=1)):
+        assert run(pp(**bad)) == b.SEER_EUNSUPPORTED, bad
+    for name in ("out", "q", "kp", "vp", "table", "ctx", "first"):
+        assert run(pp(), null=(name,)) == b.SEER_EINVAL, name
+        assert run(pp(), off=(name, 2)) == b.SEER_EALIGN, name
+    for name in ("out", "q", "kp", "vp"):
+        assert run(pp(), off=(name, 8)) == b.SEER_EALIGN, name
+    assert run(pp(), off=("status", 2)) == b.SEER_EALIGN
+    assert run(pp(), ws=None) == b.SEER_EWORKSPACE
+    assert run(pp(), ws_bytes=b.seer_prompt_attention_workspace(pp(), 50) - 1) == b.SEER_EWORKSPACE
+    assert run(pp(), ws=0x10010) == b.SEER_EALIGN
+    assert run(pp(B=0)) == b.SEER_OK and run(pp(), n=0) == b.SEER_OK
+
+
+def test_the_binding_refuses_other_tensors():
+    """On the CPU: nothing here is on a device, which is the last thing that the checks look at."""
+    import torch
+    from paper_2511_14617_amd import binding as b
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="n_tokens"):
+        b.seer_kv_reserve(i32(2, 3), i32(2), i32(9), i32(2), i32(2), -1, 16)
+    with pytest.raises(ValueError, match="page_size"):
+        b.seer_kv_reserve(i32(2, 3), i32(2), i32(9), i32(2), i32(2), 5, 2 ** 32 + 16)
+    with pytest.raises(ValueError, match="block_table"):
+        b.seer_kv_reserve(i32(2), i32(2), i32(9), i32(2), i32(2), 5, 16)
+    with pytest.raises(ValueError, match="device"):
+        b.seer_kv_reserve(i32(2, 3), i32(2), i32(9), i32(2), i32(2), 5, 16)
+    with pytest.raises(ValueError, match="want k "):
+        b.seer_kv_append(None, bf(4, 2), None, i32(4), None, bf(3, 2, 16, 8), None)
+    with pytest.raises(ValueError, match="k: want device"):
+        b.seer_kv_append(None, bf(4, 2, 8), None, i32(4), None, bf(3, 2, 16, 8), None)
+    with pytest.raises(ValueError, match="want q "):
+        b.seer_prompt_attention(bf(4, 2), bf(3, 2, 16, 64), None, i32(2, 3), i32(2), i32(3), 1.0)
+    with pytest.raises(ValueError, match="Dv"):
+        b.seer_prompt_attention(bf(4, 2, 576), bf(3, 1, 16, 576), None, i32(2, 3), i32(2), i32(3), 1.0)
+    with pytest.raises(ValueError, match="q: want"):
+        b.seer_prompt_attention(bf(4, 2, 64), bf(3, 1, 16, 64), bf(3, 1, 16, 64), i32(2, 3), i32(2), i32(3), 1.0)
