@@ -680,8 +680,8 @@ SEER_API size_t seer_prompt_attention_workspace(const seer_attn_params* p, int32
  *  k_pages, v_pages, block_table  as for seer_verify_attention
  *  ctx_len       device [B] int32, INCLUDING the new tokens (seer_kv_reserve's step_len)
  *  first_token   device [B+1] int32, ascending from 0 or more to at most n_tokens
- *  p             host; T, max_splits and flags are not looked at.  (Dqk, Dv) in {(64,64), (128,128), (192,128), (256,256)}, any
- *                page_size
+ *  p             host; T, max_splits and flags are not looked at.  (Dqk, Dv) in {(64,64), (128,128), (192,128), (256,256)}, and
+ *                (576,512) with the shared latent; any page_size
  *  status        device [1] int32 or NULL; bits are OR-ed in: 1 = a ctx_len below n_b or beyond the block table (the request's rows
  *                are zeros), 2 = a page id outside the pool (it is clamped into the pool), 4 = first_token not ascending or
  *                beyond n_tokens (the request's rows are left as they are).  The caller clears it.

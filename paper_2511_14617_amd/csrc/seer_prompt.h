@@ -54,10 +54,16 @@ struct PromptRequest {
     bool bad;              // a ctx_len that cannot be: rows of zeros
 };
 
+// Tokens of request b; 0 where first_token cannot be.
+__device__ __forceinline__ int prompt_tokens(const PromptArgs& a, int b) {
+    const int lo = a.first[b], hi = a.first[b + 1];
+    return lo >= 0 && hi >= lo && hi <= a.n_tokens ? hi - lo : 0;
+}
+// before: the sum of prompt_tokens over the requests before b (with a limit to it the line is finite whatever the array holds).
 __device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int b, int64_t before, int& error) {
     PromptRequest r{0, 0, 0, 0, false};
     const int lo = a.first[b], hi = a.first[b + 1], ctx = a.ctx_len[b];
-    if (lo < 0 || hi < lo || hi > a.n_tokens || before + (hi - lo) > a.n_tokens) {      // (the sum keeps the whole line finite whatever the array holds)
+    if (lo < 0 || hi < lo || hi > a.n_tokens || before + (hi - lo) > a.n_tokens) {
         error |= 4;
         return r;
     }
@@ -77,7 +83,7 @@ __device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, 
 
 struct PromptLds {
     int64_t sums[2][kPromptThreads / kWave];
-    int64_t base[2];
+    int64_t base[2], before[2];
     int found[2];
 };
 
@@ -85,12 +91,12 @@ struct PromptLds {
 struct PromptTile {
     int b, kvh, i;
     int64_t begin, cost;
+    int64_t before;        // tokens of the requests before
     PromptRequest r;
 };
 
 struct PromptPlan {
-    int64_t total, mine, mine_n;       // of the line; before this thread's requests: cost, new tokens
-    int64_t mine_cost;
+    int64_t total;                     // of the line
     int64_t snap;
     int W;                             // stretches in use
 };
@@ -121,67 +127,60 @@ __device__ __forceinline__ int64_t prompt_before(int64_t v, int64_t* s, int64_t&
     return before + up - v;
 }
 
-// The line, by all threads of a workgroup: each looks at ceil(B / threads) requests behind one another.
-__device__ __forceinline__ PromptPlan prompt_plan(const PromptArgs& a, PromptLds& s, int& error) {
-    PromptPlan p;
-    const int per = (a.B + kPromptThreads - 1) / kPromptThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
-    int64_t n = 0, all;
-    for (int b = b0; b < b1; ++b) {
-        const int lo = a.first[b], hi = a.first[b + 1];
-        if (lo >= 0 && hi >= lo && hi <= a.n_tokens) n += hi - lo;
-    }
-    p.mine_n = prompt_before(n, s.sums[0], all);
-    int64_t cost = 0, before = p.mine_n;
-    for (int b = b0; b < b1; ++b) {
-        const PromptRequest r = prompt_request(a, b, before, error);
-        before += r.n;
-        cost += a.Hkv * tiles_before(a, r.past, r.tiles);
-    }
-    p.mine = prompt_before(cost, s.sums[1], p.total);
-    p.mine_cost = cost;
-    const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
-    const int64_t most = (p.total + least - 1) / least;
-    p.W = static_cast<int>(most < a.W ? most : a.W);
-    p.snap = least / 2;
-    if (p.W > 0 && p.total / p.W / 16 > p.snap) p.snap = p.total / p.W / 16;
-    return p;
-}
 // Where stretch w begins on the line, before cuts are moved.
 __device__ __forceinline__ int64_t stretch_begin(const PromptPlan& p, int w) {
     const int64_t each = p.total / p.W, rest = p.total - each * p.W;
     return each * w + rest * w / p.W;
 }
 
-// Which row tiles hold x[0] and x[1] (a place at the line's end or behind it: the last row tile); all threads, ends behind a barrier.
-__device__ __forceinline__ void prompt_find(const PromptArgs& a, const PromptPlan& p, PromptLds& s, const int64_t (&at)[2], PromptTile (&t)[2]) {
+// The line, by all threads of a workgroup (each looks at ceil(B / threads) requests behind one another), and where on it stretch w
+// begins and ends: the row tiles there.  False: there is no stretch w.  No barrier behind it.
+__device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, int w, PromptPlan& p, int64_t (&x)[2], PromptTile (&t)[2], int& error) {
     const int per = (a.B + kPromptThreads - 1) / kPromptThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
-    __syncthreads();                                   // (the words of the search before have been read)
+    int64_t n = 0, all;
+    for (int b = b0; b < b1; ++b) n += prompt_tokens(a, b);
+    const int64_t mine_n = prompt_before(n, s.sums[0], all);
+    int64_t mine_cost = 0, before = mine_n;
+    for (int b = b0; b < b1; ++b) {
+        const PromptRequest r = prompt_request(a, b, before, error);
+        before += prompt_tokens(a, b);
+        mine_cost += a.Hkv * tiles_before(a, r.past, r.tiles);
+    }
+    const int64_t mine = prompt_before(mine_cost, s.sums[1], p.total);
+    const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
+    const int64_t most = (p.total + least - 1) / least;
+    p.W = static_cast<int>(most < a.W ? most : a.W);
+    p.snap = least / 2;
+    if (w >= p.W) return false;
+    if (p.total / p.W / 16 > p.snap) p.snap = p.total / p.W / 16;
     int ignored = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int64_t x = at[e] < p.total ? at[e] : p.total - 1;
-        if (x < p.mine || x >= p.mine + p.mine_cost) continue;
-        int64_t begin = p.mine, before = p.mine_n;
+        x[e] = stretch_begin(p, w + e);
+        const int64_t at = x[e] < p.total ? x[e] : p.total - 1;        // (the line's end: its last row tile)
+        if (at < mine || at >= mine + mine_cost) continue;
+        int64_t begin = mine;
+        before = mine_n;
         for (int b = b0; b < b1; ++b) {
             const PromptRequest r = prompt_request(a, b, before, ignored);
-            before += r.n;
             const int64_t cost = a.Hkv * tiles_before(a, r.past, r.tiles);
-            if (x < begin + cost) {
-                s.found[e] = b, s.base[e] = begin;
+            if (at < begin + cost) {
+                s.found[e] = b, s.base[e] = begin, s.before[e] = before;
                 break;
             }
             begin += cost;
+            before += prompt_tokens(a, b);
         }
     }
     __syncthreads();
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-        const int64_t x = at[e] < p.total ? at[e] : p.total - 1;
+        const int64_t at = x[e] < p.total ? x[e] : p.total - 1;
         PromptTile& o = t[e];
         o.b = __builtin_amdgcn_readfirstlane(s.found[e]);
-        o.r = prompt_request(a, o.b, 0, ignored);      // (valid: the search passes over the others)
-        int64_t begin = uniform64(s.base[e]);
-        const int64_t head = tiles_before(a, o.r.past, o.r.tiles), d = x - begin;
+        o.before = uniform64(s.before[e]);
+        o.r = prompt_request(a, o.b, o.before, ignored);
+        const int64_t begin = uniform64(s.base[e]), head = tiles_before(a, o.r.past, o.r.tiles), d = at - begin;
         o.kvh = static_cast<int>(d / head);
         const int64_t inside = d - o.kvh * head;
         // the largest i with tiles_before(i) <= inside
@@ -194,6 +193,39 @@ __device__ __forceinline__ void prompt_find(const PromptArgs& a, const PromptPla
         o.begin = begin + o.kvh * head + tiles_before(a, o.r.past, i);
         o.cost = tile_cost(a, o.r.past, i);
     }
+    return true;
+}
+
+// The row tile behind t on the line, which must not end there; by each wave for itself.  Of the KV head, of the next one, of the next request with
+// tokens: 64 requests are looked at together.
+__device__ __forceinline__ void next_tile(const PromptArgs& a, PromptTile& t) {
+    t.begin += t.cost;
+    if (t.i + 1 < t.r.tiles) {
+        ++t.i;
+    } else if (t.kvh + 1 < a.Hkv) {
+        ++t.kvh, t.i = 0;
+    } else {
+        int ignored = 0;
+        const int lane = threadIdx.x & (kWave - 1);
+        t.before += prompt_tokens(a, t.b);
+        t.kvh = 0, t.i = 0, t.r.tiles = 0;
+        for (int b0 = t.b + 1; b0 < a.B && t.r.tiles == 0; ) {
+            const int n = b0 + lane < a.B ? prompt_tokens(a, b0 + lane) : 0;
+            const uint64_t some = __ballot(n > 0);
+            if (some == 0) {
+                b0 += kWave;
+                continue;
+            }
+            t.b = b0 + __builtin_ctzll(some);
+            t.r = prompt_request(a, t.b, t.before, ignored);       // (nothing, if the tokens before it fill the array)
+            if (t.r.tiles == 0) t.before += prompt_tokens(a, t.b), b0 = t.b + 1;
+        }
+        t.before = uniform64(t.before);
+        t.b = __builtin_amdgcn_readfirstlane(t.b);
+        t.r.past = uniform64(t.r.past), t.r.n = __builtin_amdgcn_readfirstlane(t.r.n), t.r.tiles = __builtin_amdgcn_readfirstlane(t.r.tiles);
+        t.r.first = __builtin_amdgcn_readfirstlane(t.r.first), t.r.bad = __builtin_amdgcn_readfirstlane(t.r.bad);
+    }
+    t.cost = tile_cost(a, t.r.past, t.i);
 }
 // A cut at x inside row tile t, moved to the row tile's end if that is near.
 __device__ __forceinline__ int64_t moved_cut(const PromptPlan& p, const PromptTile& t, int64_t x) {
@@ -213,5 +245,8 @@ __device__ __forceinline__ int pieces_of(const PromptPlan& p, const PromptTile& 
     while (e < p.W && stretch_begin(p, e) < last) ++e;
     return e - w;
 }
+
+// The partition kernel for the shared latent 576/512.
+hipError_t launch_prompt_latent(const PromptArgs& a, hipStream_t stream);
 
 }  // namespace seer

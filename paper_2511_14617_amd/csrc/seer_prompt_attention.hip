@@ -35,18 +35,18 @@ void prompt_tile_kernel(PromptArgs a) {
     const int w = (blockIdx.x & 7) * (a.W >> 3) + (blockIdx.x >> 3);
 
     int error = 0;
-    const PromptPlan plan = prompt_plan(a, s_plan, error);
-    if (w == 0 && error && a.status) atomicOr(a.status, error);
-    if (w >= plan.W) {
-        if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
-        return;
-    }
+    PromptPlan plan;
     int64_t x, x_end;
     PromptTile t;
     {
-        const int64_t at[2] = {stretch_begin(plan, w), stretch_begin(plan, w + 1)};
+        int64_t at[2];
         PromptTile ends[2];
-        prompt_find(a, plan, s_plan, at, ends);
+        const bool on = prompt_plan(a, s_plan, w, plan, at, ends, error);
+        if (w == 0 && error && a.status) atomicOr(a.status, error);
+        if (!on) {
+            if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
+            return;
+        }
         x = moved_cut(plan, ends[0], at[0]);
         x_end = moved_cut(plan, ends[1], at[1]);
         t = ends[0];
@@ -58,20 +58,7 @@ void prompt_tile_kernel(PromptArgs a) {
     const Operands<DQK, DV> operands;
 
     while (x < x_end) {
-        if (x >= t.begin + t.cost) {                // the next row tile: of this KV head, of the next one, of the next request
-            t.begin += t.cost;
-            if (t.i + 1 < t.r.tiles) {
-                ++t.i;
-            } else if (t.kvh + 1 < a.Hkv) {
-                ++t.kvh, t.i = 0;
-            } else {
-                const int64_t at[2] = {x, x};
-                PromptTile next[2];
-                prompt_find(a, plan, s_plan, at, next);
-                t = next[0];
-            }
-            t.cost = tile_cost(a, t.r.past, t.i);
-        }
+        if (x >= t.begin + t.cost) next_tile(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
         const int rows = min(kRowTile, static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile))));
@@ -269,12 +256,18 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs 
     for (int i = 0; i < kEach; ++i) out[i] = f32_to_bf16(o[i] * inv);
 }
 
+static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
+    const dim3 grid(a.W * (kRowTile / kJoinRows));
+    if (a.Dv == 64) hipLaunchKernelGGL((prompt_join_kernel<64>), grid, dim3(kPromptThreads), 0, stream, a);
+    else if (a.Dv == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), grid, dim3(kPromptThreads), 0, stream, a);
+    else if (a.Dv == 256) hipLaunchKernelGGL((prompt_join_kernel<256>), grid, dim3(kPromptThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prompt_join_kernel<512>), grid, dim3(kPromptThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
 template <int DQK, int DV>
 static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
-    hipLaunchKernelGGL((prompt_join_kernel<DV>), dim3(a.W * (kRowTile / kJoinRows)), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -290,7 +283,6 @@ static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     const bool known = shared ? p->Dqk == 576 && p->Dv == 512
                               : (p->Dqk == 64 && p->Dv == 64) || (p->Dqk == 128 && p->Dv == 128) || (p->Dqk == 256 && p->Dv == 256) || (p->Dqk == 192 && p->Dv == 128);
     if (!known) return SEER_EUNSUPPORTED;
-    if (shared) return SEER_EUNSUPPORTED;
     const int64_t ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size, G = p->Hq / p->Hkv;
     // positions are counted in 32 bits, the line of row tiles in 64, rows of the pool in 32
     if (ctx > 0x7fffffffLL - 65536 || static_cast<int64_t>(p->num_pages) * p->page_size * p->Hkv > 0xffffffffLL) return SEER_ESHAPE;
@@ -359,5 +351,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     else if (p->Dqk == 128) err = seer::launch_prompt<128, 128>(a, stream);
     else if (p->Dqk == 192) err = seer::launch_prompt<192, 128>(a, stream);
     else if (p->Dqk == 256) err = seer::launch_prompt<256, 256>(a, stream);
+    else err = seer::launch_prompt_latent(a, stream);
+    if (err == hipSuccess) err = seer::launch_join(a, stream);
     return err == hipSuccess ? SEER_OK : static_cast<int>(err);
 }

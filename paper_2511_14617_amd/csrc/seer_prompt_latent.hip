@@ -1,0 +1,402 @@
+// Causal attention of packed tokens over a cache of shared latents (576 components a position, its first 512 the value): the prompt form of
+// the verify kernel for that shape, with that kernel's arithmetic (seer_mla.h) on the row tiles of seer_prompt.h.
+//
+// What bounds it: the matrix cores, and what one wave per SIMD issues between their instructions (about 1200 flop per byte of a
+// tile).  A workgroup of four waves takes 128 query rows; a tile of 32 positions (36 KB) goes HBM/L2 -> LDS directly, three stages; the
+// scores of tile u run beside the softmax of tile u - 1, then its product with V beside the reference of tile u.  With 128 heads a row tile
+// is one token, and neighbouring row tiles read the same latents: the stretches of one XCD are neighbours on the line.
+//
+// Infinities and NaN in positions that some row of the tile does not see: scores by selection; the value rows are taken out of LDS once
+// all waves have the tile's scores.  A row that sees such a latent has it in its score as well, which is then NaN or +inf and makes the whole row NaN, or -inf
+// and gives the position no weight.
+#include "seer_device.h"
+#include "seer_mla.h"
+#include "seer_prompt.h"
+#include "seer_tile.h"
+
+namespace seer {
+
+// ANY_PAGE: pages of any size; a lane finds the row of its LDS slot through the block table instead of a descriptor of the tile.
+template <bool ANY_PAGE>
+__global__ __launch_bounds__(kPromptThreads) __attribute__((amdgpu_waves_per_eu(1, 1)))
+void prompt_latent_kernel(PromptArgs a) {
+    using namespace mla;
+    static_assert(kRowsPerWg == kRowTile && kWaves * kWave == kPromptThreads, "");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kStages * kStageBytes];
+    __shared__ __attribute__((aligned(16))) u32x4 q_tail[kWaves][kQLdsSteps][kWave];      // (see the verify kernel)
+    __shared__ PromptLds s_plan;
+    __shared__ uint32_t s_found;                    // positions with infinities or NaN in the scanned tile's values
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5, l16 = lane >> 4, p16 = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int w = (blockIdx.x & 7) * (a.W >> 3) + (blockIdx.x >> 3);          // (see the kernel for separate pools)
+    int error = 0;
+    PromptPlan plan;
+    int64_t x, x_end;
+    PromptTile t;
+    {
+        int64_t at[2];
+        PromptTile ends[2];
+        const bool on = prompt_plan(a, s_plan, w, plan, at, ends, error);
+        if (w == 0 && error && a.status) atomicOr(a.status, error);
+        if (!on) {
+            if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
+            return;
+        }
+        x = moved_cut(plan, ends[0], at[0]);
+        x_end = moved_cut(plan, ends[1], at[1]);
+        t = ends[0];
+    }
+    PromptCut cut{0, 0, 0, 0};
+    bool bad_page = false;
+
+    // operand addresses (see the verify kernel)
+    int k_rd[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) k_rd[j] = ln * kRowBytes + (((2 * j + lg) ^ swz(ln)) << 4);
+    const int v_k = p16 >> 2, v_c4 = p16 & 3, v_dhalf = l16 & 1;
+    const int v_swz = swz(lg * 4 + v_k), v_row0 = (lg * 4 + v_k) * kRowBytes;
+    const int v_even = v_row0 + (((v_dhalf * 2 + (v_c4 >> 1)) ^ v_swz) << 4) + (v_c4 & 1) * 8;
+    const int v_odd = v_row0 + (((4 + v_dhalf * 2 + (v_c4 >> 1)) ^ v_swz) << 4) + (v_c4 & 1) * 8;
+    const int v_even8 = v_row0 + (((v_dhalf * 2 + (v_c4 >> 1)) ^ v_swz ^ 1) << 4) + (v_c4 & 1) * 8;
+    const int v_odd8 = v_row0 + (((4 + v_dhalf * 2 + (v_c4 >> 1)) ^ v_swz ^ 1) << 4) + (v_c4 & 1) * 8;
+    int pat[5];
+#pragma unroll
+    for (int j = 0; j < 5; ++j) {
+        const unsigned c = static_cast<unsigned>((j < 4 ? wave + 4 * j : 16 + (wave & 1)) * 64 + lane);
+        const unsigned row = c / kChunksPerRow, pos = c - row * kChunksPerRow;
+        pat[j] = static_cast<int>(row * kRowBytes + ((pos ^ static_cast<unsigned>(swz(static_cast<int>(row)))) << 4));
+    }
+    auto page_of = [&](int64_t tok) __attribute__((always_inline)) -> int {
+        return static_cast<int>(!ANY_PAGE || a.page_shift >= 0 ? tok >> a.page_shift : tok / a.P);
+    };
+
+    while (x < x_end) {
+        if (x >= t.begin + t.cost) next_tile(a, t);
+        const int64_t end = min(x_end, t.begin + t.cost);
+        const bool begins = x == t.begin, ends = end == t.begin + t.cost;
+        const int rows = static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile)));
+        const int token_first = static_cast<int>(static_cast<int64_t>(t.i) * kRowTile / a.G);
+        const int token_last = static_cast<int>((static_cast<int64_t>(t.i) * kRowTile + rows - 1) / a.G);
+        const int seen = static_cast<int>(t.r.past) + token_last + 1;
+        const int tiles = t.r.bad ? 0 : (seen + kTile - 1) / kTile;
+        const int u0 = begins ? 0 : static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
+        const int u1 = ends ? tiles : static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
+        x = end;
+        if (t.r.bad && !begins) continue;
+        const int n_tiles = u1 - u0, tok_begin = u0 * kTile;
+
+        // ---- this lane's query row -------------------------------------------------------------------------
+        const int64_t row = static_cast<int64_t>(t.i) * kRowTile + wave * 32 + ln;
+        const bool row_ok = wave * 32 + ln < rows;
+        const int token = row_ok ? static_cast<int>(row / a.G) : 0;
+        const size_t q_row = (static_cast<size_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0);
+        const int sees = row_ok ? static_cast<int>(t.r.past) + token : -1;
+        const int sees_lo = __builtin_amdgcn_readfirstlane(sees), all_see = static_cast<int>(t.r.past) + token_first;
+        f32x16 acc[kDTiles];
+#pragma unroll
+        for (int dt = 0; dt < kDTiles; ++dt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
+        float m_run = kNegInf, l_run = 0.f, alpha = 1.f;
+        bare_barrier();                             // every wave is done with the stages of the piece before
+        if (n_tiles > 0) {
+            u32x4 qreg[kQRegSteps];
+            {
+                const u32x4* qp = reinterpret_cast<const u32x4*>(a.q + q_row * kDqk + lg * 8);
+#pragma unroll
+                for (int kk = 0; kk < kQLdsSteps; ++kk) {
+                    u32x4 v = u32x4{0u, 0u, 0u, 0u};
+                    if (row_ok) v = qp[(kQRegSteps + kk) * 2];
+                    q_tail[wave][kk][lane] = v;
+                }
+                u32x4 qv[kQRegSteps];
+#pragma unroll
+                for (int kk = 0; kk < kQRegSteps; ++kk) {
+                    qv[kk] = u32x4{0u, 0u, 0u, 0u};
+                    if (row_ok) qv[kk] = qp[kk * 2];
+                }
+#pragma unroll
+                for (int kk = 0; kk < kQRegSteps; ++kk) {   // pin the arrival of these loads before the tile loop
+                    asm volatile("" : "+v"(qv[kk]));
+                    qreg[kk] = qv[kk];
+                }
+            }
+
+            // ---- page ids, 64 at a time -------------------------------------------------------------------
+            const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
+            const int last_page = page_of(t.r.past + t.r.n - 1);
+            int win = -0x40000000, pg_win = 0;
+            auto set_window = [&](int first) __attribute__((always_inline)) {
+                win = first;
+                int pg = table[min(first + lane, a.max_pages - 1)];
+                if (pg < 0 || pg >= a.num_pages) {
+                    if (first + lane <= last_page) bad_page = true;
+                    pg = min(max(pg, 0), a.num_pages - 1);
+                }
+                pg_win = pg;
+            };
+            // loads through a descriptor of the tile, which lies in one page (see the verify kernel)
+            auto tile_rsrc = [&](int tile) __attribute__((always_inline)) {
+                const int tb = tok_begin + tile * kTile, lp = tb >> a.page_shift;
+                if (lp < win || lp >= win + kWave) set_window(lp);
+                const int pg = __builtin_amdgcn_readlane(pg_win, __builtin_amdgcn_readfirstlane(lp - win));
+                const unsigned char* src = a.k_pages + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (tb & (a.P - 1))) * kRowBytes;
+                return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(src), 0, kStageBytes, 0x00020000);
+            };
+            auto issue_load = [&](auto ic, __amdgpu_buffer_rsrc_t rsrc, int stage_off) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                const int half = i < 8 ? (i & 1) : (wave >> 1);
+                const int block = (i < 8 ? wave + 4 * (i >> 1) : 16 + (wave & 1)) + 18 * half;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (SEER_AS3 void*)(lds + stage_off + block * 1024), 16, pat[i < 8 ? (i >> 1) : 4],
+                                                         half * (16 * kRowBytes), 0, 0);
+            };
+            // ... and through the row of every position
+            auto issue_rows = [&](int tile, int stage_off) __attribute__((always_inline)) {
+                const int64_t tb = tok_begin + static_cast<int64_t>(tile) * kTile;
+                if (page_of(tb) < win || page_of(tb + kTile - 1) >= win + kWave) set_window(page_of(tb));
+                const int64_t tok = tb + ln;
+                const int lp = page_of(tok);
+                const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
+                const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - static_cast<int64_t>(lp) * a.P);
+                for (int j = 0; j < kLoadsPerWave; ++j) {
+                    const int block = j * kWaves + wave, c = block * kWave + lane, r = c / kChunksPerRow, pos = c - r * kChunksPerRow;
+                    const uint32_t from = __builtin_amdgcn_ds_bpermute(r << 2, row_idx);
+                    const unsigned char* src = a.k_pages + static_cast<size_t>(from) * kRowBytes + ((pos ^ swz(r)) << 4);
+                    __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage_off + block * 1024), 16, 0, 0);
+                }
+            };
+            auto issue_tile = [&](int tile, int stage_off) __attribute__((always_inline)) {
+                if constexpr (ANY_PAGE) {
+                    issue_rows(tile, stage_off);
+                } else {
+                    const __amdgpu_buffer_rsrc_t rsrc = tile_rsrc(tile);
+                    for_each_index([&](auto ic) __attribute__((always_inline)) { issue_load(ic, rsrc, stage_off); }, std::make_integer_sequence<int, kLoadsPerWave>{});
+                }
+            };
+
+            // ---- the pipeline (see the verify kernel): step u = scores of tile u | softmax of tile u - 1, then P.V of tile u - 1 -------
+            static_assert(kStages == 3, "the three stage offsets below rotate");
+            int st_prev = 2 * kStageBytes, st_cur = 0, st_next = kStageBytes;
+            const int lds_base = lds_addr(lds);
+            const int qt = lds_addr(&q_tail[wave][0][lane]);
+            f32x16 s_a, s_b;
+            uint32_t pk[8];
+            // positions of the tile before, and of this one, whose values are kept out of the product (uniform)
+            uint32_t left_prev = 0, left_cur = 0;
+            auto step_top = [&](int u) __attribute__((always_inline)) {
+                wait_vmcnt<0>();
+                bare_barrier();                     // tile u has landed for every wave, every wave has the scores of tile u - 1
+                if constexpr (ANY_PAGE) {
+                    if (u + 1 < n_tiles) issue_rows(u + 1, st_next);
+                }
+                left_prev = left_cur, left_cur = 0;
+                if (u < n_tiles && tok_begin + u * kTile + kTile - 1 > all_see) {
+                    if (tid == 0) s_found = 0;
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    bare_barrier();
+                    uint32_t found = 0;
+                    for (int c = tid; c < kTile * (kDv / 8); c += kPromptThreads) {
+                        const int r = c / (kDv / 8), pos = c - r * (kDv / 8);
+                        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + st_cur + r * kRowBytes + ((pos ^ swz(r)) << 4));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if ((v[i] & 0x7f80u) == 0x7f80u || (v[i] & 0x7f800000u) == 0x7f800000u) found |= 1u << r;
+                    }
+                    if (found) atomicOr(&s_found, found);
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                    bare_barrier();
+                    left_cur = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
+                }
+                if (left_prev) {
+                    for (int c = tid; c < kTile * (kDv / 8); c += kPromptThreads) {
+                        const int r = c / (kDv / 8), pos = c - r * (kDv / 8);
+                        if ((left_prev >> r) & 1u) *reinterpret_cast<u32x4*>(lds + st_prev + r * kRowBytes + ((pos ^ swz(r)) << 4)) = u32x4{0u, 0u, 0u, 0u};
+                    }
+                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                }
+                if (left_prev || (u < n_tiles && tok_begin + u * kTile + kTile - 1 > all_see)) bare_barrier();      // (also: s_found has been read)
+            };
+            auto apply_mask = [&](int j, f32x16& sc) __attribute__((always_inline)) {
+                const int tb = tok_begin + j * kTile;
+                if (tb + kTile - 1 <= sees_lo) return;
+                const int lim = sees - tb;
+                uint32_t vis = lim < 0 ? 0u : (lim >= 31 ? 0xffffffffu : (2u << lim) - 1u);
+                vis >>= lg * 4;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!((vis >> ((i >> 2) * 8 + (i & 3))) & 1u)) sc[i] = kNegInf;
+            };
+            auto k_addrs = [&](int stage_off, int (&ka)[4]) __attribute__((always_inline)) {
+                const int st = lds_base + stage_off;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ka[j] = st + k_rd[j];
+            };
+            auto v_addrs = [&](int stage_off, int (&va)[4]) __attribute__((always_inline)) {
+                const int st = lds_base + stage_off;
+                va[0] = st + v_even, va[1] = st + v_even8, va[2] = st + v_odd, va[3] = st + v_odd8;
+            };
+            float m_use = 0.f, mx_part = 0.f;
+            auto reference = [&](auto ic, const f32x16& sc) __attribute__((always_inline)) {
+                constexpr int part = decltype(ic)::value;
+                if constexpr (part == 0) {
+                    mx_part = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
+#pragma unroll
+                    for (int i = 3; i < 9; i += 2) mx_part = fmaxf(fmaxf(mx_part, sc[i]), sc[i + 1]);
+                    SEER_MLA_PIN(mx_part);
+                } else if constexpr (part == 1) {
+#pragma unroll
+                    for (int i = 9; i < 15; i += 2) mx_part = fmaxf(fmaxf(mx_part, sc[i]), sc[i + 1]);
+                    mx_part = fmaxf(mx_part, sc[15]);
+                    SEER_MLA_PIN(mx_part);
+                } else if constexpr (part == 2) {
+                    mx_part = max_across_halves(mx_part) * a.scale_log2;
+                    SEER_MLA_PIN(mx_part);
+                } else {
+                    const float m_new = (mx_part > m_run + 8.f) ? mx_part : m_run;
+                    m_use = (m_new == kNegInf) ? 0.f : m_new;
+                    alpha = fast_exp2(m_run - m_use);
+                    m_run = m_new;
+                    SEER_MLA_PIN(m_use);
+                    SEER_MLA_PIN(alpha);
+                    SEER_MLA_PIN(m_run);
+                }
+            };
+            u32x2 vr[kVAhead][2];
+            int va[4];
+            auto pv = [&](int j, auto next, f32x16& sc_next, auto&& prepare) __attribute__((always_inline)) {
+                constexpr bool NEXT = decltype(next)::value;
+                if constexpr (NEXT) {
+                    if (tok_begin + (j + 1) * kTile + kTile - 1 > sees_lo) {
+                        mfma_drain();
+                        apply_mask(j + 1, sc_next);
+                    }
+                }
+                if (__any(alpha != 1.f)) {
+                    mfma_drain();
+#pragma unroll
+                    for (int dt = 0; dt < kDTiles; ++dt) {
+                        f32x16 tmp = acc[dt];
+                        asm volatile("" : "+v"(tmp));
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) tmp[i] *= alpha;
+                        acc[dt] = tmp;
+                        asm volatile("" : "+a"(acc[dt]));
+                    }
+                    asm volatile("s_nop 7");
+                }
+                constexpr int kRefFirst = 4;
+                phase_b(va, vr, pk, acc, [&](auto ic) __attribute__((always_inline)) {
+                    constexpr int m = decltype(ic)::value;
+                    if constexpr (NEXT && m >= kRefFirst && (m - kRefFirst) % 2 == 0 && (m - kRefFirst) / 2 < 4)
+                        reference(std::integral_constant<int, (m - kRefFirst) / 2>{}, sc_next);
+                    prepare(ic);
+                });
+            };
+            using yes = std::true_type;
+            using no = std::false_type;
+
+            issue_tile(0, st_cur);
+            int ka[4];
+            __amdgpu_buffer_rsrc_t next_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(a.k_pages), 0, 0, 0x00020000);
+            bool next_ok = false;
+            auto next_setup = [&](int u) __attribute__((always_inline)) {
+                if constexpr (!ANY_PAGE) {
+                    next_ok = u + 1 < n_tiles;
+                    if (next_ok) next_rsrc = tile_rsrc(u + 1);
+                }
+            };
+            auto next_load = [&](auto ic) __attribute__((always_inline)) {
+                if constexpr (!ANY_PAGE) {
+                    if (next_ok) issue_load(ic, next_rsrc, st_next);
+                }
+            };
+            auto nothing = [](auto) {};
+            int u = 0;
+            auto prepare_next = [&](auto ic) __attribute__((always_inline)) {
+                constexpr int m = decltype(ic)::value;
+                if constexpr (m == 14) {
+                    const int st = st_prev;
+                    st_prev = st_cur, st_cur = st_next, st_next = st;
+                    k_addrs(st_cur, ka);
+                } else if constexpr (m == 18) {
+                    next_setup(u + 1);
+                }
+            };
+            auto v_addrs_early = [&](auto ic) __attribute__((always_inline)) {
+                if constexpr (decltype(ic)::value == 2) v_addrs(st_prev, va);
+            };
+            k_addrs(st_cur, ka);
+            next_setup(0);
+            step_top(0);
+            phase_a<true, false>(ka, qt, qreg, s_a, s_b, pk, m_use, l_run, alpha, a.scale_log2, va, vr, next_load, nothing);
+            mfma_drain();
+            apply_mask(0, s_a);
+            for_each_index([&](auto ic) __attribute__((always_inline)) { reference(ic, s_a); }, std::make_integer_sequence<int, 4>{});
+            prepare_next(std::integral_constant<int, 14>{});
+            prepare_next(std::integral_constant<int, 18>{});
+            for (u = 1; u + 1 < n_tiles;) {
+                step_top(u);
+                phase_a<true, true>(ka, qt, qreg, s_b, s_a, pk, m_use, l_run, alpha, a.scale_log2, va, vr, next_load, v_addrs_early);
+                pv(u - 1, yes{}, s_b, prepare_next);
+                ++u;
+                step_top(u);
+                phase_a<true, true>(ka, qt, qreg, s_a, s_b, pk, m_use, l_run, alpha, a.scale_log2, va, vr, next_load, v_addrs_early);
+                pv(u - 1, yes{}, s_a, prepare_next);
+                ++u;
+            }
+            if (u < n_tiles) {
+                step_top(u);
+                phase_a<true, true>(ka, qt, qreg, s_b, s_a, pk, m_use, l_run, alpha, a.scale_log2, va, vr, next_load, v_addrs_early);
+                pv(u - 1, yes{}, s_b, prepare_next);
+                asm volatile("" : "+v"(s_b));       // the copy below reads s_b after the P.V MFMAs, not right behind the score MFMAs
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s_a[i] = s_b[i];
+            }
+            // the last tile's scores are in s_a, masked, and its reference is set; its stage is the one before the current
+            if (left_cur) step_top(n_tiles);
+            v_addrs(st_prev, va);
+            phase_a<false, true>(ka, qt, qreg, s_b, s_a, pk, m_use, l_run, alpha, a.scale_log2, va, vr, nothing, nothing);
+            pv(n_tiles - 1, no{}, s_a, nothing);
+            mfma_drain();
+        }
+
+        // ---- the row tile's output, or this piece's share of it ------------------------------------------
+        const float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
+        if (begins && (ends || t.r.bad)) {
+            const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;          // (a row of nothing but -inf: zeros)
+            if (row_ok) {
+                uint16_t* o = a.out + q_row * kDv + lg * 4;
+#pragma unroll
+                for (int dt = 0; dt < kDTiles; ++dt)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<u32x2*>(o + dt * 32 + i4 * 8) = u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv),
+                                                                               cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
+            }
+            continue;
+        }
+        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
+        if (begins) cut = PromptCut{t.b, t.kvh, t.i, pieces_of(plan, t, w)};
+        if (row_ok) {
+            const size_t prow = slot * kRowTile + wave * 32 + ln;
+            if (lg == 0) a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
+            float* po = a.part_acc + prow * kDv + lg * 4;
+#pragma unroll
+            for (int dt = 0; dt < kDTiles; ++dt)
+#pragma unroll
+                for (int i4 = 0; i4 < 4; ++i4)
+                    *reinterpret_cast<f32x4*>(po + dt * 32 + i4 * 8) = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
+        }
+    }
+    if (tid == 0) a.cuts[w] = cut;
+    if (a.status && __any(bad_page) && lane == 0) atomicOr(a.status, 2);
+}
+
+hipError_t launch_prompt_latent(const PromptArgs& a, hipStream_t stream) {
+    if (a.page_shift >= 0 && a.P >= mla::kMinPage) hipLaunchKernelGGL((prompt_latent_kernel<false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prompt_latent_kernel<true>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace seer

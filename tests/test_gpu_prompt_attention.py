@@ -97,7 +97,7 @@ def check(seed, new, past, Hq, Hkv, D, Dv, page, rows=None, **kw):
 
 
 HEADS = [(8, 2, 128, 128, 16), (4, 4, 64, 64, 16), (8, 1, 256, 256, 32), (16, 2, 192, 128, 64), (5, 1, 128, 128, 20), (6, 2, 64, 64, 1), (14, 2, 128, 128, 128),
-         (3, 3, 256, 256, 7), (2, 2, 192, 128, 48)]
+         (3, 3, 256, 256, 7), (2, 2, 192, 128, 48), (16, 1, 576, 512, 64), (128, 1, 576, 512, 32), (6, 2, 576, 512, 16), (5, 1, 576, 512, 20)]
 
 
 @pytest.mark.parametrize("heads", HEADS)
@@ -114,13 +114,13 @@ def test_one_request_and_single_tokens(heads, new, past):
     check(2, new, past, *heads, rows=300)
 
 
-@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("seed", range(8))
 def test_random_batches(seed):
     rng = np.random.default_rng(seed)
     B = int(rng.integers(1, 40))
     new = [int(rng.choice([0, 1, 1, rng.integers(1, 50), rng.integers(1, 900)])) for _ in range(B)]
     past = [int(rng.choice([0, 0, rng.integers(0, 100), rng.integers(0, 6000)])) for _ in range(B)]
-    heads = [(8, 2, 128, 128, 16), (8, 8, 128, 128, 64), (16, 1, 64, 64, 16), (10, 2, 128, 128, 16), (32, 4, 192, 128, 16), (8, 1, 256, 256, 16)][seed]
+    heads = [(8, 2, 128, 128, 16), (8, 8, 128, 128, 64), (16, 1, 64, 64, 16), (10, 2, 128, 128, 16), (32, 4, 192, 128, 16), (8, 1, 256, 256, 16), (16, 1, 576, 512, 64), (128, 1, 576, 512, 32)][seed]
     check(seed, new, past, *heads, rows=60, pad=int(rng.integers(0, 9)))
 
 
@@ -133,7 +133,8 @@ def test_more_requests_than_threads():
 
 
 @pytest.mark.parametrize("heads,new,past", [((8, 1, 128, 128, 16), [9000], [0]), ((8, 1, 128, 128, 16), [300, 1, 40], [50000, 60000, 3]), ((64, 8, 128, 128, 16), [4000, 10, 900], [0, 3000, 100]),
-                                            ((8, 1, 64, 64, 32), [12000, 5], [0, 30000]), ((16, 2, 256, 256, 16), [3000], [2000]), ((128, 1, 128, 128, 16), [700], [900])])
+                                            ((8, 1, 64, 64, 32), [12000, 5], [0, 30000]), ((16, 2, 256, 256, 16), [3000], [2000]), ((128, 1, 128, 128, 16), [700], [900]),
+                                            ((128, 1, 576, 512, 64), [300, 2], [900, 9000]), ((16, 1, 576, 512, 64), [1500, 4], [20000, 3])])
 def test_long_ones(heads, new, past):
     check(4, new, past, *heads, rows=40)
 
@@ -160,7 +161,7 @@ def spoil(x, b, j, c, value, dims=slice(None)):
     x[c["table"][b, j // c["page"]].long(), :, j % c["page"], dims] = value
 
 
-@pytest.mark.parametrize("heads", [(8, 2, 128, 128, 16), (4, 4, 64, 64, 20), (8, 1, 256, 256, 32), (16, 2, 192, 128, 64)])
+@pytest.mark.parametrize("heads", [(8, 2, 128, 128, 16), (4, 4, 64, 64, 20), (8, 1, 256, 256, 32), (16, 2, 192, 128, 64), (16, 1, 576, 512, 64), (5, 1, 576, 512, 20)])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 def test_what_a_token_does_not_see_does_not_reach_it(heads, value):
     """NaN and infinities in keys and values of the second half of a prompt, and in the page behind its end: the first half is what it is without
@@ -175,7 +176,8 @@ def test_what_a_token_does_not_see_does_not_reach_it(heads, value):
     for b, L in enumerate(c["ctx"].tolist()):                        # slots behind the last position
         for j in range(L, -(-L // c["page"]) * c["page"]):
             spoil(c["k"], b, j, c, value)
-            spoil(c["v"], b, j, c, value)
+            if c["v"] is not None:
+                spoil(c["v"], b, j, c, value)
     out, status = call(c)
     assert status == 0
     first, ctx = c["first"].tolist(), c["ctx"].tolist()
@@ -195,6 +197,23 @@ def test_values_that_are_not_finite_stay_in_their_component(heads):
     assert torch.equal(out[..., keep].cpu(), good[..., keep].cpu())
     assert torch.isinf(out[70:150, :, 5].float()).all() and torch.isinf(out[150 + 15:190, :, 5].float()).all()
     assert torch.equal(out[:70, :, 5], good[:70, :, 5])
+
+
+@pytest.mark.parametrize("page", [64, 20])
+def test_a_latent_that_is_not_finite_in_one_component(page):
+    """An infinite component of a latent whose score is -inf: rows that see it are what they are without that position, but for the component."""
+    c = make(14, [60], [10], 16, 1, 576, 512, page, std=0.5)
+    c["q"][..., 7] = c["q"][..., 7].abs() + 0.01
+    good, _ = call(c)
+    spoil(c["k"], 0, 40, c, -float("inf"), 7)                        # score -inf: probability 0, and 0 * inf in component 7
+    out, _ = call(c)
+    without = dict(c, k=c["k"].clone())
+    spoil(without["k"], 0, 40, c, -1e30, 7)                          # (a score that no probability is left of)
+    spoil(without["k"], 0, 40, c, 0.0, slice(0, 7))
+    ref, _ = call(without)
+    keep = [d for d in range(512) if d > 7]
+    assert torch.equal(out[:30], good[:30])
+    assert torch.equal(out[30:, :, keep], ref[30:, :, keep])
 
 
 def test_scores_of_nothing_but_minus_infinity_give_zeros():

@@ -129,8 +129,8 @@ def test_prompt_attention_workspace(lib):
     from paper_2511_14617_amd import binding as b
     size = b.seer_prompt_attention_workspace
     assert 0 < size(pp(), 1) <= size(pp(), 100000) <= size(pp(max_pages_per_seq=8192), 100000) < 1 << 28
-    for Dqk, Dv in ((64, 64), (192, 128), (256, 256)):
-        assert size(pp(Dqk=Dqk, Dv=Dv), 1000) > 0
+    for Dqk, Dv in ((64, 64), (192, 128), (256, 256), (576, 512)):
+        assert size(pp(Dqk=Dqk, Dv=Dv, kv_shared_latent=Dqk == 576), 1000) > 0
     for bad in (pp(B=0), pp(B=-1), pp(Hq=0), pp(Hkv=3), pp(Dqk=96), pp(Dv=64), pp(page_size=0), pp(num_pages=0), pp(max_pages_per_seq=0), pp(scale=0.0), pp(scale=float("nan"))):
         assert size(bad, 10) == 0
     assert size(pp(), 0) == 0 and size(pp(), -1) == 0 and lib.seer_prompt_attention_workspace(None, 5) == 0
@@ -151,7 +151,7 @@ def test_prompt_attention_argument_errors_before_any_launch(lib):
     for bad in (dict(Hkv=3), dict(max_pages_per_seq=1 << 27), dict(num_pages=1 << 30, page_size=16)):
         assert run(pp(**bad)) == b.SEER_ESHAPE, bad
     assert run(pp(max_pages_per_seq=1 << 26, Hq=1 << 14, Hkv=1), n=1 << 30) == b.SEER_ESHAPE
-    for bad in (dict(Dqk=96, Dv=96), dict(Dqk=128, Dv=64), dict(Dqk=576, Dv=512), dict(Dqk=128, kv_shared_latent=1)):
+    for bad in (dict(Dqk=96, Dv=96), dict(Dqk=128, Dv=64), dict(Dqk=576, Dv=512), dict(Dqk=576, Dv=576, kv_shared_latent=1), dict(Dqk=128, kv_shared_latent=1)):
         assert run(pp(**bad)) == b.SEER_EUNSUPPORTED, bad
     for name in ("out", "q", "kp", "vp", "table", "ctx", "first"):
         assert run(pp(), null=(name,)) == b.SEER_EINVAL, name
