@@ -42,10 +42,16 @@ struct PromptArgs {
     float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
     int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
     int W;
-    int page_shift;        // -1: pages are no power of two
+    uint32_t inv_p;        // 2^32 / P, at most 2^32 - 1
     float scale_log2;
     int64_t max_ctx;
 };
+
+// Page of a position.
+__device__ __forceinline__ int prompt_page(const PromptArgs& a, int position) {
+    const uint32_t x = static_cast<uint32_t>(position), q = __umulhi(x, a.inv_p);          // the quotient, or one less
+    return static_cast<int>(q + (x - q * static_cast<uint32_t>(a.P) >= static_cast<uint32_t>(a.P) ? 1u : 0u));
+}
 
 // A request as the line counts it.
 struct PromptRequest {

@@ -18,15 +18,81 @@
 
 namespace seer {
 
-// Workgroups that a CU holds: by registers (queries and outputs of 32 rows) and by LDS.
-constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 128 ? 2 : 1; }
+// Slots of the K ring and of the V ring, one tile of 32 positions each: K of tile u and V of tile u - 1 are read in step u, so each ring
+// has three tiles in flight behind the one in use.
+constexpr int kSlots = 4;
 
 template <int DQK, int DV>
-__global__ __launch_bounds__(kPromptThreads) __attribute__((amdgpu_waves_per_eu(prompt_waves_per_simd(DQK))))
+struct PromptShape {
+    static constexpr int kTile = 32;
+    static constexpr int kKRow = DQK * 2, kVRow = DV * 2;                     // bytes of a position's row
+    static constexpr int kKSlot = kTile * kKRow, kVSlot = kTile * kVRow;
+    static constexpr int kVBase = kSlots * kKSlot;                           // the V ring follows the K ring
+    static constexpr int kLds = kSlots * (kKSlot + kVSlot);
+    static constexpr int kKSteps = DQK / 16, kDTiles = DV / 32, kPv = 2 * kDTiles;      // contraction steps; d-tiles; MFMAs of a product
+    static constexpr int kKLoads = kKSlot / 4096, kVLoads = kVSlot / 4096;   // of 1 KB, per wave and tile
+    static constexpr int kKAhead = kKSteps < 8 ? kKSteps : 8;                // K operands requested ahead of their MFMA
+    static constexpr int kVAhead = kPv < 8 ? kPv : 8;                        // V operands (two reads each)
+    // waves that a SIMD holds, by registers: queries, outputs, scores of two tiles, operands
+    static constexpr int kWavesPerSimd = DQK <= 64 ? 3 : (DQK <= 128 ? 2 : 1);
+    static_assert(kKSlot % 4096 == 0 && kVSlot % 4096 == 0 && kLds <= 156 * 1024, "");
+};
+
+// One LDS read whose completion is waited for by count (LDS answers in order; see wait_lgkm): through the builtins the compiler would wait for the
+// tile loads in flight, which it cannot tell apart.  Every result is used behind such a wait in the same straight line of code.
+#define SEER_PROMPT_READ128(dst, addr, OFF) asm volatile("ds_read_b128 %0, %1 offset:%2" : "=&v"(dst) : "v"(addr), "n"(OFF))
+#define SEER_PROMPT_READ_TR(dst, addr, OFF_LO, OFF_HI)                \
+    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n"              \
+                 "ds_read_b64_tr_b16 %1, %2 offset:%4"                \
+                 : "=&v"(dst[0]), "=&v"(dst[1])                       \
+                 : "v"(addr), "n"(OFF_LO), "n"(OFF_HI))
+template <int N>
+__device__ __forceinline__ void wait_reads() {
+    static_assert(N >= 0 && N < 16, "lgkmcnt is a 4-bit counter");
+    __builtin_amdgcn_s_waitcnt(0xc07f | (N << 8));
+    __builtin_amdgcn_sched_barrier(0);
+}
+template <int N>
+using I = std::integral_constant<int, N>;
+template <typename F, int... N>
+__device__ __forceinline__ void each_index(F&& f, std::integer_sequence<int, N...>) {
+    (f(I<N>{}), ...);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const unsigned char* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(p), 0, bytes, 0x00020000);
+}
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, unsigned char* to, int offset) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (SEER_AS3 void*)(to), 16, offset, 0, 0, 0);
+}
+// Requests a wave's eight rows of a tile: at_row = row of the pool of the first of them (ANY_PAGE: of the tile's position lane % 32).
+template <int ROW, int LOADS, bool ANY_PAGE>
+__device__ __forceinline__ void issue_rows(const unsigned char* pool, uint32_t at_row, const int (&pat)[LOADS], unsigned char* slot, int wave, int lane) {
+    if constexpr (ANY_PAGE) {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int r = (j * kWave + lane) / (ROW / 16);
+            const uint32_t from = __builtin_amdgcn_ds_bpermute((wave * 8 + r) << 2, at_row);
+            const unsigned char* src = pool + static_cast<size_t>(from) * ROW + (pat[j] - r * ROW);
+            __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(slot + (wave * LOADS + j) * 1024), 16, 0, 0);
+        }
+    } else {
+        const __amdgpu_buffer_rsrc_t rsrc = rows_at(pool + static_cast<size_t>(at_row) * ROW, 8 * ROW);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) load_to_lds(rsrc, slot + (wave * LOADS + j) * 1024, pat[j]);
+    }
+}
+
+// ANY_PAGE: pages of any size; else of a multiple of 16 positions, so that the eight rows of a tile that a wave loads lie in one page.
+template <int DQK, int DV, bool ANY_PAGE>
+__global__ __launch_bounds__(kPromptThreads) __attribute__((amdgpu_waves_per_eu(PromptShape<DQK, DV>::kWavesPerSimd)))
 void prompt_tile_kernel(PromptArgs a) {
-    using namespace tile;
-    using S = Shape<DQK, DV>;
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * S::kStage];
+    using S = PromptShape<DQK, DV>;
+    using O = tile::Operands<DQK, DV>;
+    using tile::k_swz;
+    using tile::v_swz;
+    constexpr int kTile = S::kTile;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[S::kLds];
     __shared__ PromptLds s_plan;
     __shared__ uint32_t s_found;                    // V rows with infinities or NaN of the scanned tile
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
@@ -50,214 +116,402 @@ void prompt_tile_kernel(PromptArgs a) {
         x = moved_cut(plan, ends[0], at[0]);
         x_end = moved_cut(plan, ends[1], at[1]);
         t = ends[0];
+        PromptCut cut{0, 0, 0, 0};                  // the row tile that begins in this stretch and goes on behind it
+        if (x_end > ends[1].begin && x_end < ends[1].begin + ends[1].cost && ends[1].begin >= x && !ends[1].r.bad)
+            cut = PromptCut{ends[1].b, ends[1].kvh, ends[1].i, pieces_of(plan, ends[1], w)};
+        if (tid == 0) a.cuts[w] = cut;
     }
-    PromptCut cut{0, 0, 0, 0};
     bool bad_page = false;
-    const int lds0 = lds_addr(lds);
-    auto page_of = [&](int64_t tok) __attribute__((always_inline)) -> int { return static_cast<int>(a.page_shift >= 0 ? tok >> a.page_shift : tok / a.P); };
-    const Operands<DQK, DV> operands;
+    const int lds0 = tile::lds_addr(lds);
+    auto page_of = [&](int position) __attribute__((always_inline)) -> int { return prompt_page(a, position); };
+
+    // ---- what stays for the whole stretch: operand addresses, byte offsets of this lane's loads in its wave's eight rows ----------
+    const O operands;
+    int k_at[O::kPerXor], v_at[O::kPerV], k_pat[S::kKLoads], v_pat[S::kVLoads];
+#pragma unroll
+    for (int i = 0; i < O::kPerXor; ++i) k_at[i] = (lds0 + operands.k_rd) ^ (i << 5);
+#pragma unroll
+    for (int i = 0; i < O::kPerV; ++i) v_at[i] = (lds0 + S::kVBase + (operands.v_rd - tile::Shape<DQK, DV>::kKBytes)) ^ (i << 6);
+#pragma unroll
+    for (int j = 0; j < S::kKLoads; ++j) {
+        const int c = j * kWave + lane, r = c / (S::kKRow / 16), pos = c - r * (S::kKRow / 16);
+        k_pat[j] = r * S::kKRow + ((pos ^ k_swz<S::kKRow>(wave * 8 + r)) << 4);
+    }
+#pragma unroll
+    for (int j = 0; j < S::kVLoads; ++j) {
+        const int c = j * kWave + lane, r = c / (S::kVRow / 16), pos = c - r * (S::kVRow / 16);
+        v_pat[j] = r * S::kVRow + ((pos ^ v_swz<S::kVRow>(wave * 8 + r)) << 4);
+    }
 
     while (x < x_end) {
         if (x >= t.begin + t.cost) next_tile(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
-        const int rows = min(kRowTile, static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile))));
+        const int rows = static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile)));
         const int token_first = static_cast<int>(static_cast<int64_t>(t.i) * kRowTile / a.G);                      // of the request's new tokens
         const int token_last = static_cast<int>((static_cast<int64_t>(t.i) * kRowTile + rows - 1) / a.G);
         const int seen = static_cast<int>(t.r.past) + token_last + 1;                                              // positions that the last row sees
+        const int all_see = static_cast<int>(t.r.past) + token_first;                                              // the last one that all rows see
         const int tiles = t.r.bad ? 0 : (seen + kTile - 1) / kTile;
         // the piece's tiles (the same rounding on both sides of a cut)
         const int u0 = begins ? 0 : static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
         const int u1 = ends ? tiles : static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
         x = end;
         if (t.r.bad && !begins) continue;
+        const int n_tiles = u1 - u0, tok_begin = u0 * kTile;
 
         // ---- this lane's query row -------------------------------------------------------------------------
         const int64_t row = static_cast<int64_t>(t.i) * kRowTile + wave * 32 + ln;
         const bool row_ok = wave * 32 + ln < rows;
         const int token = row_ok ? static_cast<int>(row / a.G) : 0;
-        const size_t q_row = (static_cast<size_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0);
+        const uint32_t q_row = static_cast<uint32_t>((static_cast<int64_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0));
         const int sees = row_ok ? static_cast<int>(t.r.past) + token : -1;                                         // last position that it sees
-        // of the wave: its first row's, its last row's
-        const int sees_lo = __builtin_amdgcn_readfirstlane(sees);
-        const int sees_hi = sees_lo < 0 ? -1 : static_cast<int>(t.r.past) + static_cast<int>((static_cast<int64_t>(t.i) * kRowTile + min(wave * 32 + 31, rows - 1)) / a.G);
-        bf16x8 qreg[S::kKSteps];
-        {
-            const u32x4* qp = reinterpret_cast<const u32x4*>(a.q + q_row * DQK + lg * 8);
-#pragma unroll
-            for (int kk = 0; kk < S::kKSteps; ++kk) {
-                u32x4 v = {0u, 0u, 0u, 0u};
-                if (row_ok) v = qp[kk * 2];
-                qreg[kk] = as_bf16x8(v);
-            }
-        }
+        const int sees_lo = __builtin_amdgcn_readfirstlane(sees);                                                  // the wave's first row
         f32x16 acc[S::kDTiles];
 #pragma unroll
         for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-        float m_run = kNegInf, l_run = 0.f, top = kNegInf;
+        float m_run = kNegInf, l_run = 0.f;
+        __syncthreads();                            // every wave is done with the rings of the piece before
+        if (n_tiles > 0) {
+            u32x4 qreg[S::kKSteps];
+            {
+                const u32x4* qp = reinterpret_cast<const u32x4*>(a.q + static_cast<size_t>(q_row) * DQK + lg * 8);
+#pragma unroll
+                for (int kk = 0; kk < S::kKSteps; ++kk) {
+                    qreg[kk] = u32x4{0u, 0u, 0u, 0u};
+                    if (row_ok) qreg[kk] = qp[kk * 2];
+                }
+            }
+            // ---- tile loads --------------------------------------------------------------------------------
+            const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
+            const int last_page = page_of(static_cast<int>(t.r.past) + t.r.n - 1);
+            int win = -0x40000000, pg_win = 0;      // lane l holds the (clamped) page id of logical page win + l
+            auto set_window = [&](int first) __attribute__((always_inline)) {
+                win = first;
+                int pg = table[min(first + lane, a.max_pages - 1)];
+                if (pg < 0 || pg >= a.num_pages) {
+                    if (first + lane <= last_page) bad_page = true;
+                    pg = min(max(pg, 0), a.num_pages - 1);
+                }
+                pg_win = pg;
+            };
+            // Row of the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU) of tile u's position 8 wave; ANY_PAGE: of position ln.
+            // Tiles are asked for in ascending order.
+            auto tile_row = [&](int u) __attribute__((always_inline)) -> uint32_t {
+                const int tb = tok_begin + u * kTile;
+                if constexpr (ANY_PAGE) {
+                    if (page_of(tb) < win || page_of(tb + kTile - 1) >= win + kWave) set_window(page_of(tb));      // (uniform; a tile spans at most 32 pages)
+                    const int lp = page_of(tb + ln);
+                    const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
+                    return (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tb + ln - lp * a.P);
+                } else {
+                    const int tok = tb + wave * 8, lp = page_of(tok);
+                    if (lp < win || lp >= win + kWave) set_window(lp);
+                    const uint32_t pg = __builtin_amdgcn_readlane(pg_win, __builtin_amdgcn_readfirstlane(lp - win));
+                    return (pg * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - lp * a.P);
+                }
+            };
+            auto issue_k = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
+                issue_rows<S::kKRow, S::kKLoads, ANY_PAGE>(a.k_pages, at_row, k_pat, lds + (u & (kSlots - 1)) * S::kKSlot, wave, lane);
+            };
+            auto issue_v = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
+                issue_rows<S::kVRow, S::kVLoads, ANY_PAGE>(a.v_pages, at_row, v_pat, lds + S::kVBase + (u & (kSlots - 1)) * S::kVSlot, wave, lane);
+            };
 
-        // ---- tile loads ------------------------------------------------------------------------------------
-        const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
-        const int last_page = page_of(static_cast<int64_t>(t.r.past) + t.r.n - 1);
-        int win = 0, pg_win = 0;                    // lane l holds the (clamped) page id of logical page win + l
-        auto set_window = [&](int first) __attribute__((always_inline)) {
-            win = first;
-            int pg = table[min(first + lane, a.max_pages - 1)];
-            if (pg < 0 || pg >= a.num_pages) {
-                if (first + lane <= last_page) bad_page = true;
-                pg = min(max(pg, 0), a.num_pages - 1);
-            }
-            pg_win = pg;
-        };
-        auto issue_tile = [&](int u, int stage) __attribute__((always_inline)) {
-            const int64_t tb = static_cast<int64_t>(u) * kTile;
-            const int first = page_of(tb);
-            if (u == u0 || page_of(tb + kTile - 1) >= win + kWave) set_window(first);           // (uniform; a tile spans at most 32 pages)
-            const int64_t tok = tb + ln;
-            const int lp = page_of(tok);
-            const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
-            // row index in the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU)
-            const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - static_cast<int64_t>(lp) * a.P);
-            constexpr int kKChunks = S::kKRow / 16, kVChunks = S::kVRow / 16;
+            // ---- softmax ------------------------------------------------------------------------------------
+            f32x16 s_a, s_b;
+            uint32_t pk[8];
+            float m_use = 0.f, alpha = 1.f;
+            // The exponent reference for tile u's scores; it moves only when a maximum exceeds it by more than 8 (in units of log2 e: probabilities stay
+            // below 2^8, which bf16 and fp32 hold as well as any), so that outputs are seldom rescaled.
+            auto reference = [&](auto maskc, int u, f32x16& s) __attribute__((always_inline)) {
+                const int tb = tok_begin + u * kTile;
+                if (decltype(maskc)::value && tb + kTile - 1 > sees_lo) {            // (wave-uniform)
+                    const int lim = sees - tb;      // last position of the tile that the row sees
+                    uint32_t vis = lim < 0 ? 0u : (lim >= 31 ? 0xffffffffu : (2u << lim) - 1u);
+                    vis >>= lg * 4;
 #pragma unroll
-            for (int j0 = 0; j0 < S::kKBytes / 1024; j0 += 4) {
-                const int c = (j0 + wave) * kWave + lane, r = c / kKChunks, pos = c - r * kKChunks;
-                if (S::kKBytes / 1024 % 4 != 0 && j0 + wave >= S::kKBytes / 1024) break;
-                const uint32_t from = __builtin_amdgcn_ds_bpermute(r << 2, row_idx);
-                const unsigned char* src = a.k_pages + static_cast<size_t>(from) * S::kKRow + ((pos ^ k_swz<S::kKRow>(r)) << 4);
-                __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage + (j0 + wave) * 1024), 16, 0, 0);
-            }
+                    for (int i = 0; i < 16; ++i)
+                        if (!((vis >> ((i >> 2) * 8 + (i & 3))) & 1u)) s[i] = kNegInf;
+                }
+                float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-            for (int j0 = 0; j0 < S::kVBytes / 1024; j0 += 4) {
-                const int c = (j0 + wave) * kWave + lane, r = c / kVChunks, pos = c - r * kVChunks;
-                if (S::kVBytes / 1024 % 4 != 0 && j0 + wave >= S::kVBytes / 1024) break;
-                const uint32_t from = __builtin_amdgcn_ds_bpermute(r << 2, row_idx);
-                const unsigned char* src = a.v_pages + static_cast<size_t>(from) * S::kVRow + ((pos ^ v_swz<S::kVRow>(r)) << 4);
-                __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(lds + stage + S::kKBytes + (j0 + wave) * 1024), 16, 0, 0);
-            }
-        };
-        __syncthreads();                            // every wave is done with the stages of the piece before
-        if (u0 < u1) issue_tile(u0, 0);
-        for (int u = u0; u < u1; ++u) {
-            const int stage = ((u - u0) & 1) * S::kStage;
-            wait_vmcnt<0>();
-            bare_barrier();                         // tile u has landed for every wave, every wave is done with tile u - 1
-            if (u + 1 < u1) issue_tile(u + 1, S::kStage - stage);
-            __builtin_amdgcn_sched_barrier(0);
-            const int tb = u * kTile;
-            uint32_t nonfinite = 0;                 // uniform: positions of this tile whose V row is kept out of the product
-            if (tb + kTile - 1 > static_cast<int>(t.r.past) + token_first) {
-                unsigned char* vl = lds + stage + S::kKBytes;
+                for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
+                m_use = move_reference(fmaxf(mx, s[15]), a.scale_log2, m_run, alpha);
+            };
+            float psum = 0.f, p_even = 0.f;
+            auto probability = [&](auto ic, const f32x16& s) __attribute__((always_inline)) {
+                constexpr int i = decltype(ic)::value;
+                const float p = fast_exp2(fmaf(s[i], a.scale_log2, -m_use));
+                if constexpr (i % 2 == 0) {
+                    p_even = p;
+                } else {
+                    pk[i >> 1] = cvt_pk_bf16(p_even, p);
+                    psum = add_bf16_pair(pk[i >> 1], psum);          // (what the product will see)
+                }
+            };
+
+            // ---- V rows with infinities or NaN of the tile in V slot `slot_at` (tile u), where some row does not see all of it ----------
+            uint32_t left = 0;                      // uniform: positions whose V row is kept out of the product
+            auto scan = [&](int u, int slot_at) __attribute__((always_inline)) {
+                left = 0;
+                if (tok_begin + u * kTile + kTile - 1 <= all_see) return;
+                unsigned char* vl = lds + S::kVBase + slot_at;
                 if (tid == 0) s_found = 0;
-                __builtin_amdgcn_s_waitcnt(0xc07f);
+                wait_reads<0>();
                 bare_barrier();
-                const uint32_t found = tile_nonfinite<DQK, DV>(vl, tid, kPromptThreads);
+                const uint32_t found = tile::tile_nonfinite<DQK, DV>(vl, tid, kPromptThreads);
                 if (found) atomicOr(&s_found, found);
-                __builtin_amdgcn_s_waitcnt(0xc07f);
+                wait_reads<0>();
                 bare_barrier();
-                nonfinite = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
-                if (nonfinite) {
-                    tile_clear_rows<DQK, DV>(vl, nonfinite, tid, kPromptThreads);
-                    __builtin_amdgcn_s_waitcnt(0xc07f);
+                left = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
+                if (left) {
+                    tile::tile_clear_rows<DQK, DV>(vl, left, tid, kPromptThreads);
+                    wait_reads<0>();
                 }
                 bare_barrier();
-            }
-            if (tb > sees_hi) continue;             // (wave-uniform)
-            f32x16 s = tile_scores<DQK, DV>(lds0 + stage, operands, qreg);
-            const int lim = sees - tb;              // last position of the tile that the row sees
-            const uint64_t word = lim < 0 ? 0 : (lim >= 31 ? 0xffffffffull : (2ull << lim) - 1);
-            if (tb + kTile - 1 > sees_lo) tile_mask(s, word, 0);
-            float alpha;
-            uint32_t term[1][8];
-            tile_softmax<1>(s, a.scale_log2, top, m_run, l_run, alpha, term);
-            if (__any(alpha != 1.f)) {
+            };
+
+            // ---- step u: scores of tile u beside the probabilities of tile u - 1, then the product with V of tile u - 1 beside the loads and
+            // the reference of tile u ----------------------------------------------------------------------------------------------------
+            uint32_t row2 = 0;                      // row of tile u + 2: its K was requested in the step before
+            auto top = [&](int u) __attribute__((always_inline)) {
+                constexpr int K = S::kKLoads, V = S::kVLoads;        // loads that may be in flight behind those of K of tile u and V of tile u - 1
+                if (u + 2 < n_tiles) wait_vmcnt<2 * K + 2 * V>();
+                else if (u + 1 < n_tiles) wait_vmcnt<K + 2 * V>();
+                else if (u < n_tiles) wait_vmcnt<V>();
+                else wait_vmcnt<0>();
+                bare_barrier();                     // they have landed for every wave, every wave is done with step u - 1
+            };
+            auto loads = [&](int u) __attribute__((always_inline)) {
+                uint32_t row3 = 0;
+                if (u + 3 < n_tiles) {
+                    row3 = tile_row(u + 3);
+                    issue_k(u + 3, row3);
+                }
+                if (u + 2 < n_tiles) issue_v(u + 2, row2);
+                row2 = row3;
+            };
+            u32x2 vr[S::kVAhead][2];
+            // V operand m of a product (d-tile m / 2, positions of half m % 2) into its ring slot
+            auto read_v = [&](auto mc, auto slotc, int shift) __attribute__((always_inline)) {
+                constexpr int m = decltype(mc)::value, dt = m >> 1, half = m & 1;
+                constexpr int off = decltype(slotc)::value * S::kVSlot + dt / O::kPerV * (O::kPerV * 64) + half * 16 * S::kVRow;
+                (void)&vr;
+                const int from = v_at[dt % O::kPerV] + shift;
+                SEER_PROMPT_READ_TR(vr[m % S::kVAhead], from, off, off + 8 * S::kVRow);
+            };
+            auto product = [&](auto slotc, int shift, auto&& beside) __attribute__((always_inline)) {
+                const bf16x8 p0 = as_bf16x8(u32x4{pk[0], pk[1], pk[2], pk[3]}), p1 = as_bf16x8(u32x4{pk[4], pk[5], pk[6], pk[7]});
+                each_index([&](auto mc) __attribute__((always_inline)) {
+                    constexpr int m = decltype(mc)::value, later = S::kPv - 1 - m;
+                    wait_reads<2 * (later < S::kVAhead - 1 ? later : S::kVAhead - 1)>();
+                    const bf16x8 v = as_bf16x8(u32x4{vr[m % S::kVAhead][0][0], vr[m % S::kVAhead][0][1], vr[m % S::kVAhead][1][0], vr[m % S::kVAhead][1][1]});
+                    acc[m >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, (m & 1) ? p1 : p0, acc[m >> 1], 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (m + S::kVAhead < S::kPv) read_v(std::integral_constant<int, m + S::kVAhead>{}, slotc, shift);
+                    beside(mc);
+                    __builtin_amdgcn_sched_barrier(0);
+                }, std::make_integer_sequence<int, S::kPv>{});
+            };
+            auto rescale = [&]() __attribute__((always_inline)) {
+                if (__any(alpha != 1.f)) {
 #pragma unroll
-                for (int dt = 0; dt < S::kDTiles; ++dt)
+                    for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
-            }
-            tile_pv<DQK, DV, 1>(lds0 + stage, operands, term, acc);
-            if (nonfinite)
-                tile_add_rows<1>(nonfinite, term, word, 0, acc, [&](int j) __attribute__((always_inline)) -> const uint16_t* {
-                    const int64_t tok = static_cast<int64_t>(tb) + j;
-                    const int lp = page_of(tok);
+                        for (int i = 0; i < 16; ++i) acc[dt][i] *= alpha;
+                }
+            };
+            auto add_left = [&](int u) __attribute__((always_inline)) {
+                if (!left) return;
+                const int tb = tok_begin + u * kTile, lim = sees - tb;
+                const uint64_t word = lim < 0 ? 0 : (lim >= 31 ? 0xffffffffull : (2ull << lim) - 1);
+                uint32_t term[1][8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) term[0][i] = pk[i];
+                tile::tile_add_rows<1>(left, term, word, 0, acc, [&](int j) __attribute__((always_inline)) -> const uint16_t* {
+                    const int lp = page_of(tb + j);
                     const int pg = min(max(table[min(lp, a.max_pages - 1)], 0), a.num_pages - 1);
-                    return reinterpret_cast<const uint16_t*>(a.v_pages) + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (tok - static_cast<int64_t>(lp) * a.P)) * DV;
+                    return reinterpret_cast<const uint16_t*>(a.v_pages) + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (tb + j - lp * a.P)) * DV;
                 });
+            };
+            // The step itself, behind top(): K of tile u in slot SLOT (+ k_shift), V of tile u - 1 in slot BEFORE (+ v_shift).  PREV: there is a tile
+            // u - 1; EDGE, MASK: that some rows do not see all of tile u - 1, of tile u.
+            auto step = [&](auto slotc, auto beforec, auto prevc, auto edgec, auto maskc, int u, int k_shift, int v_shift, f32x16& s_new, const f32x16& s_old) __attribute__((always_inline)) {
+                constexpr int SLOT = decltype(slotc)::value;
+                constexpr bool PREV = decltype(prevc)::value, EDGE = decltype(edgec)::value;
+                u32x4 kr[S::kKAhead];
+                each_index([&](auto kc) __attribute__((always_inline)) {
+                    constexpr int kk = decltype(kc)::value;
+                    (void)&kr;                      // (asm operands alone do not capture)
+                    const int from = k_at[kk % O::kPerXor] + k_shift;
+                    SEER_PROMPT_READ128(kr[kk], from, SLOT * S::kKSlot + kk / O::kPerXor * (O::kPerXor * 32));
+                }, std::make_integer_sequence<int, S::kKAhead>{});
+                __builtin_amdgcn_sched_barrier(0);
+                loads(u);
+                __builtin_amdgcn_sched_barrier(0);
+                psum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s_new[i] = 0.f;
+                each_index([&](auto kc) __attribute__((always_inline)) {
+                    constexpr int kk = decltype(kc)::value;
+                    (void)&kr;
+                    // behind K operand kk: the K operands requested since, and the V operands, a pair behind each MFMA from kVFirst on
+                    constexpr int kAfter = S::kKSteps - 1 - kk < S::kKAhead - 1 ? S::kKSteps - 1 - kk : S::kKAhead - 1;
+                    constexpr int kVFirst = S::kKSteps - S::kVAhead;
+                    constexpr int kVSoFar = PREV && kk > kVFirst ? 2 * (kk - kVFirst) : 0;
+                    static_assert(kVFirst >= S::kKSteps - S::kKAhead && kAfter + kVSoFar < 16, "");
+                    wait_reads<kAfter + kVSoFar>();
+                    s_new = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kr[kk % S::kKAhead]), as_bf16x8(qreg[kk]), s_new, 0, 0, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if constexpr (kk + S::kKAhead < S::kKSteps) {
+                        const int from = k_at[(kk + S::kKAhead) % O::kPerXor] + k_shift;
+                        SEER_PROMPT_READ128(kr[kk % S::kKAhead], from, SLOT * S::kKSlot + (kk + S::kKAhead) / O::kPerXor * (O::kPerXor * 32));
+                    }
+                    if constexpr (PREV && kk >= kVFirst) read_v(std::integral_constant<int, kk - kVFirst>{}, beforec, v_shift);
+                    if constexpr (PREV) {
+                        constexpr int e0 = 16 * kk / S::kKSteps, e1 = 16 * (kk + 1) / S::kKSteps;
+                        each_index([&](auto ec) __attribute__((always_inline)) { probability(std::integral_constant<int, e0 + decltype(ec)::value>{}, s_old); },
+                                   std::make_integer_sequence<int, e1 - e0>{});
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }, std::make_integer_sequence<int, S::kKSteps>{});
+                if constexpr (PREV) {
+                    l_run = l_run * alpha + psum;
+                    rescale();
+                    __builtin_amdgcn_sched_barrier(0);
+                    product(beforec, v_shift, [](auto) {});
+                    if constexpr (EDGE) add_left(u - 1);
+                }
+                reference(maskc, u, s_new);
+            };
+
+            // the first tiles: K of 0, 1, 2 and V of 0, 1, in the order in which steps -3, -2, -1 would request them
+            {
+                const uint32_t row0 = tile_row(0);
+                uint32_t row1 = 0;
+                issue_k(0, row0);
+                if (n_tiles > 1) row1 = tile_row(1), issue_k(1, row1);
+                issue_v(0, row0);
+                if (n_tiles > 2) row2 = tile_row(2), issue_k(2, row2);
+                if (n_tiles > 1) issue_v(1, row1);
+            }
+            using yes = std::true_type;
+            using no = std::false_type;
+            top(0);
+            step(I<0>{}, I<0>{}, no{}, no{}, yes{}, 0, 0, 0, s_a, s_b);
+            // tiles that every row sees whole, slots at fixed places; then the others
+            const int whole = min(n_tiles, (all_see + 1 - tok_begin) / kTile);      // (below 0: none)
+            int u = 1;
+            for (; u + 3 < whole; u += 4) {
+                top(u);
+                step(I<1>{}, I<0>{}, yes{}, no{}, no{}, u, 0, 0, s_b, s_a);
+                top(u + 1);
+                step(I<2>{}, I<1>{}, yes{}, no{}, no{}, u + 1, 0, 0, s_a, s_b);
+                top(u + 2);
+                step(I<3>{}, I<2>{}, yes{}, no{}, no{}, u + 2, 0, 0, s_b, s_a);
+                top(u + 3);
+                step(I<0>{}, I<3>{}, yes{}, no{}, no{}, u + 3, 0, 0, s_a, s_b);
+            }
+            for (; u < n_tiles; ++u) {
+                top(u);
+                scan(u - 1, ((u - 1) & (kSlots - 1)) * S::kVSlot);
+                step(I<0>{}, I<0>{}, yes{}, yes{}, yes{}, u, (u & (kSlots - 1)) * S::kKSlot, ((u - 1) & (kSlots - 1)) * S::kVSlot, s_b, s_a);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s_a[i] = s_b[i];
+            }
+            // the last tile's probabilities and product
+            top(n_tiles);
+            const int shift = ((n_tiles - 1) & (kSlots - 1)) * S::kVSlot;
+            scan(n_tiles - 1, shift);
+            each_index([&](auto mc) __attribute__((always_inline)) { read_v(mc, I<0>{}, shift); }, std::make_integer_sequence<int, S::kVAhead>{});
+            __builtin_amdgcn_sched_barrier(0);
+            psum = 0.f;
+            each_index([&](auto ec) __attribute__((always_inline)) { probability(ec, s_a); }, std::make_integer_sequence<int, 16>{});
+            l_run = l_run * alpha + psum;
+            rescale();
+            __builtin_amdgcn_sched_barrier(0);
+            product(I<0>{}, shift, [](auto) {});
+            add_left(n_tiles - 1);
         }
 
         // ---- the row tile's output, or this piece's share of it ------------------------------------------
         const float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
         if (begins && (ends || t.r.bad)) {
             const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;          // (a row of nothing but -inf: zeros)
-            if (row_ok) {
-                uint16_t* o = a.out + q_row * DV + lg * 4;
-#pragma unroll
-                for (int dt = 0; dt < S::kDTiles; ++dt)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<u32x2*>(o + dt * 32 + i4 * 8) = u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv),
-                                                                               cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
-            }
-            continue;
-        }
-        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
-        if (begins) cut = PromptCut{t.b, t.kvh, t.i, pieces_of(plan, t, w)};
-        if (row_ok) {
-            const size_t prow = slot * kRowTile + wave * 32 + ln;
-            if (lg == 0) a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
-            float* po = a.part_acc + prow * DV + lg * 4;
+            // through LDS, so that a store takes whole rows: 16-byte chunk c of row r at c ^ r (its low bits)
+            constexpr int kChunks = DV / 8, kPerStore = kWave / (kChunks < kWave ? kChunks : kWave);      // rows of a store
+            static_assert(4 * 32 * DV * 2 <= S::kLds, "");
+            unsigned char* mine = lds + wave * (32 * DV * 2);
+            __syncthreads();                        // every wave is done with the rings
 #pragma unroll
             for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<f32x4*>(po + dt * 32 + i4 * 8) = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
+                    *reinterpret_cast<u32x2*>(mine + ln * (DV * 2) + (((dt * 4 + i4) ^ (ln & (kChunks - 1) & 15)) << 4) + lg * 8) =
+                        u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv), cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int j = 0; j < 32 / kPerStore; ++j) {
+                const int r = j * kPerStore + lane / kChunks, c = lane % kChunks;
+                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (DV * 2) + ((c ^ (r & (kChunks - 1) & 15)) << 4));
+                const uint32_t to = __shfl(q_row, r, kWave);
+                if (wave * 32 + r < rows) *reinterpret_cast<u32x4*>(a.out + static_cast<size_t>(to) * DV + c * 8) = v;
+            }
+            continue;
         }
+        // a lane's registers as they are, so that a store takes 1 KB: see partial_at
+        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
+        if (lg == 0) {
+            const size_t prow = slot * kRowTile + wave * 32 + ln;
+            a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
+        }
+        f32x4* po = reinterpret_cast<f32x4*>(a.part_acc) + (slot * 4 + wave) * (S::kDTiles * 4 * kWave) + lane;
+#pragma unroll
+        for (int dt = 0; dt < S::kDTiles; ++dt)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) po[(dt * 4 + i4) * kWave] = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
     }
-    if (tid == 0) a.cuts[w] = cut;
     if (a.status && __any(bad_page) && lane == 0) atomicOr(a.status, 2);
 }
 
 // Joins the pieces of the row tile that was cut at the end of stretch blockIdx.x, eight rows a workgroup.
-constexpr int kJoinRows = 8;
-
+// A workgroup takes a quarter of a wave's rows and outputs: one f32x4 of a lane (row ln, outputs dt * 32 + i4 * 8 + lg * 4 .. + 3) per thread.
 template <int DV>
 __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs a) {
-    const int w = blockIdx.x / (kRowTile / kJoinRows), part = blockIdx.x % (kRowTile / kJoinRows);
+    constexpr int kVectors = kRowTile * DV / 4, kBlocks = kVectors / kPromptThreads;
+    const int w = blockIdx.x / kBlocks, e = blockIdx.x % kBlocks * kPromptThreads + threadIdx.x;
     const PromptCut cut = a.cuts[w];
     if (cut.pieces < 2) return;
     const int first = a.first[cut.b], n = a.first[cut.b + 1] - first;
-    const int64_t row0 = static_cast<int64_t>(cut.tile) * kRowTile;
-    constexpr int kThreadsPerRow = kPromptThreads / kJoinRows, kEach = DV / kThreadsPerRow;      // 32 threads a row
-    const int r = part * kJoinRows + threadIdx.x / kThreadsPerRow, d = threadIdx.x % kThreadsPerRow * kEach;
-    const int64_t row = row0 + r;
+    const int lane = e & (kWave - 1), vec = e / kWave % (DV / 8), wave = e / kWave / (DV / 8);
+    const int r = wave * 32 + (lane & 31), d = vec * 8 + (lane >> 5) * 4;
+    const int64_t row = static_cast<int64_t>(cut.tile) * kRowTile + r;
     if (row >= static_cast<int64_t>(n) * a.G) return;
-    auto slot = [&](int k) { return (2 * static_cast<size_t>(w + k) + (k == 0 ? 1 : 0)) * kRowTile + r; };
+    auto slot = [&](int k) { return 2 * static_cast<size_t>(w + k) + (k == 0 ? 1 : 0); };
     float m = kNegInf;
-    for (int k = 0; k < cut.pieces; ++k) m = fmaxf(m, a.part_ml[2 * slot(k)]);
-    float l = 0.f, o[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) o[i] = 0.f;
+    for (int k = 0; k < cut.pieces; ++k) m = fmaxf(m, a.part_ml[2 * (slot(k) * kRowTile + r)]);
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < cut.pieces; ++k) {
-        const size_t at = slot(k);
-        const float mk = a.part_ml[2 * at], lk = a.part_ml[2 * at + 1];
+        const float mk = a.part_ml[2 * (slot(k) * kRowTile + r)], lk = a.part_ml[2 * (slot(k) * kRowTile + r) + 1];
         const float f = mk == kNegInf ? 0.f : fast_exp2(mk - m);
+        const f32x4 v = *(reinterpret_cast<const f32x4*>(a.part_acc) + slot(k) * kVectors + e);
         l = fmaf(lk, f, l);
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) o[i] = fmaf(a.part_acc[at * DV + d + i], f, o[i]);
+        for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t token = row / a.G;
     uint16_t* out = a.out + ((static_cast<size_t>(first) + token) * a.Hq + cut.kvh * a.G + (row - token * a.G)) * DV + d;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) out[i] = f32_to_bf16(o[i] * inv);
+    *reinterpret_cast<u32x2*>(out) = u32x2{cvt_pk_bf16(o[0] * inv, o[1] * inv), cvt_pk_bf16(o[2] * inv, o[3] * inv)};
 }
 
 static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
-    const dim3 grid(a.W * (kRowTile / kJoinRows));
+    const dim3 grid(a.W * (kRowTile * a.Dv / 4 / kPromptThreads));
     if (a.Dv == 64) hipLaunchKernelGGL((prompt_join_kernel<64>), grid, dim3(kPromptThreads), 0, stream, a);
     else if (a.Dv == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), grid, dim3(kPromptThreads), 0, stream, a);
     else if (a.Dv == 256) hipLaunchKernelGGL((prompt_join_kernel<256>), grid, dim3(kPromptThreads), 0, stream, a);
@@ -267,7 +521,8 @@ static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
 
 template <int DQK, int DV>
 static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
-    hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    if (a.P % 16 == 0) hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, true>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -284,8 +539,9 @@ static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
                               : (p->Dqk == 64 && p->Dv == 64) || (p->Dqk == 128 && p->Dv == 128) || (p->Dqk == 256 && p->Dv == 256) || (p->Dqk == 192 && p->Dv == 128);
     if (!known) return SEER_EUNSUPPORTED;
     const int64_t ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size, G = p->Hq / p->Hkv;
-    // positions are counted in 32 bits, the line of row tiles in 64, rows of the pool in 32
+    // positions are counted in 32 bits, the line of row tiles in 64, rows of the pool and of q in 32
     if (ctx > 0x7fffffffLL - 65536 || static_cast<int64_t>(p->num_pages) * p->page_size * p->Hkv > 0xffffffffLL) return SEER_ESHAPE;
+    if (static_cast<int64_t>(n_tokens) * p->Hq > 0xffffffffLL) return SEER_ESHAPE;
     const double tiles = static_cast<double>(n_tokens) * G / kRowTile + p->B;
     if (tiles * p->Hkv * (static_cast<double>(G) * (ctx + kTileCost) + static_cast<double>(n_tokens) * G + kRowTile) > 4e15) return SEER_ESHAPE;
     return SEER_OK;
@@ -294,6 +550,7 @@ struct PromptLayout {
     int W;
     size_t off_ml, off_acc, total;
 };
+constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 64 ? 3 : (dqk <= 128 ? 2 : 1); }
 static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     PromptLayout w{};
     // no more stretches than the GPU holds at once, nor than the host can see work for
@@ -342,7 +599,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     a.part_acc = reinterpret_cast<float*>(ws + layout.off_acc);
     a.B = p->B, a.Hq = p->Hq, a.Hkv = p->Hkv, a.G = p->Hq / p->Hkv, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq;
     a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W;
-    a.page_shift = (p->page_size & (p->page_size - 1)) == 0 ? __builtin_ctz(static_cast<unsigned>(p->page_size)) : -1;
+    a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.scale_log2 = p->scale * seer::kLog2e;
     a.max_ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);

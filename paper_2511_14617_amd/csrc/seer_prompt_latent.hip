@@ -46,8 +46,11 @@ void prompt_latent_kernel(PromptArgs a) {
         x = moved_cut(plan, ends[0], at[0]);
         x_end = moved_cut(plan, ends[1], at[1]);
         t = ends[0];
+        PromptCut cut{0, 0, 0, 0};                  // the row tile that begins in this stretch and goes on behind it
+        if (x_end > ends[1].begin && x_end < ends[1].begin + ends[1].cost && ends[1].begin >= x && !ends[1].r.bad)
+            cut = PromptCut{ends[1].b, ends[1].kvh, ends[1].i, pieces_of(plan, ends[1], w)};
+        if (tid == 0) a.cuts[w] = cut;
     }
-    PromptCut cut{0, 0, 0, 0};
     bool bad_page = false;
 
     // operand addresses (see the verify kernel)
@@ -67,9 +70,7 @@ void prompt_latent_kernel(PromptArgs a) {
         const unsigned row = c / kChunksPerRow, pos = c - row * kChunksPerRow;
         pat[j] = static_cast<int>(row * kRowBytes + ((pos ^ static_cast<unsigned>(swz(static_cast<int>(row)))) << 4));
     }
-    auto page_of = [&](int64_t tok) __attribute__((always_inline)) -> int {
-        return static_cast<int>(!ANY_PAGE || a.page_shift >= 0 ? tok >> a.page_shift : tok / a.P);
-    };
+    auto page_of = [&](int position) __attribute__((always_inline)) -> int { return prompt_page(a, position); };
 
     while (x < x_end) {
         if (x >= t.begin + t.cost) next_tile(a, t);
@@ -90,7 +91,7 @@ void prompt_latent_kernel(PromptArgs a) {
         const int64_t row = static_cast<int64_t>(t.i) * kRowTile + wave * 32 + ln;
         const bool row_ok = wave * 32 + ln < rows;
         const int token = row_ok ? static_cast<int>(row / a.G) : 0;
-        const size_t q_row = (static_cast<size_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0);
+        const uint32_t q_row = static_cast<uint32_t>((static_cast<int64_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0));
         const int sees = row_ok ? static_cast<int>(t.r.past) + token : -1;
         const int sees_lo = __builtin_amdgcn_readfirstlane(sees), all_see = static_cast<int>(t.r.past) + token_first;
         f32x16 acc[kDTiles];
@@ -99,33 +100,40 @@ void prompt_latent_kernel(PromptArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
         float m_run = kNegInf, l_run = 0.f, alpha = 1.f;
-        bare_barrier();                             // every wave is done with the stages of the piece before
+        __syncthreads();                            // every wave is done with the stages of the piece before
         if (n_tiles > 0) {
+            // Queries through LDS: a wave's 32 rows lie there as a tile does (waves 0 to 2 in the stages, wave 3 in the parked part), so that they are
+            // loaded row by row and read as K operands are (straight from memory, 16 bytes of 32 rows an instruction, 20 000 clocks a row tile).
             u32x4 qreg[kQRegSteps];
             {
-                const u32x4* qp = reinterpret_cast<const u32x4*>(a.q + q_row * kDqk + lg * 8);
-#pragma unroll
-                for (int kk = 0; kk < kQLdsSteps; ++kk) {
-                    u32x4 v = u32x4{0u, 0u, 0u, 0u};
-                    if (row_ok) v = qp[(kQRegSteps + kk) * 2];
-                    q_tail[wave][kk][lane] = v;
+                static_assert(sizeof(q_tail) >= kStageBytes, "");
+                unsigned char* mine = wave < 3 ? lds + wave * kStageBytes : reinterpret_cast<unsigned char*>(q_tail);
+#pragma unroll 4
+                for (int j = 0; j < kBlocks; ++j) {
+                    const int c = j * kWave + lane, r = c / kChunksPerRow, pos = c - r * kChunksPerRow;
+                    const uint32_t from = __shfl(q_row, min(r, max(rows - 1 - wave * 32, 0)), kWave);      // (behind the last row: again that one)
+                    const unsigned char* src = reinterpret_cast<const unsigned char*>(a.q) + static_cast<size_t>(from) * kRowBytes + ((pos ^ swz(r)) << 4);
+                    __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(mine + j * 1024), 16, 0, 0);
                 }
-                u32x4 qv[kQRegSteps];
+                wait_vmcnt<0>();
+                __builtin_amdgcn_wave_barrier();
+                u32x4 tail[kQLdsSteps];
 #pragma unroll
-                for (int kk = 0; kk < kQRegSteps; ++kk) {
-                    qv[kk] = u32x4{0u, 0u, 0u, 0u};
-                    if (row_ok) qv[kk] = qp[kk * 2];
+                for (int kk = 0; kk < kKSteps; ++kk) {
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(mine + k_rd[kk & 3] + (kk >> 2) * 128);
+                    if (kk < kQRegSteps) qreg[kk < kQRegSteps ? kk : 0] = v;
+                    else tail[kk >= kQRegSteps ? kk - kQRegSteps : 0] = v;
                 }
+                __syncthreads();                    // every wave has its queries
 #pragma unroll
-                for (int kk = 0; kk < kQRegSteps; ++kk) {   // pin the arrival of these loads before the tile loop
-                    asm volatile("" : "+v"(qv[kk]));
-                    qreg[kk] = qv[kk];
-                }
+                for (int kk = 0; kk < kQLdsSteps; ++kk) q_tail[wave][kk][lane] = tail[kk];
+#pragma unroll
+                for (int kk = 0; kk < kQRegSteps; ++kk) asm volatile("" : "+v"(qreg[kk]));
             }
 
             // ---- page ids, 64 at a time -------------------------------------------------------------------
             const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
-            const int last_page = page_of(t.r.past + t.r.n - 1);
+            const int last_page = page_of(static_cast<int>(t.r.past) + t.r.n - 1);
             int win = -0x40000000, pg_win = 0;
             auto set_window = [&](int first) __attribute__((always_inline)) {
                 win = first;
@@ -136,12 +144,12 @@ void prompt_latent_kernel(PromptArgs a) {
                 }
                 pg_win = pg;
             };
-            // loads through a descriptor of the tile, which lies in one page (see the verify kernel)
+            // loads through a descriptor of the tile, which lies in one page where pages hold a multiple of a tile (see the verify kernel)
             auto tile_rsrc = [&](int tile) __attribute__((always_inline)) {
-                const int tb = tok_begin + tile * kTile, lp = tb >> a.page_shift;
+                const int tb = tok_begin + tile * kTile, lp = page_of(tb);
                 if (lp < win || lp >= win + kWave) set_window(lp);
                 const int pg = __builtin_amdgcn_readlane(pg_win, __builtin_amdgcn_readfirstlane(lp - win));
-                const unsigned char* src = a.k_pages + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (tb & (a.P - 1))) * kRowBytes;
+                const unsigned char* src = a.k_pages + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (tb - lp * a.P)) * kRowBytes;
                 return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(src), 0, kStageBytes, 0x00020000);
             };
             auto issue_load = [&](auto ic, __amdgpu_buffer_rsrc_t rsrc, int stage_off) __attribute__((always_inline)) {
@@ -153,12 +161,11 @@ void prompt_latent_kernel(PromptArgs a) {
             };
             // ... and through the row of every position
             auto issue_rows = [&](int tile, int stage_off) __attribute__((always_inline)) {
-                const int64_t tb = tok_begin + static_cast<int64_t>(tile) * kTile;
+                const int tb = tok_begin + tile * kTile;
                 if (page_of(tb) < win || page_of(tb + kTile - 1) >= win + kWave) set_window(page_of(tb));
-                const int64_t tok = tb + ln;
-                const int lp = page_of(tok);
+                const int tok = tb + ln, lp = page_of(tok);
                 const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
-                const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - static_cast<int64_t>(lp) * a.P);
+                const uint32_t row_idx = (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - lp * a.P);
                 for (int j = 0; j < kLoadsPerWave; ++j) {
                     const int block = j * kWaves + wave, c = block * kWave + lane, r = c / kChunksPerRow, pos = c - r * kChunksPerRow;
                     const uint32_t from = __builtin_amdgcn_ds_bpermute(r << 2, row_idx);
@@ -365,36 +372,42 @@ void prompt_latent_kernel(PromptArgs a) {
         const float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
         if (begins && (ends || t.r.bad)) {
             const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;          // (a row of nothing but -inf: zeros)
-            if (row_ok) {
-                uint16_t* o = a.out + q_row * kDv + lg * 4;
-#pragma unroll
-                for (int dt = 0; dt < kDTiles; ++dt)
-#pragma unroll
-                    for (int i4 = 0; i4 < 4; ++i4)
-                        *reinterpret_cast<u32x2*>(o + dt * 32 + i4 * 8) = u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv),
-                                                                               cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
-            }
-            continue;
-        }
-        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
-        if (begins) cut = PromptCut{t.b, t.kvh, t.i, pieces_of(plan, t, w)};
-        if (row_ok) {
-            const size_t prow = slot * kRowTile + wave * 32 + ln;
-            if (lg == 0) a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
-            float* po = a.part_acc + prow * kDv + lg * 4;
+            // through LDS, so that a store takes a whole row: 16-byte chunk c of row r at c ^ (r mod 16)
+            static_assert(32 * kDv * 2 <= kStageBytes, "");
+            unsigned char* mine = wave < 3 ? lds + wave * kStageBytes : reinterpret_cast<unsigned char*>(q_tail);
+            __syncthreads();                        // every wave is done with the stages
 #pragma unroll
             for (int dt = 0; dt < kDTiles; ++dt)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<f32x4*>(po + dt * 32 + i4 * 8) = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
+                    *reinterpret_cast<u32x2*>(mine + ln * (kDv * 2) + (((dt * 4 + i4) ^ (ln & 15)) << 4) + lg * 8) =
+                        u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv), cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll 4
+            for (int r = 0; r < min(rows - wave * 32, 32); ++r) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kDv * 2) + ((lane ^ (r & 15)) << 4));
+                const uint32_t to = __builtin_amdgcn_readlane(q_row, r);
+                *reinterpret_cast<u32x4*>(a.out + static_cast<size_t>(to) * kDv + lane * 8) = v;
+            }
+            continue;
         }
+        // a lane's registers as they are, so that a store takes 1 KB (see the joining kernel)
+        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
+        if (lg == 0) {
+            const size_t prow = slot * kRowTile + wave * 32 + ln;
+            a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
+        }
+        f32x4* po = reinterpret_cast<f32x4*>(a.part_acc) + (slot * 4 + wave) * (kDTiles * 4 * kWave) + lane;
+#pragma unroll
+        for (int dt = 0; dt < kDTiles; ++dt)
+#pragma unroll
+            for (int i4 = 0; i4 < 4; ++i4) po[(dt * 4 + i4) * kWave] = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
     }
-    if (tid == 0) a.cuts[w] = cut;
     if (a.status && __any(bad_page) && lane == 0) atomicOr(a.status, 2);
 }
 
 hipError_t launch_prompt_latent(const PromptArgs& a, hipStream_t stream) {
-    if (a.page_shift >= 0 && a.P >= mla::kMinPage) hipLaunchKernelGGL((prompt_latent_kernel<false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    if (a.P % mla::kTile == 0) hipLaunchKernelGGL((prompt_latent_kernel<false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     else hipLaunchKernelGGL((prompt_latent_kernel<true>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
