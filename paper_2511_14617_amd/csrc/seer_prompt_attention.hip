@@ -46,6 +46,8 @@ struct PromptShape {
                  "ds_read_b64_tr_b16 %1, %2 offset:%4"                \
                  : "=&v"(dst[0]), "=&v"(dst[1])                       \
                  : "v"(addr), "n"(OFF_LO), "n"(OFF_HI))
+// Keeps the computation of x where it is written: it would be moved behind the next branch, out of the shadow of the MFMAs.
+#define SEER_PROMPT_PIN(x) asm volatile("" : "+v"(x))
 template <int N>
 __device__ __forceinline__ void wait_reads() {
     static_assert(N >= 0 && N < 16, "lgkmcnt is a 4-bit counter");
@@ -122,6 +124,7 @@ void prompt_tile_kernel(PromptArgs a) {
         if (tid == 0) a.cuts[w] = cut;
     }
     bool bad_page = false;
+    int win_b = -1, win = 0, pg_win = 0;            // window of page ids: request, first logical page; lane l holds the (clamped) id of page win + l
     const int lds0 = tile::lds_addr(lds);
     auto page_of = [&](int position) __attribute__((always_inline)) -> int { return prompt_page(a, position); };
 
@@ -187,15 +190,11 @@ void prompt_tile_kernel(PromptArgs a) {
             // ---- tile loads --------------------------------------------------------------------------------
             const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
             const int last_page = page_of(static_cast<int>(t.r.past) + t.r.n - 1);
-            int win = -0x40000000, pg_win = 0;      // lane l holds the (clamped) page id of logical page win + l
             auto set_window = [&](int first) __attribute__((always_inline)) {
                 win = first;
                 int pg = table[min(first + lane, a.max_pages - 1)];
-                if (pg < 0 || pg >= a.num_pages) {
-                    if (first + lane <= last_page) bad_page = true;
-                    pg = min(max(pg, 0), a.num_pages - 1);
-                }
-                pg_win = pg;
+                if ((pg < 0 || pg >= a.num_pages) && first + lane <= last_page) bad_page = true;
+                pg_win = min(max(pg, 0), a.num_pages - 1);
             };
             // Row of the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU) of tile u's position 8 wave; ANY_PAGE: of position ln.
             // Tiles are asked for in ascending order.
@@ -221,25 +220,41 @@ void prompt_tile_kernel(PromptArgs a) {
             };
 
             // ---- softmax ------------------------------------------------------------------------------------
-            f32x16 s_a, s_b;
+            f32x16 s_a, s_b = {};
             uint32_t pk[8];
             float m_use = 0.f, alpha = 1.f;
             // The exponent reference for tile u's scores; it moves only when a maximum exceeds it by more than 8 (in units of log2 e: probabilities stay
             // below 2^8, which bf16 and fp32 hold as well as any), so that outputs are seldom rescaled.
-            auto reference = [&](auto maskc, int u, f32x16& s) __attribute__((always_inline)) {
-                const int tb = tok_begin + u * kTile;
-                if (decltype(maskc)::value && tb + kTile - 1 > sees_lo) {            // (wave-uniform)
-                    const int lim = sees - tb;      // last position of the tile that the row sees
-                    uint32_t vis = lim < 0 ? 0u : (lim >= 31 ? 0xffffffffu : (2u << lim) - 1u);
-                    vis >>= lg * 4;
+            float mx = 0.f;
+            auto reference = [&](auto partc, const f32x16& s) __attribute__((always_inline)) {
+                constexpr int part = decltype(partc)::value;
+                if constexpr (part == 0) {
+                    mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (!((vis >> ((i >> 2) * 8 + (i & 3))) & 1u)) s[i] = kNegInf;
+                    for (int i = 3; i < 9; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
+                } else if constexpr (part == 1) {
+#pragma unroll
+                    for (int i = 9; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
+                    mx = fmaxf(mx, s[15]);
+                } else if constexpr (part == 2) {
+                    mx = max_across_halves(mx) * a.scale_log2;
+                } else {
+                    const float m_new = mx > m_run + 8.f ? mx : m_run;
+                    m_use = m_new == kNegInf ? 0.f : m_new;            // nothing visible yet: keep exp2 finite
+                    alpha = fast_exp2(m_run - m_use);
+                    m_run = m_new;
                 }
-                float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+            };
+            // -inf into the scores of tile u that this lane's row does not see
+            auto mask = [&](int u, f32x16& s) __attribute__((always_inline)) {
+                const int tb = tok_begin + u * kTile;
+                if (tb + kTile - 1 <= sees_lo) return;                 // (wave-uniform)
+                const int lim = sees - tb;          // last position of the tile that the row sees
+                uint32_t vis = lim < 0 ? 0u : (lim >= 31 ? 0xffffffffu : (2u << lim) - 1u);
+                vis >>= lg * 4;
 #pragma unroll
-                for (int i = 3; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
-                m_use = move_reference(fmaxf(mx, s[15]), a.scale_log2, m_run, alpha);
+                for (int i = 0; i < 16; ++i)
+                    if (!((vis >> ((i >> 2) * 8 + (i & 3))) & 1u)) s[i] = kNegInf;
             };
             float psum = 0.f, p_even = 0.f;
             auto probability = [&](auto ic, const f32x16& s) __attribute__((always_inline)) {
@@ -247,9 +262,14 @@ void prompt_tile_kernel(PromptArgs a) {
                 const float p = fast_exp2(fmaf(s[i], a.scale_log2, -m_use));
                 if constexpr (i % 2 == 0) {
                     p_even = p;
+                    SEER_PROMPT_PIN(p_even);
+                    if constexpr (i >= 2) {         // the sum of what the product will see, one pair behind
+                        psum = add_bf16_pair(pk[(i >> 1) - 1], psum);
+                        SEER_PROMPT_PIN(psum);
+                    }
                 } else {
                     pk[i >> 1] = cvt_pk_bf16(p_even, p);
-                    psum = add_bf16_pair(pk[i >> 1], psum);          // (what the product will see)
+                    SEER_PROMPT_PIN(pk[i >> 1]);
                 }
             };
 
@@ -341,7 +361,7 @@ void prompt_tile_kernel(PromptArgs a) {
             // u - 1; EDGE, MASK: that some rows do not see all of tile u - 1, of tile u.
             auto step = [&](auto slotc, auto beforec, auto prevc, auto edgec, auto maskc, int u, int k_shift, int v_shift, f32x16& s_new, const f32x16& s_old) __attribute__((always_inline)) {
                 constexpr int SLOT = decltype(slotc)::value;
-                constexpr bool PREV = decltype(prevc)::value, EDGE = decltype(edgec)::value;
+                constexpr bool PREV = decltype(prevc)::value, EDGE = decltype(edgec)::value, MASK = decltype(maskc)::value;
                 u32x4 kr[S::kKAhead];
                 each_index([&](auto kc) __attribute__((always_inline)) {
                     constexpr int kk = decltype(kc)::value;
@@ -379,16 +399,25 @@ void prompt_tile_kernel(PromptArgs a) {
                     __builtin_amdgcn_sched_barrier(0);
                 }, std::make_integer_sequence<int, S::kKSteps>{});
                 if constexpr (PREV) {
-                    l_run = l_run * alpha + psum;
+                    l_run = l_run * alpha + add_bf16_pair(pk[7], psum);
                     rescale();
                     __builtin_amdgcn_sched_barrier(0);
-                    product(beforec, v_shift, [](auto) {});
+                    product(beforec, v_shift, [&](auto mc) __attribute__((always_inline)) {
+                        // (the scores' last MFMA is two MFMAs back)
+                        constexpr int part = decltype(mc)::value - (S::kPv >= 8 ? 2 : 0);
+                        if constexpr (!MASK && part >= 0 && part < 4) reference(I<part>{}, s_new);
+                    });
                     if constexpr (EDGE) add_left(u - 1);
                 }
-                reference(maskc, u, s_new);
+                if constexpr (MASK) mask(u, s_new);
+                if constexpr (MASK || !PREV) each_index([&](auto ic) __attribute__((always_inline)) { reference(ic, s_new); }, std::make_integer_sequence<int, 4>{});
             };
 
             // the first tiles: K of 0, 1, 2 and V of 0, 1, in the order in which steps -3, -2, -1 would request them
+            if (t.b != win_b) {                     // (else the window may do: row tiles and KV heads of a request often begin with the one before's)
+                win_b = t.b;
+                set_window(page_of(tok_begin));
+            }
             {
                 const uint32_t row0 = tile_row(0);
                 uint32_t row1 = 0;
@@ -430,7 +459,7 @@ void prompt_tile_kernel(PromptArgs a) {
             __builtin_amdgcn_sched_barrier(0);
             psum = 0.f;
             each_index([&](auto ec) __attribute__((always_inline)) { probability(ec, s_a); }, std::make_integer_sequence<int, 16>{});
-            l_run = l_run * alpha + psum;
+            l_run = l_run * alpha + add_bf16_pair(pk[7], psum);
             rescale();
             __builtin_amdgcn_sched_barrier(0);
             product(I<0>{}, shift, [](auto) {});
@@ -444,18 +473,21 @@ void prompt_tile_kernel(PromptArgs a) {
             // through LDS, so that a store takes whole rows: 16-byte chunk c of row r at c ^ r (its low bits)
             constexpr int kChunks = DV / 8, kPerStore = kWave / (kChunks < kWave ? kChunks : kWave);      // rows of a store
             static_assert(4 * 32 * DV * 2 <= S::kLds, "");
+            int l = lane;
+            asm volatile("" : "+v"(l));             // (the addresses below are made here, not kept in registers through the tiles)
+            const int row_l = l & 31;
             unsigned char* mine = lds + wave * (32 * DV * 2);
             __syncthreads();                        // every wave is done with the rings
 #pragma unroll
             for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<u32x2*>(mine + ln * (DV * 2) + (((dt * 4 + i4) ^ (ln & (kChunks - 1) & 15)) << 4) + lg * 8) =
+                    *reinterpret_cast<u32x2*>(mine + row_l * (DV * 2) + (((dt * 4 + i4) ^ (row_l & (kChunks - 1) & 15)) << 4) + (l >> 5) * 8) =
                         u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv), cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
             for (int j = 0; j < 32 / kPerStore; ++j) {
-                const int r = j * kPerStore + lane / kChunks, c = lane % kChunks;
+                const int r = j * kPerStore + l / kChunks, c = l % kChunks;
                 const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (DV * 2) + ((c ^ (r & (kChunks - 1) & 15)) << 4));
                 const uint32_t to = __shfl(q_row, r, kWave);
                 if (wave * 32 + r < rows) *reinterpret_cast<u32x4*>(a.out + static_cast<size_t>(to) * DV + c * 8) = v;
