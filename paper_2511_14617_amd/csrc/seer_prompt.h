@@ -42,16 +42,22 @@ struct PromptArgs {
     float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
     int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
     int W;
-    uint32_t inv_p;        // 2^32 / P, at most 2^32 - 1
+    uint32_t inv_p, inv_g; // 2^32 / P and 2^32 / G, at most 2^32 - 1
     float scale_log2;
     int64_t max_ctx;
 };
 
+// x / d from inv = 2^32 / d rounded down (d = 1: 2^32 - 1): the product's upper half is the quotient or one less.
+__device__ __forceinline__ uint32_t quotient(uint32_t x, uint32_t d, uint32_t inv) {
+    const uint32_t q = __umulhi(x, inv);
+    return q + ((d - 1u - (x - q * d)) >> 31);         // (rests of 2 d and more do not occur, so the sign says it)
+}
 // Page of a position.
 __device__ __forceinline__ int prompt_page(const PromptArgs& a, int position) {
-    const uint32_t x = static_cast<uint32_t>(position), q = __umulhi(x, a.inv_p);          // the quotient, or one less
-    return static_cast<int>(q + (x - q * static_cast<uint32_t>(a.P) >= static_cast<uint32_t>(a.P) ? 1u : 0u));
+    return static_cast<int>(quotient(static_cast<uint32_t>(position), static_cast<uint32_t>(a.P), a.inv_p));
 }
+// Token of a query row of a request.
+__device__ __forceinline__ int prompt_token(const PromptArgs& a, uint32_t row) { return static_cast<int>(quotient(row, static_cast<uint32_t>(a.G), a.inv_g)); }
 
 // A request as the line counts it.
 struct PromptRequest {

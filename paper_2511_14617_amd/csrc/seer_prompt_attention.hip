@@ -79,7 +79,7 @@ __device__ __forceinline__ void issue_rows(const unsigned char* pool, uint32_t a
             __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(slot + (wave * LOADS + j) * 1024), 16, 0, 0);
         }
     } else {
-        const __amdgpu_buffer_rsrc_t rsrc = rows_at(pool + static_cast<size_t>(at_row) * ROW, 8 * ROW);
+        const __amdgpu_buffer_rsrc_t rsrc = rows_at(pool + static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(at_row))) * ROW, 8 * ROW);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) load_to_lds(rsrc, slot + (wave * LOADS + j) * 1024, pat[j]);
     }
@@ -150,24 +150,26 @@ void prompt_tile_kernel(PromptArgs a) {
         if (x >= t.begin + t.cost) next_tile(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
-        const int rows = static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile)));
-        const int token_first = static_cast<int>(static_cast<int64_t>(t.i) * kRowTile / a.G);                      // of the request's new tokens
-        const int token_last = static_cast<int>((static_cast<int64_t>(t.i) * kRowTile + rows - 1) / a.G);
+        // (rows of q are counted in 32 bits)
+        const uint32_t row0 = static_cast<uint32_t>(t.i) * kRowTile;
+        const int rows = static_cast<int>(min(static_cast<uint32_t>(t.r.n) * static_cast<uint32_t>(a.G) - row0, static_cast<uint32_t>(kRowTile)));
+        const int token_first = prompt_token(a, row0), token_last = prompt_token(a, row0 + rows - 1);              // of the request's new tokens
         const int seen = static_cast<int>(t.r.past) + token_last + 1;                                              // positions that the last row sees
         const int all_see = static_cast<int>(t.r.past) + token_first;                                              // the last one that all rows see
         const int tiles = t.r.bad ? 0 : (seen + kTile - 1) / kTile;
         // the piece's tiles (the same rounding on both sides of a cut)
-        const int u0 = begins ? 0 : static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
-        const int u1 = ends ? tiles : static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
+        int u0 = 0, u1 = tiles;
+        if (!begins) u0 = static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
+        if (!ends) u1 = static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
         x = end;
         if (t.r.bad && !begins) continue;
         const int n_tiles = u1 - u0, tok_begin = u0 * kTile;
 
         // ---- this lane's query row -------------------------------------------------------------------------
-        const int64_t row = static_cast<int64_t>(t.i) * kRowTile + wave * 32 + ln;
+        const uint32_t row = row0 + wave * 32 + ln;
         const bool row_ok = wave * 32 + ln < rows;
-        const int token = row_ok ? static_cast<int>(row / a.G) : 0;
-        const uint32_t q_row = static_cast<uint32_t>((static_cast<int64_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0));
+        const int token = row_ok ? prompt_token(a, row) : 0;
+        const uint32_t q_row = static_cast<uint32_t>(t.r.first + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<uint32_t>(token) * a.G : 0u);
         const int sees = row_ok ? static_cast<int>(t.r.past) + token : -1;                                         // last position that it sees
         const int sees_lo = __builtin_amdgcn_readfirstlane(sees);                                                  // the wave's first row
         f32x16 acc[S::kDTiles];
@@ -209,7 +211,8 @@ void prompt_tile_kernel(PromptArgs a) {
                     const int tok = tb + wave * 8, lp = page_of(tok);
                     if (lp < win || lp >= win + kWave) set_window(lp);
                     const uint32_t pg = __builtin_amdgcn_readlane(pg_win, __builtin_amdgcn_readfirstlane(lp - win));
-                    return (pg * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - lp * a.P);
+                    // (said to be uniform: a descriptor that may differ from lane to lane is taken apart lane by lane)
+                    return __builtin_amdgcn_readfirstlane((pg * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - lp * a.P));
                 }
             };
             auto issue_k = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
@@ -297,39 +300,40 @@ void prompt_tile_kernel(PromptArgs a) {
             // ---- step u: scores of tile u beside the probabilities of tile u - 1, then the product with V of tile u - 1 beside the loads and
             // the reference of tile u ----------------------------------------------------------------------------------------------------
             uint32_t row2 = 0;                      // row of tile u + 2: its K was requested in the step before
-            auto top = [&](int u) __attribute__((always_inline)) {
+            // (SURE: u + 2 < n_tiles, and for the loads u + 3 < n_tiles)
+            auto top = [&](auto surec, int u) __attribute__((always_inline)) {
                 constexpr int K = S::kKLoads, V = S::kVLoads;        // loads that may be in flight behind those of K of tile u and V of tile u - 1
-                if (u + 2 < n_tiles) wait_vmcnt<2 * K + 2 * V>();
+                if (decltype(surec)::value || u + 2 < n_tiles) wait_vmcnt<2 * K + 2 * V>();
                 else if (u + 1 < n_tiles) wait_vmcnt<K + 2 * V>();
                 else if (u < n_tiles) wait_vmcnt<V>();
                 else wait_vmcnt<0>();
                 bare_barrier();                     // they have landed for every wave, every wave is done with step u - 1
             };
-            auto loads = [&](int u) __attribute__((always_inline)) {
+            auto loads = [&](auto surec, int u) __attribute__((always_inline)) {
                 uint32_t row3 = 0;
-                if (u + 3 < n_tiles) {
+                if (decltype(surec)::value || u + 3 < n_tiles) {
                     row3 = tile_row(u + 3);
                     issue_k(u + 3, row3);
                 }
-                if (u + 2 < n_tiles) issue_v(u + 2, row2);
+                if (decltype(surec)::value || u + 2 < n_tiles) issue_v(u + 2, row2);
                 row2 = row3;
             };
             u32x2 vr[S::kVAhead][2];
-            // V operand m of a product (d-tile m / 2, positions of half m % 2) into its ring slot
+            // V operand m of a product (positions of half m / kDTiles, d-tile m % kDTiles) into its ring slot
             auto read_v = [&](auto mc, auto slotc, int shift) __attribute__((always_inline)) {
-                constexpr int m = decltype(mc)::value, dt = m >> 1, half = m & 1;
+                constexpr int m = decltype(mc)::value, dt = m % S::kDTiles, half = m / S::kDTiles;
                 constexpr int off = decltype(slotc)::value * S::kVSlot + dt / O::kPerV * (O::kPerV * 64) + half * 16 * S::kVRow;
                 (void)&vr;
                 const int from = v_at[dt % O::kPerV] + shift;
                 SEER_PROMPT_READ_TR(vr[m % S::kVAhead], from, off, off + 8 * S::kVRow);
             };
             auto product = [&](auto slotc, int shift, auto&& beside) __attribute__((always_inline)) {
-                const bf16x8 p0 = as_bf16x8(u32x4{pk[0], pk[1], pk[2], pk[3]}), p1 = as_bf16x8(u32x4{pk[4], pk[5], pk[6], pk[7]});
                 each_index([&](auto mc) __attribute__((always_inline)) {
                     constexpr int m = decltype(mc)::value, later = S::kPv - 1 - m;
                     wait_reads<2 * (later < S::kVAhead - 1 ? later : S::kVAhead - 1)>();
                     const bf16x8 v = as_bf16x8(u32x4{vr[m % S::kVAhead][0][0], vr[m % S::kVAhead][0][1], vr[m % S::kVAhead][1][0], vr[m % S::kVAhead][1][1]});
-                    acc[m >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, (m & 1) ? p1 : p0, acc[m >> 1], 0, 0, 0);
+                    constexpr int dt = m % S::kDTiles, h = m / S::kDTiles * 4;
+                    acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, as_bf16x8(u32x4{pk[h], pk[h + 1], pk[h + 2], pk[h + 3]}), acc[dt], 0, 0, 0);
                     __builtin_amdgcn_sched_barrier(0);
                     if constexpr (m + S::kVAhead < S::kPv) read_v(std::integral_constant<int, m + S::kVAhead>{}, slotc, shift);
                     beside(mc);
@@ -359,8 +363,8 @@ void prompt_tile_kernel(PromptArgs a) {
             };
             // The step itself, behind top(): K of tile u in slot SLOT (+ k_shift), V of tile u - 1 in slot BEFORE (+ v_shift).  PREV: there is a tile
             // u - 1; EDGE, MASK: that some rows do not see all of tile u - 1, of tile u.
-            auto step = [&](auto slotc, auto beforec, auto prevc, auto edgec, auto maskc, int u, int k_shift, int v_shift, f32x16& s_new, const f32x16& s_old) __attribute__((always_inline)) {
-                constexpr int SLOT = decltype(slotc)::value;
+            auto step = [&](auto slotc, auto beforec, auto prevc, auto edgec, auto maskc, auto surec, int u, int k_shift, int v_shift, f32x16& s_new, const f32x16& s_old) __attribute__((always_inline)) {
+                constexpr int SLOT = decltype(slotc)::value, kEarly = 10;          // probabilities beside the scores' MFMAs
                 constexpr bool PREV = decltype(prevc)::value, EDGE = decltype(edgec)::value, MASK = decltype(maskc)::value;
                 u32x4 kr[S::kKAhead];
                 each_index([&](auto kc) __attribute__((always_inline)) {
@@ -370,7 +374,7 @@ void prompt_tile_kernel(PromptArgs a) {
                     SEER_PROMPT_READ128(kr[kk], from, SLOT * S::kKSlot + kk / O::kPerXor * (O::kPerXor * 32));
                 }, std::make_integer_sequence<int, S::kKAhead>{});
                 __builtin_amdgcn_sched_barrier(0);
-                loads(u);
+                loads(surec, u);
                 __builtin_amdgcn_sched_barrier(0);
                 psum = 0.f;
 #pragma unroll
@@ -392,20 +396,29 @@ void prompt_tile_kernel(PromptArgs a) {
                     }
                     if constexpr (PREV && kk >= kVFirst) read_v(std::integral_constant<int, kk - kVFirst>{}, beforec, v_shift);
                     if constexpr (PREV) {
-                        constexpr int e0 = 16 * kk / S::kKSteps, e1 = 16 * (kk + 1) / S::kKSteps;
+                        constexpr int e0 = kEarly * kk / S::kKSteps, e1 = kEarly * (kk + 1) / S::kKSteps;
                         each_index([&](auto ec) __attribute__((always_inline)) { probability(std::integral_constant<int, e0 + decltype(ec)::value>{}, s_old); },
                                    std::make_integer_sequence<int, e1 - e0>{});
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }, std::make_integer_sequence<int, S::kKSteps>{});
                 if constexpr (PREV) {
-                    l_run = l_run * alpha + add_bf16_pair(pk[7], psum);
+                    l_run *= alpha;
                     rescale();
                     __builtin_amdgcn_sched_barrier(0);
                     product(beforec, v_shift, [&](auto mc) __attribute__((always_inline)) {
-                        // (the scores' last MFMA is two MFMAs back)
-                        constexpr int part = decltype(mc)::value - (S::kPv >= 8 ? 2 : 0);
-                        if constexpr (!MASK && part >= 0 && part < 4) reference(I<part>{}, s_new);
+                        // beside the first half the other probabilities, which the second half takes; beside that the reference of tile u
+                        constexpr int m = decltype(mc)::value, kHalf = S::kDTiles;
+                        if constexpr (m < kHalf) {
+                            constexpr int e0 = kEarly + (16 - kEarly) * m / kHalf, e1 = kEarly + (16 - kEarly) * (m + 1) / kHalf;
+                            each_index([&](auto ec) __attribute__((always_inline)) { probability(I<e0 + decltype(ec)::value>{}, s_old); },
+                                       std::make_integer_sequence<int, e1 - e0>{});
+                        }
+                        if constexpr (m == kHalf) l_run = add_bf16_pair(pk[7], psum) + l_run;
+                        constexpr int r0 = m < kHalf ? 0 : 4 * (m - kHalf) / kHalf, r1 = m < kHalf ? 0 : 4 * (m + 1 - kHalf) / kHalf;
+                        if constexpr (!MASK && r1 > r0)
+                            each_index([&](auto rc) __attribute__((always_inline)) { reference(I<r0 + decltype(rc)::value>{}, s_new); },
+                                       std::make_integer_sequence<int, r1 - r0>{});
                     });
                     if constexpr (EDGE) add_left(u - 1);
                 }
@@ -429,30 +442,30 @@ void prompt_tile_kernel(PromptArgs a) {
             }
             using yes = std::true_type;
             using no = std::false_type;
-            top(0);
-            step(I<0>{}, I<0>{}, no{}, no{}, yes{}, 0, 0, 0, s_a, s_b);
-            // tiles that every row sees whole, slots at fixed places; then the others
-            const int whole = min(n_tiles, (all_see + 1 - tok_begin) / kTile);      // (below 0: none)
+            top(no{}, 0);
+            step(I<0>{}, I<0>{}, no{}, no{}, yes{}, no{}, 0, 0, 0, s_a, s_b);
+            // tiles that every row sees whole, with the next ones requested in any case, slots at fixed places; then the others
+            const int whole = min(n_tiles - 3, (all_see + 1 - tok_begin) / kTile);      // (below 0: none)
             int u = 1;
             for (; u + 3 < whole; u += 4) {
-                top(u);
-                step(I<1>{}, I<0>{}, yes{}, no{}, no{}, u, 0, 0, s_b, s_a);
-                top(u + 1);
-                step(I<2>{}, I<1>{}, yes{}, no{}, no{}, u + 1, 0, 0, s_a, s_b);
-                top(u + 2);
-                step(I<3>{}, I<2>{}, yes{}, no{}, no{}, u + 2, 0, 0, s_b, s_a);
-                top(u + 3);
-                step(I<0>{}, I<3>{}, yes{}, no{}, no{}, u + 3, 0, 0, s_a, s_b);
+                top(yes{}, u);
+                step(I<1>{}, I<0>{}, yes{}, no{}, no{}, yes{}, u, 0, 0, s_b, s_a);
+                top(yes{}, u + 1);
+                step(I<2>{}, I<1>{}, yes{}, no{}, no{}, yes{}, u + 1, 0, 0, s_a, s_b);
+                top(yes{}, u + 2);
+                step(I<3>{}, I<2>{}, yes{}, no{}, no{}, yes{}, u + 2, 0, 0, s_b, s_a);
+                top(yes{}, u + 3);
+                step(I<0>{}, I<3>{}, yes{}, no{}, no{}, yes{}, u + 3, 0, 0, s_a, s_b);
             }
             for (; u < n_tiles; ++u) {
-                top(u);
+                top(no{}, u);
                 scan(u - 1, ((u - 1) & (kSlots - 1)) * S::kVSlot);
-                step(I<0>{}, I<0>{}, yes{}, yes{}, yes{}, u, (u & (kSlots - 1)) * S::kKSlot, ((u - 1) & (kSlots - 1)) * S::kVSlot, s_b, s_a);
+                step(I<0>{}, I<0>{}, yes{}, yes{}, yes{}, no{}, u, (u & (kSlots - 1)) * S::kKSlot, ((u - 1) & (kSlots - 1)) * S::kVSlot, s_b, s_a);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s_a[i] = s_b[i];
             }
             // the last tile's probabilities and product
-            top(n_tiles);
+            top(no{}, n_tiles);
             const int shift = ((n_tiles - 1) & (kSlots - 1)) * S::kVSlot;
             scan(n_tiles - 1, shift);
             each_index([&](auto mc) __attribute__((always_inline)) { read_v(mc, I<0>{}, shift); }, std::make_integer_sequence<int, S::kVAhead>{});
@@ -630,6 +643,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     a.part_ml = reinterpret_cast<float*>(ws + layout.off_ml);
     a.part_acc = reinterpret_cast<float*>(ws + layout.off_acc);
     a.B = p->B, a.Hq = p->Hq, a.Hkv = p->Hkv, a.G = p->Hq / p->Hkv, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq;
+    a.inv_g = a.G > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(a.G)) : 0xffffffffu;
     a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W;
     a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.scale_log2 = p->scale * seer::kLog2e;

@@ -76,22 +76,24 @@ void prompt_latent_kernel(PromptArgs a) {
         if (x >= t.begin + t.cost) next_tile(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
-        const int rows = static_cast<int>(min(static_cast<int64_t>(t.r.n) * a.G - static_cast<int64_t>(t.i) * kRowTile, static_cast<int64_t>(kRowTile)));
-        const int token_first = static_cast<int>(static_cast<int64_t>(t.i) * kRowTile / a.G);
-        const int token_last = static_cast<int>((static_cast<int64_t>(t.i) * kRowTile + rows - 1) / a.G);
+        // (rows of q are counted in 32 bits)
+        const uint32_t row0 = static_cast<uint32_t>(t.i) * kRowTile;
+        const int rows = static_cast<int>(min(static_cast<uint32_t>(t.r.n) * static_cast<uint32_t>(a.G) - row0, static_cast<uint32_t>(kRowTile)));
+        const int token_first = prompt_token(a, row0), token_last = prompt_token(a, row0 + rows - 1);              // of the request's new tokens
         const int seen = static_cast<int>(t.r.past) + token_last + 1;
         const int tiles = t.r.bad ? 0 : (seen + kTile - 1) / kTile;
-        const int u0 = begins ? 0 : static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
-        const int u1 = ends ? tiles : static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
+        int u0 = 0, u1 = tiles;
+        if (!begins) u0 = static_cast<int>(static_cast<double>(x - t.begin) * tiles / static_cast<double>(t.cost));
+        if (!ends) u1 = static_cast<int>(static_cast<double>(end - t.begin) * tiles / static_cast<double>(t.cost));
         x = end;
         if (t.r.bad && !begins) continue;
         const int n_tiles = u1 - u0, tok_begin = u0 * kTile;
 
         // ---- this lane's query row -------------------------------------------------------------------------
-        const int64_t row = static_cast<int64_t>(t.i) * kRowTile + wave * 32 + ln;
+        const uint32_t row = row0 + wave * 32 + ln;
         const bool row_ok = wave * 32 + ln < rows;
-        const int token = row_ok ? static_cast<int>(row / a.G) : 0;
-        const uint32_t q_row = static_cast<uint32_t>((static_cast<int64_t>(t.r.first) + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<int64_t>(token) * a.G : 0));
+        const int token = row_ok ? prompt_token(a, row) : 0;
+        const uint32_t q_row = static_cast<uint32_t>(t.r.first + token) * a.Hq + t.kvh * a.G + (row_ok ? row - static_cast<uint32_t>(token) * a.G : 0u);
         const int sees = row_ok ? static_cast<int>(t.r.past) + token : -1;
         const int sees_lo = __builtin_amdgcn_readfirstlane(sees), all_see = static_cast<int>(t.r.past) + token_first;
         f32x16 acc[kDTiles];
