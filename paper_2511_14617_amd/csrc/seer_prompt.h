@@ -3,7 +3,7 @@
 // Rows: a request's n tokens times the G heads that share a KV head are n G consecutive query rows (row r = token r / G, head r % G), cut into
 // row tiles of kRowTile.  A row tile reads the positions that its last row sees, so its cost grows along a prompt: with past = ctx - n
 // cached positions before the new ones, row tile i of a request costs (in units of a position times a head of the group)
-//     c_i = G past + kRowTile (i + 1) + kTileCost,     i < R = ceil(n G / kRowTile).
+//     c_i = G (past + tile_cost) + kRowTile (i + 1),     i < R = ceil(n G / kRowTile).
 // All row tiles -- requests in order, their KV heads in order, their row tiles in order -- lie end to end on one line, whose
 // prefix sums have closed forms in i and in the KV head, and whose sums over requests are one scan.  Workgroup w of W takes the stretch from
 // x_w = total w / W to x_(w+1): equal work whatever the mix of lengths, one launch, no queue.
@@ -20,7 +20,6 @@ namespace seer {
 
 constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves
 constexpr int kPromptThreads = 256;
-constexpr int kTileCost = 64;          // of a row tile beside its positions (queries, output), per head of the group
 constexpr int kMinStretch = 256;       // positions per head of the group
 
 // The pieces that end a stretch inside a row tile: the row tile, and in how many stretches it lies (0: none begins here and goes on).
@@ -42,6 +41,7 @@ struct PromptArgs {
     float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
     int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
     int W;
+    int tile_cost;         // what a row tile costs beside its positions, in positions
     uint32_t inv_p, inv_g; // 2^32 / P and 2^32 / G, at most 2^32 - 1
     float scale_log2;
     int64_t max_ctx;
@@ -89,9 +89,9 @@ __device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int
 }
 // Cost of the first i row tiles of a KV head, and of row tile i.
 __device__ __forceinline__ int64_t tiles_before(const PromptArgs& a, int64_t past, int64_t i) {
-    return i * (a.G * (past + kTileCost)) + kRowTile / 2 * (i * (i + 1));
+    return i * (a.G * (past + a.tile_cost)) + kRowTile / 2 * (i * (i + 1));
 }
-__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + kTileCost) + kRowTile * (i + 1); }
+__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + kRowTile * (i + 1); }
 
 struct PromptLds {
     int64_t sums[2][kPromptThreads / kWave];
@@ -164,7 +164,6 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
     p.W = static_cast<int>(most < a.W ? most : a.W);
     p.snap = least / 2;
     if (w >= p.W) return false;
-    if (p.total / p.W / 16 > p.snap) p.snap = p.total / p.W / 16;
     int ignored = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
@@ -196,7 +195,7 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
         o.kvh = static_cast<int>(d / head);
         const int64_t inside = d - o.kvh * head;
         // the largest i with tiles_before(i) <= inside
-        const double A = static_cast<double>(a.G * (o.r.past + kTileCost) + kRowTile / 2);
+        const double A = static_cast<double>(a.G * (o.r.past + a.tile_cost) + kRowTile / 2);
         int64_t i = static_cast<int64_t>((sqrt(A * A + 2.0 * kRowTile * static_cast<double>(inside)) - A) / kRowTile);
         i = i < 0 ? 0 : (i >= o.r.tiles ? o.r.tiles - 1 : i);
         while (i > 0 && tiles_before(a, o.r.past, i) > inside) --i;

@@ -574,6 +574,8 @@ static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+// What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.
+constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 448); }
 static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (!p) return SEER_EINVAL;
     if (p->B < 0 || n_tokens < 0 || p->Hq < 1 || p->Hkv < 1 || p->page_size < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1) return SEER_EINVAL;
@@ -588,7 +590,7 @@ static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (ctx > 0x7fffffffLL - 65536 || static_cast<int64_t>(p->num_pages) * p->page_size * p->Hkv > 0xffffffffLL) return SEER_ESHAPE;
     if (static_cast<int64_t>(n_tokens) * p->Hq > 0xffffffffLL) return SEER_ESHAPE;
     const double tiles = static_cast<double>(n_tokens) * G / kRowTile + p->B;
-    if (tiles * p->Hkv * (static_cast<double>(G) * (ctx + kTileCost) + static_cast<double>(n_tokens) * G + kRowTile) > 4e15) return SEER_ESHAPE;
+    if (tiles * p->Hkv * (static_cast<double>(G) * (ctx + prompt_tile_cost(p->Dqk)) + static_cast<double>(n_tokens) * G + kRowTile) > 4e15) return SEER_ESHAPE;
     return SEER_OK;
 }
 struct PromptLayout {
@@ -603,7 +605,7 @@ static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     const int64_t ctx = static_cast<int64_t>(p.max_pages_per_seq) * p.page_size, G = p.Hq / p.Hkv;
     const int64_t requests = p.B < n_tokens ? p.B : n_tokens;
     const double row_tiles = (static_cast<double>(n_tokens) * G / kRowTile + requests) * p.Hkv;
-    const double most = row_tiles * (static_cast<double>(ctx + kTileCost + kRowTile) / kMinStretch + 2);
+    const double most = row_tiles * (static_cast<double>(ctx + prompt_tile_cost(p.Dqk) + kRowTile) / kMinStretch + 2);
     if (most < resident) resident = static_cast<int>(most);
     w.W = (resident + 7) / 8 * 8;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -644,7 +646,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     a.part_acc = reinterpret_cast<float*>(ws + layout.off_acc);
     a.B = p->B, a.Hq = p->Hq, a.Hkv = p->Hkv, a.G = p->Hq / p->Hkv, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq;
     a.inv_g = a.G > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(a.G)) : 0xffffffffu;
-    a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W;
+    a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W, a.tile_cost = seer::prompt_tile_cost(p->Dqk);
     a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.scale_log2 = p->scale * seer::kLog2e;
     a.max_ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size;

@@ -110,10 +110,11 @@ void prompt_latent_kernel(PromptArgs a) {
             {
                 static_assert(sizeof(q_tail) >= kStageBytes, "");
                 unsigned char* mine = wave < 3 ? lds + wave * kStageBytes : reinterpret_cast<unsigned char*>(q_tail);
-#pragma unroll 4
+#pragma unroll 6
                 for (int j = 0; j < kBlocks; ++j) {
                     const int c = j * kWave + lane, r = c / kChunksPerRow, pos = c - r * kChunksPerRow;
-                    const uint32_t from = __shfl(q_row, min(r, max(rows - 1 - wave * 32, 0)), kWave);      // (behind the last row: again that one)
+                    const uint32_t of = row0 + min(wave * 32 + r, rows - 1), at = prompt_token(a, of);      // (behind the last row: again that one)
+                    const uint32_t from = static_cast<uint32_t>(t.r.first + at) * a.Hq + t.kvh * a.G + (of - at * a.G);
                     const unsigned char* src = reinterpret_cast<const unsigned char*>(a.q) + static_cast<size_t>(from) * kRowBytes + ((pos ^ swz(r)) << 4);
                     __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(mine + j * 1024), 16, 0, 0);
                 }
@@ -205,6 +206,7 @@ void prompt_latent_kernel(PromptArgs a) {
                     __builtin_amdgcn_s_waitcnt(0xc07f);
                     bare_barrier();
                     uint32_t found = 0;
+#pragma unroll 1
                     for (int c = tid; c < kTile * (kDv / 8); c += kPromptThreads) {
                         const int r = c / (kDv / 8), pos = c - r * (kDv / 8);
                         const u32x4 v = *reinterpret_cast<const u32x4*>(lds + st_cur + r * kRowBytes + ((pos ^ swz(r)) << 4));
@@ -218,6 +220,7 @@ void prompt_latent_kernel(PromptArgs a) {
                     left_cur = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
                 }
                 if (left_prev) {
+#pragma unroll 1
                     for (int c = tid; c < kTile * (kDv / 8); c += kPromptThreads) {
                         const int r = c / (kDv / 8), pos = c - r * (kDv / 8);
                         if ((left_prev >> r) & 1u) *reinterpret_cast<u32x4*>(lds + st_prev + r * kRowBytes + ((pos ^ swz(r)) << 4)) = u32x4{0u, 0u, 0u, 0u};
@@ -374,22 +377,36 @@ void prompt_latent_kernel(PromptArgs a) {
         const float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
         if (begins && (ends || t.r.bad)) {
             const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;          // (a row of nothing but -inf: zeros)
-            // through LDS, so that a store takes a whole row: 16-byte chunk c of row r at c ^ (r mod 16)
-            static_assert(32 * kDv * 2 <= kStageBytes, "");
+            // Through LDS, so that a store takes 512 bytes of a row: the unscaled outputs of 256 components at a time, 16-byte chunk c of row r at
+            // c ^ r; divided and rounded on the way out, in a loop (unrolled over all accumulators that is 6 KB of code for once a row tile, and
+            // its fetch took longer than the work).
+            constexpr int kPart = 256;
+            static_assert(32 * kPart * 4 <= kStageBytes && kDv % kPart == 0, "");
             unsigned char* mine = wave < 3 ? lds + wave * kStageBytes : reinterpret_cast<unsigned char*>(q_tail);
+            int l = lane;
+            asm volatile("" : "+v"(l));             // (the addresses below are made here, not kept in registers through the tiles)
             __syncthreads();                        // every wave is done with the stages
+            const int rows_here = min(rows - wave * 32, 32);
 #pragma unroll
-            for (int dt = 0; dt < kDTiles; ++dt)
+            for (int part = 0; part < kDv / kPart; ++part) {
 #pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4)
-                    *reinterpret_cast<u32x2*>(mine + ln * (kDv * 2) + (((dt * 4 + i4) ^ (ln & 15)) << 4) + lg * 8) =
-                        u32x2{cvt_pk_bf16(acc[dt][i4 * 4] * inv, acc[dt][i4 * 4 + 1] * inv), cvt_pk_bf16(acc[dt][i4 * 4 + 2] * inv, acc[dt][i4 * 4 + 3] * inv)};
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll 4
-            for (int r = 0; r < min(rows - wave * 32, 32); ++r) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * (kDv * 2) + ((lane ^ (r & 15)) << 4));
-                const uint32_t to = __builtin_amdgcn_readlane(q_row, r);
-                *reinterpret_cast<u32x4*>(a.out + static_cast<size_t>(to) * kDv + lane * 8) = v;
+                for (int dt = 0; dt < kPart / 32; ++dt)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const f32x16& o = acc[part * (kPart / 32) + dt];
+                        *reinterpret_cast<f32x4*>(mine + (l & 31) * (kPart * 4) + (((dt * 8 + i4 * 2 + (l >> 5)) ^ (l & 31)) << 4)) =
+                            f32x4{o[i4 * 4], o[i4 * 4 + 1], o[i4 * 4 + 2], o[i4 * 4 + 3]};
+                    }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll 8
+                for (int r = 0; r < rows_here; ++r) {
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * (kPart * 4) + ((l ^ r) << 4));
+                    const uint32_t to = __builtin_amdgcn_readlane(q_row, r);
+                    const float scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(inv), r));
+                    *reinterpret_cast<u32x2*>(a.out + static_cast<size_t>(to) * kDv + part * kPart + l * 4) =
+                        u32x2{cvt_pk_bf16(v[0] * scale, v[1] * scale), cvt_pk_bf16(v[2] * scale, v[3] * scale)};
+                }
+                __builtin_amdgcn_wave_barrier();
             }
             continue;
         }

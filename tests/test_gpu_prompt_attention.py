@@ -188,13 +188,16 @@ def test_what_a_token_does_not_see_does_not_reach_it(heads, value):
 
 @pytest.mark.parametrize("heads", [(8, 2, 128, 128, 16), (4, 4, 64, 64, 20), (8, 1, 256, 256, 32), (16, 2, 192, 128, 64)])
 def test_values_that_are_not_finite_stay_in_their_component(heads):
+    """The other components are held to the outputs without the infinity, within the tolerance above: where a tile has masked positions, a value row
+    that is not finite enters the sums by itself, in another order than by the matrix product (bits may differ where a sum lies by a border of bf16)."""
     c = make(8, [150, 40], [0, 200], *heads, std=0.5)
     good, _ = call(c)
+    want = plain(c)
     for b, j in ((0, 70), (1, 215)):
         spoil(c["v"], b, j, c, float("inf"), 5)
     out, _ = call(c)
-    keep = [d for d in range(c["Dv"]) if d != 5]
-    assert torch.equal(out[..., keep].cpu(), good[..., keep].cpu())
+    keep = torch.tensor([d for d in range(c["Dv"]) if d != 5], device="cuda")
+    compare(out[..., keep], [(t, hq, ref[:, keep], weight[:, keep]) for t, hq, ref, weight in want])
     assert torch.isinf(out[70:150, :, 5].float()).all() and torch.isinf(out[150 + 15:190, :, 5].float()).all()
     assert torch.equal(out[:70, :, 5], good[:70, :, 5])
 
