@@ -7,8 +7,9 @@
 // All row tiles -- requests in order, their KV heads in order, their row tiles in order -- lie end to end on one line, whose
 // prefix sums have closed forms in i and in the KV head, and whose sums over requests are one scan.  Workgroup w of W takes the stretch from
 // x_w = total w / W to x_(w+1): equal work whatever the mix of lengths, one launch, no queue.
-// A cut inside a row tile costs two partial results and their joining; a cut that comes within `snap` of a row tile's end is moved
-// there.  Stretches are at least 2 `snap` long, so short row tiles are never cut, and calls with little to do use fewer workgroups.
+// A cut inside a row tile costs two partial results and their joining: one that comes within `snap` of a row tile's end is moved there, and row
+// tiles of up to kWholePositions are never cut, their cuts are moved to where they begin.  Stretches are at least 2 `snap` long, or as many as
+// there are row tiles, so that calls with little to do use one workgroup a row tile.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,6 +22,7 @@ namespace seer {
 constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves
 constexpr int kPromptThreads = 256;
 constexpr int kMinStretch = 256;       // positions per head of the group
+constexpr int kWholePositions = 512;
 
 // The pieces that end a stretch inside a row tile: the row tile, and in how many stretches it lies (0: none begins here and goes on).
 struct PromptCut {
@@ -94,7 +96,7 @@ __device__ __forceinline__ int64_t tiles_before(const PromptArgs& a, int64_t pas
 __device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + kRowTile * (i + 1); }
 
 struct PromptLds {
-    int64_t sums[2][kPromptThreads / kWave];
+    int64_t sums[3][kPromptThreads / kWave];
     int64_t base[2], before[2];
     int found[2];
 };
@@ -109,7 +111,7 @@ struct PromptTile {
 
 struct PromptPlan {
     int64_t total;                     // of the line
-    int64_t snap;
+    int64_t snap, whole;               // row tiles of up to this cost are not cut
     int W;                             // stretches in use
 };
 
@@ -152,17 +154,21 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
     int64_t n = 0, all;
     for (int b = b0; b < b1; ++b) n += prompt_tokens(a, b);
     const int64_t mine_n = prompt_before(n, s.sums[0], all);
-    int64_t mine_cost = 0, before = mine_n;
+    int64_t mine_cost = 0, before = mine_n, tiles = 0;
     for (int b = b0; b < b1; ++b) {
         const PromptRequest r = prompt_request(a, b, before, error);
         before += prompt_tokens(a, b);
         mine_cost += a.Hkv * tiles_before(a, r.past, r.tiles);
+        tiles += a.Hkv * static_cast<int64_t>(r.tiles);
     }
+    int64_t all_tiles;
+    prompt_before(tiles, s.sums[2], all_tiles);
     const int64_t mine = prompt_before(mine_cost, s.sums[1], p.total);
     const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
-    const int64_t most = (p.total + least - 1) / least;
+    const int64_t most = max((p.total + least - 1) / least, all_tiles);
     p.W = static_cast<int>(most < a.W ? most : a.W);
     p.snap = least / 2;
+    p.whole = static_cast<int64_t>(a.G) * (kWholePositions + a.tile_cost);
     if (w >= p.W) return false;
     int ignored = 0;
 #pragma unroll
@@ -241,7 +247,7 @@ __device__ __forceinline__ void next_tile(const PromptArgs& a, PromptTile& t) {
 // A cut at x inside row tile t, moved to the row tile's end if that is near.
 __device__ __forceinline__ int64_t moved_cut(const PromptPlan& p, const PromptTile& t, int64_t x) {
     if (x >= t.begin + t.cost) return t.begin + t.cost;        // (the line's end)
-    if (x - t.begin <= p.snap) return t.begin;
+    if (x - t.begin <= p.snap || t.cost <= p.whole) return t.begin;
     if (t.begin + t.cost - x <= p.snap) return t.begin + t.cost;
     return x;
 }

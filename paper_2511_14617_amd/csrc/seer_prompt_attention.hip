@@ -556,6 +556,8 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs 
 }
 
 static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
+    // (a block table so short that no row tile is cut leaves nothing to join)
+    if (a.G * (a.max_ctx + a.tile_cost) + kRowTile <= static_cast<int64_t>(a.G) * (kWholePositions + a.tile_cost)) return hipSuccess;
     const dim3 grid(a.W * (kRowTile * a.Dv / 4 / kPromptThreads));
     if (a.Dv == 64) hipLaunchKernelGGL((prompt_join_kernel<64>), grid, dim3(kPromptThreads), 0, stream, a);
     else if (a.Dv == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), grid, dim3(kPromptThreads), 0, stream, a);
@@ -575,7 +577,7 @@ static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
 // host
 // ---------------------------------------------------------------------------
 // What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.
-constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 448); }
+constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 384); }
 static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (!p) return SEER_EINVAL;
     if (p->B < 0 || n_tokens < 0 || p->Hq < 1 || p->Hkv < 1 || p->page_size < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1) return SEER_EINVAL;
@@ -605,7 +607,7 @@ static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     const int64_t ctx = static_cast<int64_t>(p.max_pages_per_seq) * p.page_size, G = p.Hq / p.Hkv;
     const int64_t requests = p.B < n_tokens ? p.B : n_tokens;
     const double row_tiles = (static_cast<double>(n_tokens) * G / kRowTile + requests) * p.Hkv;
-    const double most = row_tiles * (static_cast<double>(ctx + prompt_tile_cost(p.Dqk) + kRowTile) / kMinStretch + 2);
+    const double most = row_tiles * (static_cast<double>(ctx + prompt_tile_cost(p.Dqk) + kRowTile) / kMinStretch + 1);
     if (most < resident) resident = static_cast<int>(most);
     w.W = (resident + 7) / 8 * 8;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
