@@ -622,7 +622,7 @@ SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
  *  position      device [n_tokens] int32, written: ctx_len[b] + i for the row's i-th token (but see tree_mask); -1 as for slot
  *  status        device [1] int32 or NULL; bits are OR-ed in: 1 = numbers out of range (n_new, ctx_len beyond the table or the pages
  *                held, share_from), 4 = tokens beyond n_tokens, 8 = no pages left: such rows are left as they were.  2 = a page id
- *                outside the pool, 16 = a page given back more often than taken (its count is below 0: it is not given out again).  The caller clears it.
+ *                outside the pool, 16 = a page with a count below 0: it was given back more often than taken (and is not given out again).  The caller clears it.
  *  workspace     device, >= seer_kv_reserve_workspace(p) bytes, 16-byte aligned
  * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
  */

@@ -26,7 +26,9 @@ constexpr int kSmallThreads = 1024, kSmallPages = 32 * kSmallThreads, kSmallRows
 constexpr int kThreads = 256;
 constexpr int kPieceStep = kThreads * 16;            // pages that a workgroup looks at together
 constexpr int kMaxPieces = 2048;
-constexpr int kTokensPerBlock = kThreads * 4;
+// Tokens of a thread, behind one another: mostly of one row and of one page, looked up once; below kFewTokens one each, with the shorter chain of loads
+// (512 rows of five tokens: 10.4 us of the kernel with four, 349 708 tokens: 20 us with one).
+constexpr int kTokensPerThread = 4, kFewTokens = 65536;
 
 // A row of the call: positions and pages before it, pages it needs beside them (-1: refused, left as it is), new tokens (-1: over).
 struct ReserveRow {
@@ -51,17 +53,29 @@ struct ReserveArgs {
     int32_t* counts;         // [pieces] free pages of a piece
     int32_t* list;           // [pieces][piece] the free pages of a piece
     int B, P, num_pages, max_pages, n_tokens, piece, pieces;
+    uint32_t inv_p;          // 2^32 / P, at most 2^32 - 1
 };
+
+// Page of a position: the product's upper half is the quotient or one less.
+__device__ __forceinline__ int reserve_page(const ReserveArgs& a, int position) {
+    const uint32_t x = static_cast<uint32_t>(position), d = static_cast<uint32_t>(a.P), q = __umulhi(x, a.inv_p);
+    return static_cast<int>(q + ((d - 1u - (x - q * d)) >> 31));
+}
 
 __device__ __forceinline__ void raise(const ReserveArgs& a, int bits) {
     if (bits && a.status) atomicOr(a.status, bits);
 }
 
-// The record of row b, from the arrays as they are before the call; `before`: new tokens of the rows before it.  error: status bits.
-__device__ __forceinline__ ReserveRow reserve_row(const ReserveArgs& a, int b, int64_t before, int& error) {
-    ReserveRow r;
-    r.n = a.n_new[b], r.ctx = a.ctx_len[b], r.base = a.held[b], r.grow = -1;
-    const int share = a.share_from ? a.share_from[b] : -1;
+// What the arrays hold for row b before the call (requested together).
+struct ReserveInput {
+    int n, ctx, held, share;
+};
+__device__ __forceinline__ ReserveInput reserve_input(const ReserveArgs& a, int b) {
+    return ReserveInput{a.n_new[b], a.ctx_len[b], a.held[b], a.share_from ? a.share_from[b] : -1};
+}
+// The record of row b; `before`: new tokens of the rows before it.  error: status bits.
+__device__ __forceinline__ ReserveRow reserve_row(const ReserveArgs& a, int b, const ReserveInput& in, int64_t before, int& error) {
+    ReserveRow r{in.ctx, in.held, -1, in.n};
     error = 1;
     if (r.n < -1 || r.base < 0 || r.base > a.max_pages) return r;
     if (r.n < 0) {
@@ -70,62 +84,62 @@ __device__ __forceinline__ ReserveRow reserve_row(const ReserveArgs& a, int b, i
     }
     const int64_t end = static_cast<int64_t>(r.ctx) + r.n;
     if (r.ctx < 0 || end > static_cast<int64_t>(a.max_pages) * a.P) return r;
-    if (share >= 0) {
-        if (share >= a.B || share == b || r.base != 0 || r.ctx % a.P != 0) return r;
-        const int theirs = a.held[share];
-        r.base = r.ctx / a.P;
-        if (theirs < 0 || theirs > a.max_pages || r.base > theirs) {
-            r.base = 0;
-            return r;
-        }
+    if (in.share >= 0) {
+        const int pages = reserve_page(a, r.ctx);
+        if (in.share >= a.B || in.share == b || r.base != 0 || r.ctx != pages * a.P) return r;
+        const int theirs = a.held[in.share];
+        if (theirs < 0 || theirs > a.max_pages || pages > theirs) return r;
     } else if (r.ctx > static_cast<int64_t>(r.base) * a.P) {
         return r;
     }
-    if (before + r.n > a.n_tokens) {
-        if (share >= 0) r.base = 0;
-        error = 4;
-        return r;
-    }
-    const int need = static_cast<int>((end + a.P - 1) / a.P);
+    error = 4;
+    if (before + r.n > a.n_tokens) return r;
+    if (in.share >= 0) r.base = reserve_page(a, r.ctx);
+    const int need = end == 0 ? 0 : reserve_page(a, static_cast<int>(end) - 1) + 1;
     r.grow = max(0, need - r.base), error = 0;
     return r;
 }
 __device__ __forceinline__ int reserve_need(const ReserveArgs& a, const ReserveRow& r) {
-    return r.n < 0 ? 0 : static_cast<int>((static_cast<int64_t>(r.ctx) + r.n + a.P - 1) / a.P);
+    return r.n < 0 || r.ctx + r.n == 0 ? 0 : reserve_page(a, r.ctx + r.n - 1) + 1;
 }
 
-// Counts of the pages in row[from .. to) up or down, one wave (by = 0: looks whether one was given back more often than taken).
-__device__ __forceinline__ int count_pages(const ReserveArgs& a, const int32_t* row, int from, int to, int by, int lane) {
+// count(page) for the pages in row[from .. to), `lanes` threads to a row, several requested at a time.
+template <class Count>
+__device__ __forceinline__ int count_pages(const ReserveArgs& a, const int32_t* row, int from, int to, int lane, int lanes, Count&& count) {
+    constexpr int kAhead = 8;
     int error = 0;
-    for (int j = from + lane; j < to; j += kWave) {
-        const int page = row[j];
-        if (page < 0 || page >= a.num_pages) error |= 2;
-        else if (by != 0) atomicAdd(a.refs + page, by);
-        else if (__hip_atomic_load(a.refs + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0) error |= 16;
+    for (int j0 = from + lane; j0 < to; j0 += kAhead * lanes) {
+        int page[kAhead];
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x) page[x] = row[min(j0 + x * lanes, to - 1)];
+#pragma unroll
+        for (int x = 0; x < kAhead; ++x)
+            if (j0 + x * lanes < to) {
+                if (page[x] >= 0 && page[x] < a.num_pages) count(page[x]);
+                else error = 2;
+            }
     }
     return error;
 }
 // Row b's shared pages up, or those that it no longer needs down.
-__device__ __forceinline__ int count_row(const ReserveArgs& a, int b, const ReserveRow& r, int lane) {
+template <class Count>
+__device__ __forceinline__ int count_row(const ReserveArgs& a, int b, const ReserveRow& r, int share, int lane, int lanes, Count&& count) {
     if (r.grow < 0) return 0;
-    const int share = a.share_from && r.n >= 0 ? a.share_from[b] : -1;
-    if (share >= 0) return count_pages(a, a.block_table + static_cast<size_t>(share) * a.max_pages, 0, r.base, 1, lane);
-    return count_pages(a, a.block_table + static_cast<size_t>(b) * a.max_pages, reserve_need(a, r), r.base, -1, lane);
+    if (share >= 0 && r.n >= 0) return count_pages(a, a.block_table + static_cast<size_t>(share) * a.max_pages, 0, r.base, lane, lanes, [&](int page) { count(page, 1); });
+    return count_pages(a, a.block_table + static_cast<size_t>(b) * a.max_pages, reserve_need(a, r), r.base, lane, lanes, [&](int page) { count(page, -1); });
 }
 // What a row holds from now on; `granted`: it got its pages.
-__device__ __forceinline__ int finish_row(const ReserveArgs& a, int b, const ReserveRow& r, bool granted, int lane) {
+__device__ __forceinline__ int finish_row(const ReserveArgs& a, int b, const ReserveRow& r, int share, bool granted, int lane, int lanes) {
     int error = 0;
-    const int share = a.share_from && r.grow >= 0 && r.n >= 0 ? a.share_from[b] : -1;
-    if (share >= 0) {
+    if (share >= 0 && r.grow >= 0 && r.n >= 0) {
         const int32_t* from = a.block_table + static_cast<size_t>(share) * a.max_pages;
         if (granted) {
             int32_t* to = a.block_table + static_cast<size_t>(b) * a.max_pages;
-            for (int j = lane; j < r.base; j += kWave) to[j] = from[j];
+#pragma unroll 8
+            for (int j = lane; j < r.base; j += lanes) to[j] = from[j];
         } else {
-            error = count_pages(a, from, 0, r.base, -1, lane);
+            error = count_pages(a, from, 0, r.base, lane, lanes, [&](int page) { atomicAdd(a.refs + page, -1); });
         }
-    } else if (r.grow >= 0) {
-        error = count_pages(a, a.block_table + static_cast<size_t>(b) * a.max_pages, reserve_need(a, r), r.base, 0, lane);
     }
     if (lane == 0) {
         if (granted) a.held[b] = reserve_need(a, r);
@@ -135,20 +149,18 @@ __device__ __forceinline__ int finish_row(const ReserveArgs& a, int b, const Res
     return error;
 }
 
-// Slot and position of new token i, of row b whose tokens begin at `begin`; page_at(rank): the rank-th free page.
+// Slot and position of new token i, of row b whose tokens begin at `begin`; page_at(rank): the rank-th free page.  (at_lp, page): the row's page that was
+// looked up last.
 template <class PageAt>
-__device__ __forceinline__ int place_token(const ReserveArgs& a, int i, int b, int begin, const ReserveRow& r, int start, bool granted, PageAt&& page_at) {
+__device__ __forceinline__ int place_token(const ReserveArgs& a, int i, int b, int begin, const ReserveRow& r, int start, bool granted, int& at_lp, int& page,
+                                           PageAt&& page_at) {
     int slot = -1, position = -1, error = 0;
     if (granted) {
-        const int at = r.ctx + (i - begin), lp = at / a.P, inside = at - lp * a.P;
+        const int at = r.ctx + (i - begin), lp = reserve_page(a, at), inside = at - lp * a.P;
         int32_t* entry = a.block_table + static_cast<size_t>(b) * a.max_pages + lp;
-        int page;
-        if (lp < r.base) {
-            page = *entry;
-        } else {
-            page = page_at(start + lp - r.base);
-            if (inside == 0) *entry = page, a.refs[page] = 1;       // (every position of a new page is a new token's, its first one too)
-        }
+        if (lp != at_lp) page = lp < r.base ? *entry : page_at(start + lp - r.base);
+        at_lp = lp;
+        if (lp >= r.base && inside == 0) *entry = page, a.refs[page] = 1;       // (every position of a new page is a new token's, its first one too)
         position = at;
         if (page >= 0 && page < a.num_pages) slot = page * a.P + inside;
         else error = 2;
@@ -202,22 +214,28 @@ __device__ __forceinline__ int64_t block_before(int64_t v, int64_t* s_sums, int6
 }
 __device__ __forceinline__ int32_t saturate(int64_t x) { return x > 0x7fffffff ? 0x7fffffff : static_cast<int32_t>(x); }
 
-// Which of ROWS * 64 pages from page0 on are free: lane x < ROWS gets the bits of pages page0 + 64 x ...  (Read past the vector cache: another
-// workgroup, or this one, may have counted them a moment ago.)
-template <int ROWS>
-__device__ __forceinline__ uint64_t free_pages(const ReserveArgs& a, int64_t page0, int64_t end) {
+// Which of ROWS * 64 pages from page0 on are free: lane x < ROWS gets the bits of pages page0 + 64 x ...  below: the same for counts below 0 (BITS),
+// or whether this lane saw one.  (Read past the vector cache: another workgroup may have counted them a moment ago.)
+template <int ROWS, bool BITS>
+__device__ __forceinline__ void look_at_pages(const ReserveArgs& a, int64_t page0, int64_t end, uint64_t& free, uint64_t& below) {
     const int lane = threadIdx.x & (kWave - 1);
     int refs[ROWS];
 #pragma unroll
     for (int x = 0; x < ROWS; ++x)
         refs[x] = __hip_atomic_load(a.refs + min(page0 + x * kWave + lane, static_cast<int64_t>(a.num_pages) - 1), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    uint64_t mine = 0;
+    free = below = 0;
 #pragma unroll
     for (int x = 0; x < ROWS; ++x) {
-        const uint64_t bits = __ballot(refs[x] == 0 && page0 + x * kWave + lane < end);
-        if (lane == x) mine = bits;
+        const bool there = page0 + x * kWave + lane < end;
+        const uint64_t f = __ballot(refs[x] == 0 && there);
+        if (lane == x) free = f;
+        if constexpr (BITS) {
+            const uint64_t n = __ballot(refs[x] < 0 && there);
+            if (lane == x) below = n;
+        } else {
+            if (refs[x] < 0 && there) below = 1;
+        }
     }
-    return mine;
 }
 // Writes those pages behind one another, lane x's at `at` and on, as far as `limit`.
 template <int ROWS>
@@ -236,46 +254,59 @@ __device__ __forceinline__ void write_pages(int32_t* list, int limit, int page0,
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(kSmallThreads) void reserve_small(ReserveArgs a) {
     __shared__ ReserveRow s_row[kSmallRows];
+    __shared__ int32_t s_share[kSmallRows];
     __shared__ int32_t s_first[kSmallRows + 1], s_start[kSmallRows];
     __shared__ int32_t s_list[kSmallTokens];
+    __shared__ unsigned long long s_free[kSmallPages / kWave], s_below[kSmallPages / kWave];
     __shared__ int64_t s_sums[kSmallThreads / kWave];
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     int error = 0;
-    int64_t total;
+    int64_t total, all_tokens;
+    constexpr int kRows = kSmallPages / kSmallThreads;                         // (of 64 pages, a wave)
+    const int page0 = wave * kRows * kWave;
     {
-        const int64_t mine = tid < a.B ? max(a.n_new[tid], 0) : 0;
-        const int64_t before = block_before<kSmallThreads>(mine, s_sums, total);
+        // the rows' numbers and the counts as they are before the call are requested together
+        const ReserveInput in = reserve_input(a, min(tid, a.B - 1));
+        uint64_t free = 0, below = 0;
+        if (page0 < a.num_pages) look_at_pages<kRows, true>(a, page0, a.num_pages, free, below);
+        if (lane < kRows) s_free[wave * kRows + lane] = free, s_below[wave * kRows + lane] = below;
+        const int64_t before = block_before<kSmallThreads>(tid < a.B ? max(in.n, 0) : 0, s_sums, all_tokens);
         int64_t grow = 0;
         if (tid < a.B) {
-            const ReserveRow r = reserve_row(a, tid, before, error);
-            s_row[tid] = r, s_first[tid] = saturate(before), a.first[tid] = saturate(before);
+            const ReserveRow r = reserve_row(a, tid, in, before, error);
+            s_row[tid] = r, s_share[tid] = in.share, s_first[tid] = saturate(before), a.first[tid] = saturate(before);
             grow = max(r.grow, 0);
-            if (tid == a.B - 1) s_first[a.B] = saturate(total), a.first[a.B] = saturate(total);
+            if (tid == a.B - 1) s_first[a.B] = saturate(all_tokens), a.first[a.B] = saturate(all_tokens);
         }
         const int64_t start = block_before<kSmallThreads>(grow, s_sums, total);
         if (tid < a.B) s_start[tid] = saturate(start);
     }
     __syncthreads();
-    for (int b = wave; b < a.B; b += kSmallThreads / kWave) error |= count_row(a, b, s_row[b], lane);
-    __threadfence();
-    __syncthreads();                                 // the counts are what they are before pages are given
+    // a count that comes to zero or leaves it turns its page's bit over, in whatever order that happens; one that passes below zero its other bit
+    const int lanes = min(kWave, kSmallThreads >> (32 - __clz(a.B - 1 | 1))), at_lane = tid & (lanes - 1), at_row = tid / lanes;      // (all rows at once)
+    if (at_row < a.B)
+        error |= count_row(a, at_row, s_row[at_row], s_share[at_row], at_lane, lanes, [&](int page, int by) {
+            const int was = atomicAdd(a.refs + page, by);
+            if (was == 0 || was + by == 0) atomicXor(s_free + page / kWave, 1ull << (page % kWave));
+            if ((was < 0) != (was + by < 0)) atomicXor(s_below + page / kWave, 1ull << (page % kWave));
+        });
+    __syncthreads();
     const int wanted = saturate(total);
     int64_t free_total;
     {
-        constexpr int kRows = kSmallPages / kSmallThreads;                     // (of 64 pages, a wave)
-        const int page0 = wave * kRows * kWave;
-        uint64_t mine = 0;
-        if (wanted > 0 && page0 < a.num_pages) mine = free_pages<kRows>(a, page0, a.num_pages);
+        const uint64_t mine = lane < kRows ? s_free[wave * kRows + lane] : 0;
+        if (lane < kRows && s_below[wave * kRows + lane]) error |= 16;
         const int at = static_cast<int>(block_before<kSmallThreads>(__popcll(mine), s_sums, free_total));
-        if (__any(mine != 0)) write_pages<kRows>(s_list, min(wanted, kSmallTokens), page0, mine, at);
+        if (wanted > 0 && __any(mine != 0)) write_pages<kRows>(s_list, min(wanted, kSmallTokens), page0, mine, at);
     }
     __syncthreads();
     auto granted = [&](int b) { return s_row[b].grow == 0 || (s_row[b].grow > 0 && static_cast<int64_t>(s_start[b]) + s_row[b].grow <= free_total); };
-    for (int b = wave; b < a.B; b += kSmallThreads / kWave) error |= finish_row(a, b, s_row[b], granted(b), lane);
+    if (at_row < a.B) error |= finish_row(a, at_row, s_row[at_row], s_share[at_row], granted(at_row), at_lane, lanes);
     for (int i = tid; i < a.n_tokens; i += kSmallThreads) {
         const bool real = i < s_first[a.B];
         const int b = row_of_token(s_first, a.B, i);
-        error |= place_token(a, i, b, s_first[b], s_row[b], s_start[b], real && granted(b), [&](int rank) { return s_list[rank]; });
+        int lp = -1, page = 0;
+        error |= place_token(a, i, b, s_first[b], s_row[b], s_start[b], real && granted(b), lp, page, [&](int rank) { return s_list[rank]; });
     }
     raise(a, error);
 }
@@ -284,19 +315,30 @@ __global__ __launch_bounds__(kSmallThreads) void reserve_small(ReserveArgs a) {
 // three launches
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(kThreads) void reserve_rows(ReserveArgs a) {
-    const int lane = threadIdx.x & (kWave - 1), b = blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave;
-    if (b >= a.B) return;
+    constexpr int kRows = kThreads / kWave;
+    __shared__ int64_t s_sums[kRows];
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, b0 = blockIdx.x * kRows, b = b0 + wave;
+    const ReserveInput in = reserve_input(a, min(b, a.B - 1));
+    // tokens of the rows before this workgroup's, then of those before this wave's
+    int64_t sum = 0;
+#pragma unroll 4
+    for (int i = tid; i < b0; i += kThreads) sum += max(a.n_new[i], 0);
+    sum = wave_sum64(sum);
+    if (lane == 0) s_sums[wave] = sum;
+    __syncthreads();
     int64_t before = 0;
-    for (int i = lane; i < b; i += kWave) before += max(a.n_new[i], 0);
-    before = wave_sum64(before);
+#pragma unroll
+    for (int x = 0; x < kRows; ++x) before += s_sums[x];
+    if (b >= a.B) return;
+    for (int x = b0; x < b; ++x) before += max(a.n_new[x], 0);
     int error;
-    const ReserveRow r = reserve_row(a, b, before, error);
+    const ReserveRow r = reserve_row(a, b, in, before, error);
     if (lane == 0) {
         a.rows[b] = r;
         a.first[b] = saturate(before);
         if (b == a.B - 1) a.first[a.B] = saturate(before + max(r.n, 0));
     }
-    error |= count_row(a, b, r, lane);
+    error |= count_row(a, b, r, in.share, lane, kWave, [&](int page, int by) { atomicAdd(a.refs + page, by); });
     raise(a, error);
 }
 
@@ -321,7 +363,9 @@ __global__ __launch_bounds__(kThreads) void reserve_pages(ReserveArgs a) {
     for (int page0 = first; page0 < end; page0 += kPieceStep) {
         constexpr int kRows = kPieceStep / kThreads;
         const int wave0 = page0 + tid / kWave * kRows * kWave;
-        const uint64_t mine = free_pages<kRows>(a, wave0, end);
+        uint64_t mine, below;
+        look_at_pages<kRows, false>(a, wave0, end, mine, below);
+        if (below) raise(a, 16);
         const int at = count + static_cast<int>(block_before<kThreads>(__popcll(mine), s_sums, total));
         write_pages<kRows>(list, a.piece, wave0, mine, at);
         count += static_cast<int>(total);
@@ -331,6 +375,7 @@ __global__ __launch_bounds__(kThreads) void reserve_pages(ReserveArgs a) {
 
 constexpr int kFirstInLds = 4096;
 
+template <int TOKENS>
 __global__ __launch_bounds__(kThreads) void reserve_give(ReserveArgs a, int token_blocks) {
     __shared__ int32_t s_before[kMaxPieces + 1];      // free pages of the pieces before
     __shared__ int32_t s_first[kFirstInLds + 1];
@@ -349,7 +394,7 @@ __global__ __launch_bounds__(kThreads) void reserve_give(ReserveArgs a, int toke
         const int lane = tid & (kWave - 1), b = (blockIdx.x - token_blocks) * (kThreads / kWave) + tid / kWave;
         if (b < a.B) {
             const ReserveRow r = a.rows[b];
-            error = finish_row(a, b, r, granted(r, a.start[b]), lane);
+            error = finish_row(a, b, r, a.share_from ? a.share_from[b] : -1, granted(r, a.start[b]), lane, kWave);
         }
         raise(a, error);
         return;
@@ -368,15 +413,23 @@ __global__ __launch_bounds__(kThreads) void reserve_give(ReserveArgs a, int toke
         }
         return a.list[static_cast<size_t>(lo) * a.piece + (rank - s_before[lo])];
     };
+    const int64_t i0 = (static_cast<int64_t>(blockIdx.x) * kThreads + tid) * TOKENS;
+    if (i0 < a.n_tokens) {
+        int b = row_of_token(first, a.B, static_cast<int>(i0));
+        int begin = first[b], behind = first[b + 1];
+        ReserveRow r = a.rows[b];
+        int start = a.start[b], lp = -1, page = 0;
 #pragma unroll
-    for (int x = 0; x < kTokensPerBlock / kThreads; ++x) {
-        const int64_t i = static_cast<int64_t>(blockIdx.x) * kTokensPerBlock + x * kThreads + tid;
-        if (i >= a.n_tokens) break;
-        const bool real = i < first[a.B];
-        const int b = row_of_token(first, a.B, static_cast<int>(i));
-        const ReserveRow r = a.rows[b];
-        const int start = a.start[b];
-        error |= place_token(a, static_cast<int>(i), b, first[b], r, start, real && granted(r, start), page_at);
+        for (int x = 0; x < TOKENS; ++x) {
+            const int64_t i = i0 + x;
+            if (i >= a.n_tokens) break;
+            const bool real = i < first[a.B];
+            if (real && i >= behind) {
+                b = row_of_token(first, a.B, static_cast<int>(i));
+                begin = first[b], behind = first[b + 1], r = a.rows[b], start = a.start[b], lp = -1;
+            }
+            error |= place_token(a, static_cast<int>(i), b, begin, r, start, real && granted(r, start), lp, page, page_at);
+        }
     }
     raise(a, error);
 }
@@ -439,6 +492,7 @@ extern "C" int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_
     a.slot = slot, a.position = position, a.status = status;
     a.B = p->B, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq, a.n_tokens = p->n_tokens;
     a.piece = layout.piece, a.pieces = layout.pieces;
+    a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (seer::reserve_is_small(*p)) {
         hipLaunchKernelGGL(seer::reserve_small, dim3(1), dim3(seer::kSmallThreads), 0, stream, a);
@@ -451,12 +505,15 @@ extern "C" int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_
     a.counts = reinterpret_cast<int32_t*>(ws + layout.off_counts);
     a.list = reinterpret_cast<int32_t*>(ws + layout.off_list);
     const unsigned row_blocks = (p->B + seer::kThreads / seer::kWave - 1) / (seer::kThreads / seer::kWave);
-    const int token_blocks = (p->n_tokens + seer::kTokensPerBlock - 1) / seer::kTokensPerBlock;
+    const int per_block = seer::kThreads * (p->n_tokens < seer::kFewTokens ? 1 : seer::kTokensPerThread), token_blocks = (p->n_tokens + per_block - 1) / per_block;
     hipLaunchKernelGGL(seer::reserve_rows, dim3(row_blocks), dim3(seer::kThreads), 0, stream, a);
     hipLaunchKernelGGL(seer::reserve_pages, dim3(1u + layout.pieces), dim3(seer::kThreads), 0, stream, a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess) return static_cast<int>(err);
-    hipLaunchKernelGGL(seer::reserve_give, dim3(token_blocks + row_blocks), dim3(seer::kThreads), 0, stream, a, token_blocks);
+    if (p->n_tokens < seer::kFewTokens)
+        hipLaunchKernelGGL((seer::reserve_give<1>), dim3(token_blocks + row_blocks), dim3(seer::kThreads), 0, stream, a, token_blocks);
+    else
+        hipLaunchKernelGGL((seer::reserve_give<seer::kTokensPerThread>), dim3(token_blocks + row_blocks), dim3(seer::kThreads), 0, stream, a, token_blocks);
     err = hipGetLastError();
     return err == hipSuccess ? SEER_OK : static_cast<int>(err);
 }

@@ -54,7 +54,7 @@ def reserve(table, held, refs, ctx, new, share, mask, n_tokens, page):
                     status |= 2
                 else:
                     refs[p] -= 1
-    if any(refs[p] < 0 for b in range(B) if good[b] and shared[b] < 0 for p in table0[b][need[b]:base[b]] if 0 <= p < pages):
+    if min(refs) < 0:
         status |= 16
     free = [p for p in range(pages) if refs[p] == 0]
     asked = 0
