@@ -497,6 +497,17 @@ def _here(stream: Optional[torch.cuda.Stream], **tensors: Optional[torch.Tensor]
             raise ValueError("%s: want it on the current device, cuda:%d, got %s" % (name, device, t.device))
 
 
+def _want_here(stream: Optional[torch.cuda.Stream], *wanted) -> None:
+    """_want and _here in one pass over (tensor or None, dtype, shape, name): short calls are bound by the host."""
+    device = torch.cuda.current_device()
+    if stream is not None and stream.device_index != device:
+        raise ValueError("stream: want one of the current device, cuda:%d, got one of cuda:%d" % (device, stream.device_index))
+    for t, dtype, shape, name in wanted:
+        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != device):
+            raise ValueError("%s: want contiguous %s%s on the current device, cuda:%d, got %s%s on %s" %
+                             (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+
+
 def _empty(shape, dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
     """New memory of the stream that writes it: what the allocator hands out on the current stream may have work pending there, and a workspace
     that is given back there may be handed out again, while the other stream is still at work."""
@@ -704,41 +715,39 @@ def seer_kv_reserve(block_table: torch.Tensor, pages_held: torch.Tensor, page_re
         raise ValueError("want block_table [B,max_pages] and page_refs [num_pages]")
     B, max_pages = block_table.shape
     p = SeerReserveParams(B, int(page_size), page_refs.shape[0], max_pages, int(n_tokens))
-    _want(block_table, torch.int32, (B, max_pages), "block_table")
-    _want(pages_held, torch.int32, (B,), "pages_held")
-    _want(page_refs, torch.int32, (p.num_pages,), "page_refs")
-    _want(ctx_len, torch.int32, (B,), "ctx_len")
-    _want(n_new, torch.int32, (B,), "n_new")
-    if share_from is not None:
-        _want(share_from, torch.int32, (B,), "share_from")
-    if tree_mask is not None:
-        _want(tree_mask, torch.int64, (p.n_tokens,), "tree_mask")
-    if status is not None:
-        _want(status, torch.int32, (1,), "status")
-    dev = block_table.device
-    if out is None:                                         # (one allocation: short calls are bound by the host)
-        out = _empty(2 * B + 1 + 2 * p.n_tokens, torch.int32, dev, stream).split((B, B + 1, p.n_tokens, p.n_tokens))
-    else:
-        for t, shape, name in zip(out, ((B,), (B + 1,), (p.n_tokens,), (p.n_tokens,)), ("step_len", "first_token", "slot", "position")):
-            _want(t, torch.int32, shape, name)
+    ref, scratch = ctypes.byref(p), 0
     if workspace is None:
-        need = int(lib.seer_kv_reserve_workspace(ctypes.byref(p)))
-        workspace = _empty(max(need, 256), torch.uint8, dev, stream)
-    _here(stream, block_table=block_table, pages_held=pages_held, page_refs=page_refs, ctx_len=ctx_len, n_new=n_new, share_from=share_from,
-          tree_mask=tree_mask, step_len=out[0], first_token=out[1], slot=out[2], position=out[3], status=status, workspace=workspace)
-    _check(lib.seer_kv_reserve(ctypes.byref(p), _ptr(ctx_len), _ptr(n_new), _ptr(share_from), _ptr(tree_mask), _ptr(block_table),
-                               _ptr(pages_held), _ptr(page_refs), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(out[3]), _ptr(status),
-                               _ptr(workspace), workspace.numel(), _stream_handle(stream)))
-    return tuple(out)
+        scratch = (int(lib.seer_kv_reserve_workspace(ref)) + 255) // 256 * 64 or 64        # (in int32)
+    if out is None:                                         # one allocation, with a small workspace in front: short calls are bound by the host
+        front = scratch if scratch <= 1024 else 0
+        made = _empty(front + 2 * B + 1 + 2 * p.n_tokens, torch.int32, block_table.device, stream)
+        head, step_len, first_token, slot, position = made.split_with_sizes((front, B, B + 1, p.n_tokens, p.n_tokens))
+        if front:
+            workspace = head
+    else:
+        step_len, first_token, slot, position = out
+    if workspace is None:
+        workspace = _empty(scratch, torch.int32, block_table.device, stream)
+    i32, rows, tokens = torch.int32, (B,), (p.n_tokens,)
+    _want_here(stream, (block_table, i32, (B, max_pages), "block_table"), (pages_held, i32, rows, "pages_held"), (page_refs, i32, (p.num_pages,), "page_refs"),
+               (ctx_len, i32, rows, "ctx_len"), (n_new, i32, rows, "n_new"), (share_from, i32, rows, "share_from"), (tree_mask, torch.int64, tokens, "tree_mask"),
+               (step_len, i32, rows, "step_len"), (first_token, i32, (B + 1,), "first_token"), (slot, i32, tokens, "slot"), (position, i32, tokens, "position"),
+               (status, i32, (1,), "status"), (workspace, workspace.dtype, workspace.shape, "workspace"))
+    _check(lib.seer_kv_reserve(ref, ctx_len.data_ptr(), n_new.data_ptr(), _ptr(share_from), _ptr(tree_mask), block_table.data_ptr(),
+                               pages_held.data_ptr(), page_refs.data_ptr(), step_len.data_ptr(), first_token.data_ptr(), slot.data_ptr(),
+                               position.data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                               _stream_handle(stream)))
+    return step_len, first_token, slot, position
 
 
-def _token_rows(t: torch.Tensor, N: int, name: str) -> int:
+def _token_rows(t: torch.Tensor, N: int, device: int, name: str) -> int:
     """Elements from one token to the next of rows [N,H,D] (tokens may be apart, their heads not)."""
-    if (t.dim() != 3 or t.shape[0] != N or t.dtype != torch.bfloat16 or not t.is_cuda or (t.shape[2] > 1 and t.stride(2) != 1)
-            or (t.shape[1] > 1 and t.stride(1) != t.shape[2])):
-        raise ValueError("%s: want device bfloat16 [%d,H,D], the heads of a token behind one another, got %s%s with strides %s on %s" %
-                         (name, N, t.dtype, tuple(t.shape), t.stride(), t.device))
-    return t.stride(0) if N > 1 else max(t.stride(0), t.shape[1] * t.shape[2]) // 8 * 8
+    shape, stride = t.shape, t.stride()
+    if (len(shape) != 3 or shape[0] != N or t.dtype != torch.bfloat16 or t.get_device() != device or (shape[2] > 1 and stride[2] != 1)
+            or (shape[1] > 1 and stride[1] != shape[2])):
+        raise ValueError("%s: want bfloat16 [%d,H,D] on the current device, the heads of a token behind one another, got %s%s with strides %s on %s" %
+                         (name, N, t.dtype, tuple(shape), stride, t.device))
+    return stride[0] if N > 1 else max(stride[0], shape[1] * shape[2]) // 8 * 8
 
 
 def seer_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch.Tensor], slot: torch.Tensor, position: Optional[torch.Tensor],
@@ -753,40 +762,34 @@ def seer_kv_append(q: Optional[torch.Tensor], k: torch.Tensor, v: Optional[torch
         raise ValueError("want k [N,Hkv,Dqk] and k_pages [num_pages,Hkv,page,Dqk]")
     N, Hkv, Dqk = k.shape
     num_pages, P = k_pages.shape[0], k_pages.shape[2]
-    k_stride, v_stride, q_stride, out_stride, Hq, Dv = _token_rows(k, N, "k"), 0, 0, 0, 0, 0
-    _want(k_pages, torch.bfloat16, (num_pages, Hkv, P, Dqk), "k_pages")
+    device = torch.cuda.current_device()
+    k_stride, v_stride, q_stride, out_stride, Hq, Dv, R = _token_rows(k, N, device, "k"), 0, 0, 0, 0, 0, 0
     if (v is None) != (v_pages is None):
         raise ValueError("v, v_pages: want both or neither")
     if v is not None:
-        v_stride, Dv = _token_rows(v, N, "v"), v.shape[2]
-        _want(v_pages, torch.bfloat16, (num_pages, Hkv, P, Dv), "v_pages")
+        v_stride, Dv = _token_rows(v, N, device, "v"), v.shape[2]
         if v.shape[1] != Hkv:
             raise ValueError("v: want [N,%d,Dv], got %s" % (Hkv, tuple(v.shape)))
-    _want(slot, torch.int32, (N,), "slot")
-    R = 0
     if inv_freq is not None:
         R = 2 * inv_freq.numel()
-        _want(inv_freq, torch.float32, (R // 2,), "inv_freq")
         if position is None:
             raise ValueError("position: needed for a rotation")
-    if position is not None:
-        _want(position, torch.int32, (N,), "position")
-    if status is not None:
-        _want(status, torch.int32, (1,), "status")
     if not 0 <= int(rotary_at) < 2 ** 31:
         raise ValueError("rotary_at: want a number from 0 to 2^31 - 1, got %s" % (rotary_at,))
     if q is not None:
-        q_stride, Hq = _token_rows(q, N, "q"), q.shape[1]
+        q_stride, Hq = _token_rows(q, N, device, "q"), q.shape[1]
         if q.shape[2] != Dqk:
             raise ValueError("q: want [N,Hq,%d], got %s" % (Dqk, tuple(q.shape)))
         if q_out is None:
             q_out = _empty((N, Hq, Dqk), torch.bfloat16, q.device, stream)
-        out_stride = _token_rows(q_out, N, "q_out")
+        out_stride = _token_rows(q_out, N, device, "q_out")
         if q_out.shape != q.shape:
             raise ValueError("q_out: want %s, got %s" % (tuple(q.shape), tuple(q_out.shape)))
     elif q_out is not None:
         raise ValueError("q_out: there is no q")
-    _here(stream, q=q, k=k, v=v, slot=slot, position=position, k_pages=k_pages, v_pages=v_pages, inv_freq=inv_freq, q_out=q_out, status=status)
+    _want_here(stream, (k_pages, torch.bfloat16, (num_pages, Hkv, P, Dqk), "k_pages"), (v_pages, torch.bfloat16, (num_pages, Hkv, P, Dv), "v_pages"),
+               (slot, torch.int32, (N,), "slot"), (position, torch.int32, (N,), "position"), (inv_freq, torch.float32, (R // 2,), "inv_freq"),
+               (status, torch.int32, (1,), "status"))
     p = SeerAppendParams(N, Hq, Hkv, Dqk, Dv, P, num_pages, 1 if v is None else 0, int(rotary_at), R, 1 if interleaved else 0,
                          q_stride, k_stride, v_stride, out_stride)
     _check(lib.seer_kv_append(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(slot), _ptr(position), _ptr(inv_freq), _ptr(q_out), _ptr(k_pages),
@@ -813,24 +816,14 @@ def seer_prompt_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: Optio
     B = block_table.shape[0]
     p = attn_params(q.unsqueeze(1), k_pages, v_pages, block_table, scale, Dv)
     p.B = B
-    _want(q, torch.bfloat16, (N, Hq, Dqk), "q")
-    _want(k_pages, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size, Dqk), "k_pages")
-    if v_pages is not None:
-        _want(v_pages, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size, p.Dv), "v_pages")
-    _want(block_table, torch.int32, (B, p.max_pages_per_seq), "block_table")
-    _want(ctx_len, torch.int32, (B,), "ctx_len")
-    _want(first_token, torch.int32, (B + 1,), "first_token")
     if out is None:
         out = _empty((N, Hq, p.Dv), torch.bfloat16, q.device, stream)
-    else:
-        _want(out, torch.bfloat16, (N, Hq, p.Dv), "out")
-    if status is not None:
-        _want(status, torch.int32, (1,), "status")
     if workspace is None:
-        need = int(lib.seer_prompt_attention_workspace(ctypes.byref(p), N))
-        workspace = _empty(max(need, 256), torch.uint8, q.device, stream)
-    _here(stream, q=q, k_pages=k_pages, v_pages=v_pages, block_table=block_table, ctx_len=ctx_len, first_token=first_token, out=out, status=status,
-          workspace=workspace)
+        workspace = _empty(max(int(lib.seer_prompt_attention_workspace(ctypes.byref(p), N)), 256), torch.uint8, q.device, stream)
+    i32, bf16, pool = torch.int32, torch.bfloat16, (p.num_pages, p.Hkv, p.page_size)
+    _want_here(stream, (q, bf16, (N, Hq, Dqk), "q"), (k_pages, bf16, (*pool, Dqk), "k_pages"), (v_pages, bf16, (*pool, p.Dv), "v_pages"),
+               (block_table, i32, (B, p.max_pages_per_seq), "block_table"), (ctx_len, i32, (B,), "ctx_len"), (first_token, i32, (B + 1,), "first_token"),
+               (out, bf16, (N, Hq, p.Dv), "out"), (status, i32, (1,), "status"), (workspace, workspace.dtype, workspace.shape, "workspace"))
     _check(lib.seer_prompt_attention(_ptr(out), _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table), _ptr(ctx_len), _ptr(first_token),
-                                     ctypes.byref(p), N, _ptr(status), _ptr(workspace), workspace.numel(), _stream_handle(stream)))
+                                     ctypes.byref(p), N, _ptr(status), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_handle(stream)))
     return out

@@ -22,6 +22,7 @@ constexpr int kAppendMaxRotary = 512;                 // components rotated, at 
 constexpr int kAppendTokens = 4;                      // tokens of a workgroup, at most
 constexpr int kAppendHold = 4;                        // jobs that a thread has in flight
 constexpr int kJobsWanted = kAppendThreads * kAppendHold;
+constexpr int kManyBlocks = 1024;                     // workgroups that the GPU is full with
 
 struct AppendArgs {
     const uint16_t* q;
@@ -206,9 +207,10 @@ extern "C" int seer_kv_append(const seer_append_params* p, const void* q, const 
     a.jobs = (p->Hq + p->Hkv) * a.jobs_qk + (shared ? 0 : p->Hkv * a.jobs_v);
     auto reciprocal = [](int d) { return static_cast<uint32_t>(((uint64_t{1} << 32) + d - 1) / d); };     // (d = 1: not looked at)
     a.inv_qk = reciprocal(a.jobs_qk), a.inv_v = reciprocal(a.jobs_v);
-    // Small tokens are taken up to four at a time, large ones shared by several workgroups, as long as a thread has its jobs in flight.
+    // Small tokens are taken up to four at a time where there are enough of them, large ones shared by several workgroups, as long as a thread has its
+    // jobs in flight.
     a.tokens = 1, a.parts = 1;
-    while (a.tokens < seer::kAppendTokens && a.tokens * a.jobs < seer::kJobsWanted) a.tokens *= 2;
+    while (a.tokens < seer::kAppendTokens && a.tokens * a.jobs < seer::kJobsWanted && p->n_tokens / (2 * a.tokens) >= seer::kManyBlocks) a.tokens *= 2;
     if (a.tokens == 1) a.parts = (a.jobs + 2 * seer::kJobsWanted - 1) / (2 * seer::kJobsWanted);
     const int64_t blocks = (static_cast<int64_t>(p->n_tokens) + a.tokens - 1) / a.tokens * a.parts;
     if (blocks > 0xffffffffLL / seer::kAppendThreads) return SEER_ESHAPE;

@@ -177,15 +177,37 @@ def test_the_binding_refuses_other_tensors():
         b.seer_kv_reserve(i32(2, 3), i32(2), i32(9), i32(2), i32(2), 5, 2 ** 32 + 16)
     with pytest.raises(ValueError, match="block_table"):
         b.seer_kv_reserve(i32(2), i32(2), i32(9), i32(2), i32(2), 5, 16)
-    with pytest.raises(ValueError, match="device"):
-        b.seer_kv_reserve(i32(2, 3), i32(2), i32(9), i32(2), i32(2), 5, 16)
     with pytest.raises(ValueError, match="want k "):
         b.seer_kv_append(None, bf(4, 2), None, i32(4), None, bf(3, 2, 16, 8), None)
-    with pytest.raises(ValueError, match="k: want device"):
-        b.seer_kv_append(None, bf(4, 2, 8), None, i32(4), None, bf(3, 2, 16, 8), None)
     with pytest.raises(ValueError, match="want q "):
         b.seer_prompt_attention(bf(4, 2), bf(3, 2, 16, 64), None, i32(2, 3), i32(2), i32(3), 1.0)
     with pytest.raises(ValueError, match="Dv"):
         b.seer_prompt_attention(bf(4, 2, 576), bf(3, 1, 16, 576), None, i32(2, 3), i32(2), i32(3), 1.0)
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_tensors_of_other_places():
+    """On the GPU machine: host tensors, other types and shapes, tensors that are not contiguous."""
+    import torch
+    from paper_2511_14617_amd import binding as b
+    i32 = lambda *s: torch.zeros(s, dtype=torch.int32, device="cuda")
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16, device="cuda")
+    for name, args in (("block_table", (i32(2, 3).cpu(), i32(2), i32(9), i32(2), i32(2))), ("pages_held", (i32(2, 3), i32(3), i32(9), i32(2), i32(2))),
+                       ("page_refs", (i32(2, 3), i32(2), i32(18)[::2], i32(2), i32(2))), ("ctx_len", (i32(2, 3), i32(2), i32(9), i32(2).long(), i32(2))),
+                       ("n_new", (i32(2, 3), i32(2), i32(9), i32(2), i32(2).cpu()))):
+        with pytest.raises(ValueError, match=name):
+            b.seer_kv_reserve(*args, 5, 16)
+    with pytest.raises(ValueError, match="slot"):
+        b.seer_kv_append(None, bf(4, 2, 8), None, i32(5), None, bf(3, 2, 16, 8), None)
+    with pytest.raises(ValueError, match="k: want"):
+        b.seer_kv_append(None, bf(4, 2, 8).cpu(), None, i32(4), None, bf(3, 2, 16, 8), None)
     with pytest.raises(ValueError, match="q: want"):
-        b.seer_prompt_attention(bf(4, 2, 64), bf(3, 1, 16, 64), bf(3, 1, 16, 64), i32(2, 3), i32(2), i32(3), 1.0)
+        b.seer_kv_append(bf(4, 2, 16), bf(4, 2, 8), None, i32(4), None, bf(3, 2, 16, 8), None)
+    with pytest.raises(ValueError, match="position"):
+        b.seer_kv_append(None, bf(4, 2, 8), None, i32(4), None, bf(3, 2, 16, 8), None, inv_freq=torch.ones(4, device="cuda"))
+    good = (bf(4, 2, 64), bf(3, 1, 16, 64), bf(3, 1, 16, 64), i32(2, 3), i32(2), i32(3), 1.0)
+    for k, name in enumerate(("q", "k_pages", "v_pages", "block_table", "ctx_len", "first_token")):
+        with pytest.raises(ValueError, match=name):
+            b.seer_prompt_attention(*[x.cpu() if i == k else x for i, x in enumerate(good)])
+    with pytest.raises(b.SeerError, match="head"):
+        b.seer_prompt_attention(bf(4, 2, 96), bf(3, 1, 16, 96), bf(3, 1, 16, 96), *good[3:])
