@@ -34,7 +34,7 @@ struct PromptShape {
     static constexpr int kKAhead = kKSteps < 8 ? kKSteps : 8;                // K operands requested ahead of their MFMA
     static constexpr int kVAhead = kPv < 8 ? kPv : 8;                        // V operands (two reads each)
     // waves that a SIMD holds, by registers: queries, outputs, scores of two tiles, operands
-    static constexpr int kWavesPerSimd = DQK <= 64 ? 3 : (DQK <= 128 ? 2 : 1);
+    static constexpr int kWavesPerSimd = DQK <= 64 ? 3 : (DQK <= 192 ? 2 : 1);
     static_assert(kKSlot % 4096 == 0 && kVSlot % 4096 == 0 && kLds <= 156 * 1024, "");
 };
 
@@ -94,9 +94,9 @@ void prompt_tile_kernel(PromptArgs a) {
     using tile::k_swz;
     using tile::v_swz;
     constexpr int kTile = S::kTile;
+    // (nothing beside the rings: two workgroups of the 192/128 shape take all 160 KB of a CU; the plan's words lie where the rings come)
     __shared__ __attribute__((aligned(1024))) unsigned char lds[S::kLds];
-    __shared__ PromptLds s_plan;
-    __shared__ uint32_t s_found;                    // V rows with infinities or NaN of the scanned tile
+    PromptLds& s_plan = *reinterpret_cast<PromptLds*>(lds);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     // neighbouring stretches read the same positions: one XCD (ids are dealt round-robin to eight) takes an eighth of the line
@@ -282,14 +282,16 @@ void prompt_tile_kernel(PromptArgs a) {
                 left = 0;
                 if (tok_begin + u * kTile + kTile - 1 <= all_see) return;
                 unsigned char* vl = lds + S::kVBase + slot_at;
-                if (tid == 0) s_found = 0;
+                // (where the tile's K was, which all waves have left: the next K goes there behind this)
+                uint32_t* found_in = reinterpret_cast<uint32_t*>(lds + (u & (kSlots - 1)) * S::kKSlot);
+                if (tid == 0) *found_in = 0;
                 wait_reads<0>();
                 bare_barrier();
                 const uint32_t found = tile::tile_nonfinite<DQK, DV>(vl, tid, kPromptThreads);
-                if (found) atomicOr(&s_found, found);
+                if (found) atomicOr(found_in, found);
                 wait_reads<0>();
                 bare_barrier();
-                left = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
+                left = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(found_in));
                 if (left) {
                     tile::tile_clear_rows<DQK, DV>(vl, left, tid, kPromptThreads);
                     wait_reads<0>();
@@ -599,7 +601,7 @@ struct PromptLayout {
     int W;
     size_t off_ml, off_acc, total;
 };
-constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 64 ? 3 : (dqk <= 128 ? 2 : 1); }
+constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 64 ? 3 : (dqk <= 192 ? 2 : 1); }
 static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     PromptLayout w{};
     // no more stretches than the GPU holds at once, nor than the host can see work for
