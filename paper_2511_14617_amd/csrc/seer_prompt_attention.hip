@@ -124,7 +124,10 @@ void prompt_tile_kernel(PromptArgs a) {
         if (tid == 0) a.cuts[w] = cut;
     }
     bool bad_page = false;
-    int win_b = -1, win = 0, pg_win = 0;            // window of page ids: request, first logical page; lane l holds the (clamped) id of page win + l
+    // ANY_PAGE: window of page ids: request, first logical page; lane l holds the (clamped) id of page win + l.
+    // Else a window of rows: request, KV head, first tile; lane l holds the row of the pool where tile win + l's position 8 wave is; and the window of the request's
+    // first tiles, with which most row tiles begin.
+    int win_b = -1, win_h = -1, win = 0, in_win = 0, first_win = 0;
     const int lds0 = tile::lds_addr(lds);
     auto page_of = [&](int position) __attribute__((always_inline)) -> int { return prompt_page(a, position); };
 
@@ -192,27 +195,36 @@ void prompt_tile_kernel(PromptArgs a) {
             // ---- tile loads --------------------------------------------------------------------------------
             const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
             const int last_page = page_of(static_cast<int>(t.r.past) + t.r.n - 1);
+            const int last = static_cast<int>(t.r.past) + t.r.n - 1;
             auto set_window = [&](int first) __attribute__((always_inline)) {
                 win = first;
-                int pg = table[min(first + lane, a.max_pages - 1)];
-                if ((pg < 0 || pg >= a.num_pages) && first + lane <= last_page) bad_page = true;
-                pg_win = min(max(pg, 0), a.num_pages - 1);
+                int pg;
+                if constexpr (ANY_PAGE) {
+                    pg = table[min(first + lane, a.max_pages - 1)];
+                    if ((pg < 0 || pg >= a.num_pages) && first + lane <= last_page) bad_page = true;
+                    in_win = min(max(pg, 0), a.num_pages - 1);
+                } else {
+                    // (behind the request's last position: its last eight again)
+                    const int position = min((first + lane) * kTile + wave * 8, last & ~7), lp = page_of(position);
+                    pg = table[lp];
+                    if (pg < 0 || pg >= a.num_pages) bad_page = true;
+                    pg = min(max(pg, 0), a.num_pages - 1);
+                    in_win = static_cast<int>((static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(position - lp * a.P));
+                    if (first == 0) first_win = in_win;
+                }
             };
             // Row of the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU) of tile u's position 8 wave; ANY_PAGE: of position ln.
             // Tiles are asked for in ascending order.
             auto tile_row = [&](int u) __attribute__((always_inline)) -> uint32_t {
-                const int tb = tok_begin + u * kTile;
                 if constexpr (ANY_PAGE) {
+                    const int tb = tok_begin + u * kTile;
                     if (page_of(tb) < win || page_of(tb + kTile - 1) >= win + kWave) set_window(page_of(tb));      // (uniform; a tile spans at most 32 pages)
                     const int lp = page_of(tb + ln);
-                    const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, pg_win);
+                    const int pg = __builtin_amdgcn_ds_bpermute((lp - win) << 2, in_win);
                     return (static_cast<uint32_t>(pg) * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tb + ln - lp * a.P);
                 } else {
-                    const int tok = tb + wave * 8, lp = page_of(tok);
-                    if (lp < win || lp >= win + kWave) set_window(lp);
-                    const uint32_t pg = __builtin_amdgcn_readlane(pg_win, __builtin_amdgcn_readfirstlane(lp - win));
-                    // (said to be uniform: a descriptor that may differ from lane to lane is taken apart lane by lane)
-                    return __builtin_amdgcn_readfirstlane((pg * a.Hkv + t.kvh) * static_cast<uint32_t>(a.P) + static_cast<uint32_t>(tok - lp * a.P));
+                    if (u0 + u - win >= kWave) set_window(u0 + u);
+                    return __builtin_amdgcn_readlane(in_win, u0 + u - win);
                 }
             };
             auto issue_k = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
@@ -429,9 +441,13 @@ void prompt_tile_kernel(PromptArgs a) {
             };
 
             // the first tiles: K of 0, 1, 2 and V of 0, 1, in the order in which steps -3, -2, -1 would request them
-            if (t.b != win_b) {                     // (else the window may do: row tiles and KV heads of a request often begin with the one before's)
-                win_b = t.b;
-                set_window(page_of(tok_begin));
+            if constexpr (ANY_PAGE) {
+                if (t.b != win_b) win_b = t.b, set_window(page_of(tok_begin));      // (else the window may do)
+            } else if (t.b == win_b && t.kvh == win_h && u0 == 0) {
+                win = 0, in_win = first_win;
+            } else {
+                win_b = u0 == 0 ? t.b : -1, win_h = t.kvh;
+                set_window(u0);
             }
             {
                 const uint32_t row0 = tile_row(0);
