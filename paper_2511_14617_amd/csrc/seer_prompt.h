@@ -21,6 +21,9 @@ namespace seer {
 
 constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves
 constexpr int kPromptThreads = 256;
+// The exponent reference of a row that has seen no finite score: the lowest float, which no finite score is below.  Every difference of references is then a
+// number or -inf, and a row that stays without a score asks for no rescaling.
+constexpr float kNoScore = -3.402823466e38f;
 constexpr int kMinStretch = 256;       // positions per head of the group
 constexpr int kWholePositions = 512;
 

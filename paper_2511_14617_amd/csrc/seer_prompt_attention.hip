@@ -180,7 +180,7 @@ void prompt_tile_kernel(PromptArgs a) {
         for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-        float m_run = kNegInf, l_run = 0.f;
+        float m_run = kNoScore, l_run = 0.f;
         __syncthreads();                            // every wave is done with the rings of the piece before
         if (n_tiles > 0) {
             u32x4 qreg[S::kKSteps];
@@ -254,10 +254,9 @@ void prompt_tile_kernel(PromptArgs a) {
                 } else if constexpr (part == 2) {
                     mx = max_across_halves(mx) * a.scale_log2;
                 } else {
-                    const float m_new = mx > m_run + 8.f ? mx : m_run;
-                    m_use = m_new == kNegInf ? 0.f : m_new;            // nothing visible yet: keep exp2 finite
+                    m_use = mx > m_run + 8.f ? mx : m_run;
                     alpha = fast_exp2(m_run - m_use);
-                    m_run = m_new;
+                    m_run = m_use;
                 }
             };
             // -inf into the scores of tile u that this lane's row does not see
@@ -554,14 +553,14 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs 
     const int64_t row = static_cast<int64_t>(cut.tile) * kRowTile + r;
     if (row >= static_cast<int64_t>(n) * a.G) return;
     auto slot = [&](int k) { return 2 * static_cast<size_t>(w + k) + (k == 0 ? 1 : 0); };
-    float m = kNegInf;
+    float m = kNoScore;
     for (int k = 0; k < cut.pieces; ++k) m = fmaxf(m, a.part_ml[2 * (slot(k) * kRowTile + r)]);
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < cut.pieces; ++k) {
         const float mk = a.part_ml[2 * (slot(k) * kRowTile + r)], lk = a.part_ml[2 * (slot(k) * kRowTile + r) + 1];
-        const float f = mk == kNegInf ? 0.f : fast_exp2(mk - m);
+        const float f = fast_exp2(mk - m);
         const f32x4 v = *(reinterpret_cast<const f32x4*>(a.part_acc) + slot(k) * kVectors + e);
         l = fmaf(lk, f, l);
 #pragma unroll

@@ -101,7 +101,7 @@ void prompt_latent_kernel(PromptArgs a) {
         for (int dt = 0; dt < kDTiles; ++dt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
-        float m_run = kNegInf, l_run = 0.f, alpha = 1.f;
+        float m_run = kNoScore, l_run = 0.f, alpha = 1.f;
         __syncthreads();                            // every wave is done with the stages of the piece before
         if (n_tiles > 0) {
             // Queries through LDS: a wave's 32 rows lie there as a tile does (waves 0 to 2 in the stages, wave 3 in the parked part), so that they are
@@ -265,10 +265,9 @@ void prompt_latent_kernel(PromptArgs a) {
                     mx_part = max_across_halves(mx_part) * a.scale_log2;
                     SEER_MLA_PIN(mx_part);
                 } else {
-                    const float m_new = (mx_part > m_run + 8.f) ? mx_part : m_run;
-                    m_use = (m_new == kNegInf) ? 0.f : m_new;
+                    m_use = mx_part > m_run + 8.f ? mx_part : m_run;
                     alpha = fast_exp2(m_run - m_use);
-                    m_run = m_new;
+                    m_run = m_use;
                     SEER_MLA_PIN(m_use);
                     SEER_MLA_PIN(alpha);
                     SEER_MLA_PIN(m_run);

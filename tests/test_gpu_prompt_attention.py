@@ -157,6 +157,20 @@ def test_equal_scores_and_far_ones():
         compare(out, plain(c))
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128, 128, 16), (16, 1, 576, 512, 64)])
+def test_scores_far_below_zero(heads):
+    """All scores of a row equal and as low as -10^37 (exactly equal: no rounding is between them): still a running mean of V."""
+    c = make(15, [150, 3], [0, 90], *heads)
+    c["q"].fill_(1e18)
+    if c["v"] is not None:
+        c["k"].fill_(-1e18)
+    else:                                                            # (the latent's value components stay as they are and meet queries of zero)
+        c["q"][..., :512] = 0
+        c["k"][..., 512:] = -1e18
+    out, _ = call(c)
+    compare(out, plain(c))
+
+
 def spoil(x, b, j, c, value, dims=slice(None)):
     x[c["table"][b, j // c["page"]].long(), :, j % c["page"], dims] = value
 
