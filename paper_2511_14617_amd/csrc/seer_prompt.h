@@ -42,13 +42,13 @@ struct PromptArgs {
     const int32_t* first;
     int32_t* status;
     PromptCut* cuts;       // [W]
-    float* part_ml;        // [2 W][kRowTile][2]: reference exponent (in units of log2 e), sum
+    float* part_ml;        // [2 W][kRowTile][2]: reference (a raw score), sum
     float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
     int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
     int W;
     int tile_cost;         // what a row tile costs beside its positions, in positions
     uint32_t inv_p, inv_g; // 2^32 / P and 2^32 / G, at most 2^32 - 1
-    float scale_log2;
+    float scale_log2, move_at;      // scale in units of log2 e; raw scores by which a reference is exceeded before it moves, 8 / scale_log2
     int64_t max_ctx;
 };
 

@@ -237,11 +237,13 @@ void prompt_tile_kernel(PromptArgs a) {
             // ---- softmax ------------------------------------------------------------------------------------
             f32x16 s_a, s_b = {};
             uint32_t pk[8];
-            float m_use = 0.f, alpha = 1.f;
-            // The exponent reference for tile u's scores; it moves only when a maximum exceeds it by more than 8 (in units of log2 e: probabilities stay
-            // below 2^8, which bf16 and fp32 hold as well as any), so that outputs are seldom rescaled.
-            float mx = 0.f;
-            auto reference = [&](auto partc, const f32x16& s) __attribute__((always_inline)) {
+            // The exponent reference of a row: a score near its highest so far.  It moves only when a score exceeds it by more than 8 in units of log2 e
+            // (probabilities stay below 2^8, which bf16 and fp32 hold as well as any), so that outputs are seldom rescaled and the arithmetic of a move stands in a
+            // branch.  m_run: the reference as a raw score; m_use: scaled, what a scaled score is taken from in one fma.  The fma takes the unrounded product from the
+            // rounded reference: from 2^30 on what is left is no longer small, and the raw reference is taken from the scores first (far).
+            float m_use = 0.f, alpha = 1.f, mx = 0.f;
+            bool moved = false, far = false;        // uniform: alpha is not 1 for some row
+            auto highest = [&](auto partc, const f32x16& s) __attribute__((always_inline)) {
                 constexpr int part = decltype(partc)::value;
                 if constexpr (part == 0) {
                     mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
@@ -251,12 +253,24 @@ void prompt_tile_kernel(PromptArgs a) {
 #pragma unroll
                     for (int i = 9; i < 15; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
                     mx = fmaxf(mx, s[15]);
-                } else if constexpr (part == 2) {
-                    mx = max_across_halves(mx) * a.scale_log2;
                 } else {
-                    m_use = mx > m_run + 8.f ? mx : m_run;
-                    alpha = fast_exp2(m_run - m_use);
-                    m_run = m_use;
+                    mx = max_across_halves(mx);
+                }
+            };
+            auto reference = [&](f32x16& s) __attribute__((always_inline)) {
+                const bool moves = mx > m_run + a.move_at;
+                moved = __any(moves);
+                if (moved) {
+                    const float m_new = moves ? mx : m_run;
+                    alpha = fast_exp2((m_run - m_new) * a.scale_log2);
+                    m_run = m_new;
+                    m_use = m_new == kNoScore ? 0.f : m_new * a.scale_log2;
+                    far = far || __any(fabsf(m_use) > 1073741824.f);
+                }
+                if (far) {
+                    m_use = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] -= m_run;
                 }
             };
             // -inf into the scores of tile u that this lane's row does not see
@@ -354,7 +368,8 @@ void prompt_tile_kernel(PromptArgs a) {
                 }, std::make_integer_sequence<int, S::kPv>{});
             };
             auto rescale = [&]() __attribute__((always_inline)) {
-                if (__any(alpha != 1.f)) {
+                if (moved) {
+                    l_run *= alpha;
 #pragma unroll
                     for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
@@ -416,11 +431,10 @@ void prompt_tile_kernel(PromptArgs a) {
                     __builtin_amdgcn_sched_barrier(0);
                 }, std::make_integer_sequence<int, S::kKSteps>{});
                 if constexpr (PREV) {
-                    l_run *= alpha;
                     rescale();
                     __builtin_amdgcn_sched_barrier(0);
                     product(beforec, v_shift, [&](auto mc) __attribute__((always_inline)) {
-                        // beside the first half the other probabilities, which the second half takes; beside that the reference of tile u
+                        // beside the first half the other probabilities, which the second half takes; beside that the highest scores of tile u
                         constexpr int m = decltype(mc)::value, kHalf = S::kDTiles;
                         if constexpr (m < kHalf) {
                             constexpr int e0 = kEarly + (16 - kEarly) * m / kHalf, e1 = kEarly + (16 - kEarly) * (m + 1) / kHalf;
@@ -428,15 +442,16 @@ void prompt_tile_kernel(PromptArgs a) {
                                        std::make_integer_sequence<int, e1 - e0>{});
                         }
                         if constexpr (m == kHalf) l_run = add_bf16_pair(pk[7], psum) + l_run;
-                        constexpr int r0 = m < kHalf ? 0 : 4 * (m - kHalf) / kHalf, r1 = m < kHalf ? 0 : 4 * (m + 1 - kHalf) / kHalf;
+                        constexpr int r0 = m < kHalf ? 0 : 3 * (m - kHalf) / kHalf, r1 = m < kHalf ? 0 : 3 * (m + 1 - kHalf) / kHalf;
                         if constexpr (!MASK && r1 > r0)
-                            each_index([&](auto rc) __attribute__((always_inline)) { reference(I<r0 + decltype(rc)::value>{}, s_new); },
+                            each_index([&](auto rc) __attribute__((always_inline)) { highest(I<r0 + decltype(rc)::value>{}, s_new); },
                                        std::make_integer_sequence<int, r1 - r0>{});
                     });
                     if constexpr (EDGE) add_left(u - 1);
                 }
                 if constexpr (MASK) mask(u, s_new);
-                if constexpr (MASK || !PREV) each_index([&](auto ic) __attribute__((always_inline)) { reference(ic, s_new); }, std::make_integer_sequence<int, 4>{});
+                if constexpr (MASK || !PREV) each_index([&](auto ic) __attribute__((always_inline)) { highest(ic, s_new); }, std::make_integer_sequence<int, 3>{});
+                reference(s_new);
             };
 
             // the first tiles: K of 0, 1, 2 and V of 0, 1, in the order in which steps -3, -2, -1 would request them
@@ -489,8 +504,8 @@ void prompt_tile_kernel(PromptArgs a) {
             __builtin_amdgcn_sched_barrier(0);
             psum = 0.f;
             each_index([&](auto ec) __attribute__((always_inline)) { probability(ec, s_a); }, std::make_integer_sequence<int, 16>{});
-            l_run = l_run * alpha + add_bf16_pair(pk[7], psum);
             rescale();
+            l_run += add_bf16_pair(pk[7], psum);
             __builtin_amdgcn_sched_barrier(0);
             product(I<0>{}, shift, [](auto) {});
             add_left(n_tiles - 1);
@@ -560,7 +575,7 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs 
 #pragma unroll 4
     for (int k = 0; k < cut.pieces; ++k) {
         const float mk = a.part_ml[2 * (slot(k) * kRowTile + r)], lk = a.part_ml[2 * (slot(k) * kRowTile + r) + 1];
-        const float f = fast_exp2(mk - m);
+        const float f = fast_exp2((mk - m) * a.scale_log2);
         const f32x4 v = *(reinterpret_cast<const f32x4*>(a.part_acc) + slot(k) * kVectors + e);
         l = fmaf(lk, f, l);
 #pragma unroll
@@ -668,6 +683,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W, a.tile_cost = seer::prompt_tile_cost(p->Dqk);
     a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.scale_log2 = p->scale * seer::kLog2e;
+    a.move_at = a.scale_log2 > 1e-36f ? 8.f / a.scale_log2 : 8e36f;
     a.max_ctx = static_cast<int64_t>(p->max_pages_per_seq) * p->page_size;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     hipError_t err = hipErrorInvalidValue;

@@ -248,29 +248,41 @@ void prompt_latent_kernel(PromptArgs a) {
                 const int st = lds_base + stage_off;
                 va[0] = st + v_even, va[1] = st + v_even8, va[2] = st + v_odd, va[3] = st + v_odd8;
             };
-            float m_use = 0.f, mx_part = 0.f;
-            auto reference = [&](auto ic, const f32x16& sc) __attribute__((always_inline)) {
+            // (references as in the kernel for separate pools; the move itself stands behind the product, where no read is in flight)
+            float m_use = 0.f, mx = 0.f;
+            bool moved = false, far = false;
+            auto highest = [&](auto ic, const f32x16& sc) __attribute__((always_inline)) {
                 constexpr int part = decltype(ic)::value;
                 if constexpr (part == 0) {
-                    mx_part = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
+                    mx = fmaxf(fmaxf(sc[0], sc[1]), sc[2]);
 #pragma unroll
-                    for (int i = 3; i < 9; i += 2) mx_part = fmaxf(fmaxf(mx_part, sc[i]), sc[i + 1]);
-                    SEER_MLA_PIN(mx_part);
+                    for (int i = 3; i < 9; i += 2) mx = fmaxf(fmaxf(mx, sc[i]), sc[i + 1]);
+                    SEER_MLA_PIN(mx);
                 } else if constexpr (part == 1) {
 #pragma unroll
-                    for (int i = 9; i < 15; i += 2) mx_part = fmaxf(fmaxf(mx_part, sc[i]), sc[i + 1]);
-                    mx_part = fmaxf(mx_part, sc[15]);
-                    SEER_MLA_PIN(mx_part);
-                } else if constexpr (part == 2) {
-                    mx_part = max_across_halves(mx_part) * a.scale_log2;
-                    SEER_MLA_PIN(mx_part);
+                    for (int i = 9; i < 15; i += 2) mx = fmaxf(fmaxf(mx, sc[i]), sc[i + 1]);
+                    mx = fmaxf(mx, sc[15]);
+                    SEER_MLA_PIN(mx);
                 } else {
-                    m_use = mx_part > m_run + 8.f ? mx_part : m_run;
-                    alpha = fast_exp2(m_run - m_use);
-                    m_run = m_use;
-                    SEER_MLA_PIN(m_use);
-                    SEER_MLA_PIN(alpha);
-                    SEER_MLA_PIN(m_run);
+                    mx = max_across_halves(mx);
+                    SEER_MLA_PIN(mx);
+                }
+            };
+            auto reference = [&](f32x16& sc) __attribute__((always_inline)) {
+                const bool moves = mx > m_run + a.move_at;
+                moved = __any(moves);
+                alpha = 1.f;
+                if (moved) {
+                    const float m_new = moves ? mx : m_run;
+                    alpha = fast_exp2((m_run - m_new) * a.scale_log2);
+                    m_run = m_new;
+                    m_use = m_new == kNoScore ? 0.f : m_new * a.scale_log2;
+                    far = far || __any(fabsf(m_use) > 1073741824.f);
+                }
+                if (far) {
+                    m_use = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) sc[i] -= m_run;
                 }
             };
             u32x2 vr[kVAhead][2];
@@ -283,7 +295,7 @@ void prompt_latent_kernel(PromptArgs a) {
                         apply_mask(j + 1, sc_next);
                     }
                 }
-                if (__any(alpha != 1.f)) {
+                if (moved) {
                     mfma_drain();
 #pragma unroll
                     for (int dt = 0; dt < kDTiles; ++dt) {
@@ -299,10 +311,11 @@ void prompt_latent_kernel(PromptArgs a) {
                 constexpr int kRefFirst = 4;
                 phase_b(va, vr, pk, acc, [&](auto ic) __attribute__((always_inline)) {
                     constexpr int m = decltype(ic)::value;
-                    if constexpr (NEXT && m >= kRefFirst && (m - kRefFirst) % 2 == 0 && (m - kRefFirst) / 2 < 4)
-                        reference(std::integral_constant<int, (m - kRefFirst) / 2>{}, sc_next);
+                    if constexpr (NEXT && m >= kRefFirst && (m - kRefFirst) % 2 == 0 && (m - kRefFirst) / 2 < 3)
+                        highest(std::integral_constant<int, (m - kRefFirst) / 2>{}, sc_next);
                     prepare(ic);
                 });
+                if constexpr (NEXT) reference(sc_next);
             };
             using yes = std::true_type;
             using no = std::false_type;
@@ -343,7 +356,8 @@ void prompt_latent_kernel(PromptArgs a) {
             phase_a<true, false>(ka, qt, qreg, s_a, s_b, pk, m_use, l_run, alpha, a.scale_log2, va, vr, next_load, nothing);
             mfma_drain();
             apply_mask(0, s_a);
-            for_each_index([&](auto ic) __attribute__((always_inline)) { reference(ic, s_a); }, std::make_integer_sequence<int, 4>{});
+            for_each_index([&](auto ic) __attribute__((always_inline)) { highest(ic, s_a); }, std::make_integer_sequence<int, 3>{});
+            reference(s_a);
             prepare_next(std::integral_constant<int, 14>{});
             prepare_next(std::integral_constant<int, 18>{});
             for (u = 1; u + 1 < n_tiles;) {
