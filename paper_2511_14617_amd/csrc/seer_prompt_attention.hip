@@ -239,8 +239,9 @@ void prompt_tile_kernel(PromptArgs a) {
             uint32_t pk[8];
             // The exponent reference of a row: a score near its highest so far.  It moves only when a score exceeds it by more than 8 in units of log2 e
             // (probabilities stay below 2^8, which bf16 and fp32 hold as well as any), so that outputs are seldom rescaled and the arithmetic of a move stands in a
-            // branch.  m_run: the reference as a raw score; m_use: scaled, what a scaled score is taken from in one fma.  The fma takes the unrounded product from the
-            // rounded reference: from 2^30 on what is left is no longer small, and the raw reference is taken from the scores first (far).
+            // branch.  m_run: the reference as a raw score; m_use: scaled, what is taken from a scaled score in one fma.  m_use is rounded, which no other tile
+            // or piece knows of: up to 2^10 that is 2^-15 at most in the exponent, far below the probabilities' own rounding; beyond, the raw reference is taken from the
+            // raw scores first (far).
             float m_use = 0.f, alpha = 1.f, mx = 0.f;
             bool moved = false, far = false;        // uniform: alpha is not 1 for some row
             auto highest = [&](auto partc, const f32x16& s) __attribute__((always_inline)) {
@@ -265,7 +266,7 @@ void prompt_tile_kernel(PromptArgs a) {
                     alpha = fast_exp2((m_run - m_new) * a.scale_log2);
                     m_run = m_new;
                     m_use = m_new == kNoScore ? 0.f : m_new * a.scale_log2;
-                    far = far || __any(fabsf(m_use) > 1073741824.f);
+                    far = far || __any(fabsf(m_use) > 1024.f);
                 }
                 if (far) {
                     m_use = 0.f;

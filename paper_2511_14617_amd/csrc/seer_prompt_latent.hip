@@ -277,7 +277,7 @@ void prompt_latent_kernel(PromptArgs a) {
                     alpha = fast_exp2((m_run - m_new) * a.scale_log2);
                     m_run = m_new;
                     m_use = m_new == kNoScore ? 0.f : m_new * a.scale_log2;
-                    far = far || __any(fabsf(m_use) > 1073741824.f);
+                    far = far || __any(fabsf(m_use) > 1024.f);
                 }
                 if (far) {
                     m_use = 0.f;

@@ -171,6 +171,33 @@ def test_scores_far_below_zero(heads):
     compare(out, plain(c))
 
 
+@pytest.mark.parametrize("base", [2.0 ** 23, -2.0 ** 23, 2.0 ** 11])
+@pytest.mark.parametrize("heads", [(8, 1, 128, 128, 16), (4, 1, 64, 64, 20), (16, 1, 576, 512, 64)])
+def test_small_differences_of_scores_far_from_zero(heads, base):
+    """Scores of base + 0 .. 11, rising with the position and exact in fp32, values of 1 and -1 in turn: what is rounded on the way to the exponential may not be
+    rounded at the size of the scores, and pieces of one row, whose references differ, have to agree on it."""
+    c = make(27, [40, 3], [4000, 2500], *heads)
+    D, Dv = heads[2], heads[3]
+    c["scale"] = 1.0
+    c["q"].zero_()
+    c["q"][..., D - 2], c["q"][..., D - 1] = 2.0 ** 11, 1.0
+    c["k"][..., D - 2:] = 0
+    for b, L in enumerate(c["ctx"].tolist()):
+        j = torch.arange(L)
+        at = c["table"][b, j // c["page"]].long(), 0, j % c["page"]
+        k = c["k"][at]
+        k[:, D - 2], k[:, D - 1] = base / 2 ** 11, (j * 12 // L).bfloat16()
+        c["k"][at] = k
+        value = (1.0 - 2.0 * (j * 12 // L % 2)).bfloat16()[:, None].expand(L, Dv)
+        if c["v"] is None:
+            k[:, :Dv] = value
+            c["k"][at] = k
+        else:
+            c["v"][at] = value
+    out, _ = call(c)
+    compare(out, plain(c))
+
+
 def spoil(x, b, j, c, value, dims=slice(None)):
     x[c["table"][b, j // c["page"]].long(), :, j % c["page"], dims] = value
 
