@@ -7,7 +7,8 @@
 //
 // What bounds it: HBM.  2 bytes read and 2 written per component, nothing read twice.  A workgroup takes the heads of a few tokens: it makes
 // the tokens' sines and cosines once (R / 2 of them a token, in LDS) and then moves 16-byte chunks; a thread of the rotated part takes
-// both chunks whose components belong together, so q_out may be q.
+// both chunks whose components belong together, so q_out may be q.  16 384 tokens on 64/8 heads of 128: 131 us, 5.1 TB/s; 4096 on 128 heads of 576
+// 235 us, 5.2 TB/s (a large copy: 4.9).  576 tokens: 10.9 us, a launch, two loads that wait for one another and a read and write of 41 KB a token.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -208,7 +209,8 @@ extern "C" int seer_kv_append(const seer_append_params* p, const void* q, const 
     auto reciprocal = [](int d) { return static_cast<uint32_t>(((uint64_t{1} << 32) + d - 1) / d); };     // (d = 1: not looked at)
     a.inv_qk = reciprocal(a.jobs_qk), a.inv_v = reciprocal(a.jobs_v);
     // Small tokens are taken up to four at a time where there are enough of them, large ones shared by several workgroups, as long as a thread has its
-    // jobs in flight.
+    // jobs in flight.  With one | two | four tokens: 16 384 tokens on 8/1 heads of 128 33.6 | 24.2 | 18.9 us (four taken), on 64/8 128.7 | 131.5 | 136.5 (one), 1500 on 64/8
+    // 11.6 | 12.8 | 13.8 (one); calls of a few hundred are alike.
     a.tokens = 1, a.parts = 1;
     while (a.tokens < seer::kAppendTokens && a.tokens * a.jobs < seer::kJobsWanted && p->n_tokens / (2 * a.tokens) >= seer::kManyBlocks) a.tokens *= 2;
     if (a.tokens == 1) a.parts = (a.jobs + 2 * seer::kJobsWanted - 1) / (2 * seer::kJobsWanted);

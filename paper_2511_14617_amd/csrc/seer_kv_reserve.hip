@@ -10,8 +10,9 @@
 //   pages   the free pages of every piece of the pool, in order (and the sums over the rows)
 //   give    a thread per new token finds its row, its page, its slot; the thread of a page's first position writes the page's
 //           entries, so tables and references cost no pass of their own
-// Pools of up to kSmallPages pages take one workgroup and one launch, in which a barrier separates the phases; beyond that they are three
-// launches.
+// Calls of up to kSmallPages pages, kSmallRows rows and some thousand tokens take one workgroup and one launch, in which a barrier separates the
+// phases and the pages' counts stay as bits in LDS: 64 rows of 9 tokens, 16 384 pages, 11.9 us.  Beyond that they are three launches, 6.3 + 5.0 + 5.3 us for
+// 512 rows and 327 680 pages, 10.6 + 5.5 + 6.3 for 64 whole prompts and a million pages (4 MB): each is a launch and three or four loads that wait for one another.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -432,7 +433,12 @@ static int check_reserve_params(const seer_reserve_params* p) {
     if (static_cast<int64_t>(p->max_pages_per_seq) * p->page_size > 0x7fffffffLL) return SEER_ESHAPE;
     return SEER_OK;
 }
-inline bool reserve_is_small(const seer_reserve_params& p) { return p.num_pages <= kSmallPages && p.B <= kSmallRows && p.n_tokens <= kSmallTokens; }
+// One workgroup against three launches, calls with their host part: 8 rows of a token in 1024 pages 12.8 | 18.8 us, 64 of 9 in 16 384 13.0 | 19.5; in 32 768 pages,
+// 1000 of 1 14.2 | 19.4, 8 of 1000 16.7 | 19.7, 256 of 30 19.3 | 19.1, 500 of 8 16.8 | 19.6, of 16 21.1 | 19.5, 1000 of 4 17.5 | 19.4, of 6 20.1 | 19.5: a pass over 1024
+// tokens costs more where they are of many rows.
+inline bool reserve_is_small(const seer_reserve_params& p) {
+    return p.num_pages <= kSmallPages && p.B <= kSmallRows && p.n_tokens <= (p.B <= kSmallRows / 4 ? kSmallTokens : kSmallTokens * 5 / 8);
+}
 struct ReserveLayout {
     int piece, pieces;
     size_t off_start, off_counts, off_list, total;

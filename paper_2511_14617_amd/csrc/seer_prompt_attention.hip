@@ -1,11 +1,26 @@
 // Causal attention of packed tokens over the paged cache, separate K and V pools: (64, 64), (128, 128), (192, 128) and (256, 256),
 // pages of any size.
 //
+// out = sum_j p_j V_j / sum_j p_j, p_j = exp(scale q.K_j - m) over the positions j that a token sees (those before it and itself), in one pass: a
+// running reference m, sums and outputs in fp32.  Positions that no row of the tile sees are not read, a cached row is read once per row tile.
+//
 // Workgroup = 4 waves = a row tile of 128 query rows of one KV head, 32 rows a wave; the work is cut into equal stretches of a line
-// of row tiles (seer_prompt.h).  A tile of 32 positions goes HBM/L2 -> LDS directly, K rows then V rows, two stages; S^T = K.Q^T
-// leaves a query row to a lane, so its softmax needs one exchange between two lanes, and the probabilities are, packed to bf16, the
-// operand of O^T += V^T.P^T as they are.  Running maximum and sum: one pass over the positions.  Positions that no row of the tile sees are not
-// read; a wave whose rows see nothing of a tile does not compute it; only tiles that some row does not see whole are masked.
+// of row tiles (seer_prompt.h).  A tile of 32 positions goes HBM/L2 -> LDS directly into rings of four tiles, three of them in flight.  S^T = K.Q^T
+// leaves a query row to a lane pair, so its softmax needs one exchange between two lanes, and the probabilities are, packed to bf16 (the matrix
+// operand's type; the sum is taken of the rounded values, so what is common cancels), the operand of O^T += V^T.P^T as they are.
+//
+// Neighbouring tiles run side by side: behind every MFMA of the scores of tile u stand a K read for a later one and a few of tile u - 1's probabilities,
+// behind those of its product with V the rest of them and the highest scores of tile u.  Before that, scores, softmax and product of a tile one
+// after the other, one prompt of 32 768 tokens on 8/1 heads of 128 took 3.09 ms; side by side 2.67; with the arithmetic pinned beside its
+// MFMA 2.53; with waits and loads without conditions and descriptors in scalar registers 2.25; with today's shares of the line 2.17 (1015 TFLOP/s, where an
+// 8192^3 bf16 library product reaches 1378).
+//
+// What bounds it: the power that matrix cores, LDS and vector ALU take together.  In that prompt the matrix cores are busy 56 % of the cycles, vector
+// instructions 47 %, LDS 30 % (0.15 % of it conflicts), at 1.79 GHz instead of 2.4, and every change that saved cycles lowered the clock by nearly as much:
+// without the exponentials the time is 1 % less, without tile loads 13 to 19, without the product with V 15.  Earlier K reads, loads in the shadow of the scores'
+// MFMAs, other shares of probabilities, wave priorities changed nothing.  Requests of one token are bound by HBM: 64 of 16 384 positions on
+// 8 KV heads read 4.8 TB/s, though 28 of the 32 rows of a wave and three of four waves have nothing to do (loads that stream past the
+// caches gain 4 % there and cost prompts 30 %, which share what they read: not used).
 //
 // Infinities and NaN: scores of positions that a row does not see are replaced by selection.  In the product with V a position's row is
 // multiplied into all query rows, so in tiles with masked positions V rows that hold an infinity or NaN are taken out and added to the rows that see
@@ -33,7 +48,8 @@ struct PromptShape {
     static constexpr int kKLoads = kKSlot / 4096, kVLoads = kVSlot / 4096;   // of 1 KB, per wave and tile
     static constexpr int kKAhead = kKSteps < 8 ? kKSteps : 8;                // K operands requested ahead of their MFMA
     static constexpr int kVAhead = kPv < 8 ? kPv : 8;                        // V operands (two reads each)
-    // waves that a SIMD holds, by registers: queries, outputs, scores of two tiles, operands
+    // Waves that a SIMD holds, by registers (queries, outputs, scores of two tiles, operands) and LDS.  Heads of 192/128 with one: 531 us for four sequences
+    // of 4096 on 16 heads, with two 431.
     static constexpr int kWavesPerSimd = DQK <= 64 ? 3 : (DQK <= 192 ? 2 : 1);
     static_assert(kKSlot % 4096 == 0 && kVSlot % 4096 == 0 && kLds <= 156 * 1024, "");
 };
@@ -601,6 +617,7 @@ static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
 
 template <int DQK, int DV>
 static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
+    // (pages of 16 through the form for any page, against their own: one prompt of 32 768 tokens on 8/1 heads 2553 | 2162 us, heads of 256 439 | 348, 64 253 | 226)
     if (a.P % 16 == 0) hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     else hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, true>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
@@ -609,7 +626,9 @@ static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
-// What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.
+// What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.  Measured, with 1 | 128 | 256 | 384 | 512:
+// heads of 64, 12 prompts of up to 6000 tokens 289 | 248 | 250 | 259 | 266 us; of 128, 16 prompts of up to 8192 4175 | 3499 | 3253 | 3297 | 3411; of 256, four
+// of 4096 531 | 392 | 346 | 353 | 358; shared latent, four pieces of up to 2048 2269 | 1667 | 1498 | 1482 | 1491.
 constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 384); }
 static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (!p) return SEER_EINVAL;

@@ -79,7 +79,7 @@ class Server:
                 self.len[b] = step[b]
 
 
-# (pools of up to 32 768 pages, 1024 rows and 8192 tokens take one workgroup)
+# (pools of up to 32 768 pages, 1024 rows and 8192 tokens, 5120 of more than 256 rows, take one workgroup)
 @pytest.mark.parametrize("seed,B,pages,width,page,longest", [
     (1, 1, 3, 3, 16, 40), (2, 7, 40, 9, 16, 100), (3, 33, 200, 12, 1, 12), (4, 64, 5000, 60, 16, 700), (5, 5, 64, 30, 7, 150),
     (6, 130, 32768, 100, 4, 60), (7, 65, 32769, 40, 16, 300), (8, 40, 70000, 300, 3, 700), (9, 1025, 4000, 8, 16, 10), (10, 300, 2500, 50, 20, 900)])
@@ -87,6 +87,14 @@ def test_steps_of_a_server(seed, B, pages, width, page, longest):
     server = Server(seed, B, pages, width, page)
     for k in range(6):
         server.step(longest, pad=(0, 5, 0, 300, 1, 0)[k])
+
+
+@pytest.mark.parametrize("B,tokens", [(256, 8192), (256, 8193), (257, 5120), (257, 5121)])
+def test_as_many_tokens_as_one_workgroup_takes(B, tokens):
+    page, each = 16, tokens // B
+    new = [each + (b < tokens - each * B) for b in range(B)]
+    want = check([[0] * 4 for _ in range(B)], [0] * B, [0] * 1000, [0] * B, new, None, None, tokens, page)
+    assert want[7] == 0 and want[4][-1] == tokens
 
 
 @pytest.mark.parametrize("pages", [64, 40000])
