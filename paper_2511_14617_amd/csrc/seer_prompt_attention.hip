@@ -15,7 +15,7 @@
 // MFMA 2.53; with waits and loads without conditions and descriptors in scalar registers 2.25; with today's shares of the line 2.17 (1015 TFLOP/s, where an
 // 8192^3 bf16 library product reaches 1378).
 //
-// What bounds it: the power that matrix cores, LDS and vector ALU take together.  In that prompt the matrix cores are busy 56 % of the cycles, vector
+// What bounds it: the power that matrix cores, LDS and vector ALU take together.  In that prompt the matrix cores are busy 56 % of the time, vector
 // instructions 47 %, LDS 30 % (0.15 % of it conflicts), at 1.79 GHz instead of 2.4, and every change that saved cycles lowered the clock by nearly as much:
 // without the exponentials the time is 1 % less, without tile loads 13 to 19, without the product with V 15.  Earlier K reads, loads in the shadow of the scores'
 // MFMAs, other shares of probabilities, wave priorities changed nothing.  Requests of one token are bound by HBM: 64 of 16 384 positions on

@@ -4,14 +4,14 @@
 // What bounds it: the matrix cores at the clock that the power limit leaves them, and what one wave per SIMD issues between their instructions
 // (about 1200 flop per byte of a tile).  A workgroup of four waves takes 128 query rows; a tile of 32 positions (36 KB) goes HBM/L2 -> LDS
 // directly, three stages; the scores of tile u run beside the softmax of tile u - 1, then its product with V beside the highest scores of tile u.  Four
-// pieces of 256 .. 2048 tokens on 128 heads: 1.5 ms, 980 TFLOP/s; matrix cores busy 53 % of the cycles, LDS 34 % without conflicts.  With 128
+// pieces of 256 .. 2048 tokens on 128 heads: 1.5 ms, 980 TFLOP/s; matrix cores busy 49 % of the time, LDS 34 % without conflicts.  With 128
 // heads a row tile is one token, and neighbouring row tiles read the same latents: the stretches of one XCD are neighbours on the line.
 // Queries and outputs (276 KB a row tile) pass through LDS, the outputs in a loop: unrolled they were 6 KB of code, fetched anew for every row tile
 // (with that and row tiles counted without a fixed cost 2.10 ms).
 //
 // Infinities and NaN in positions that some row of the tile does not see: scores by selection; the value rows are taken out of LDS once
-// all waves have the tile's scores.  A row that sees such a latent has it in its score as well, which is then NaN or +inf and makes the whole row NaN, or -inf
-// and gives the position no weight.
+// all waves have the tile's scores.  A row that sees such a latent has it in its score as well, which is then NaN or +inf and makes the whole row NaN, or -inf:
+// 0 times the latent, which is added at the end.
 #include "seer_device.h"
 #include "seer_mla.h"
 #include "seer_prompt.h"
@@ -29,6 +29,8 @@ void prompt_latent_kernel(PromptArgs a) {
     __shared__ __attribute__((aligned(16))) u32x4 q_tail[kWaves][kQLdsSteps][kWave];      // (see the verify kernel)
     __shared__ PromptLds s_plan;
     __shared__ uint32_t s_found;                    // positions with infinities or NaN in the scanned tile's values
+    constexpr int kEdgeTiles = 8;                   // (that some row does not see whole: 128 tokens at most touch six)
+    __shared__ uint32_t s_left[kWaves][kEdgeTiles]; // the positions left out, by tile (each wave its own copy)
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5, l16 = lane >> 4, p16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -105,6 +107,7 @@ void prompt_latent_kernel(PromptArgs a) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[dt][i] = 0.f;
         float m_run = kNoScore, l_run = 0.f, alpha = 1.f;
+        bool any_left = false;                      // uniform
         __syncthreads();                            // every wave is done with the stages of the piece before
         if (n_tiles > 0) {
             // Queries through LDS: a wave's 32 rows lie there as a tile does (waves 0 to 2 in the stages, wave 3 in the parked part), so that they are
@@ -197,6 +200,7 @@ void prompt_latent_kernel(PromptArgs a) {
             uint32_t pk[8];
             // positions of the tile before, and of this one, whose values are kept out of the product (uniform)
             uint32_t left_prev = 0, left_cur = 0;
+            if (lane < kEdgeTiles) *const_cast<volatile uint32_t*>(&s_left[wave][lane]) = 0;
             auto step_top = [&](int u) __attribute__((always_inline)) {
                 wait_vmcnt<0>();
                 bare_barrier();                     // tile u has landed for every wave, every wave has the scores of tile u - 1
@@ -221,6 +225,11 @@ void prompt_latent_kernel(PromptArgs a) {
                     __builtin_amdgcn_s_waitcnt(0xc07f);
                     bare_barrier();
                     left_cur = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_found));
+                    if (left_cur) {
+                        const int edge = u0 + u - (all_see + 1) / kTile;
+                        if (edge < kEdgeTiles) *const_cast<volatile uint32_t*>(&s_left[wave][edge]) = left_cur;
+                        any_left = true;
+                    }
                 }
                 if (left_prev) {
 #pragma unroll 1
@@ -389,6 +398,26 @@ void prompt_latent_kernel(PromptArgs a) {
             mfma_drain();
         }
 
+        // Positions that were left out, for the rows that see them: the probability is 0, or the row is NaN already, so what is added to component d is 0 times the
+        // latent's.  each(latent, the last position that does not see it): for every one of them.
+        auto left_out = [&](auto&& each) __attribute__((always_inline)) {
+            const int32_t* table = a.block_table + static_cast<size_t>(t.b) * a.max_pages;
+#pragma unroll 1
+            for (int e = 0; e < kEdgeTiles; ++e) {
+                uint32_t words = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(&s_left[wave][e]));
+#pragma unroll 1
+                for (; words; words &= words - 1) {
+                    const int position = ((all_see + 1) / kTile + e) * kTile + __builtin_ctz(words), lp = page_of(position);
+                    const int pg = min(max(table[min(lp, a.max_pages - 1)], 0), a.num_pages - 1);
+                    each(reinterpret_cast<const uint16_t*>(a.k_pages) + ((static_cast<size_t>(pg) * a.Hkv + t.kvh) * a.P + (position - lp * a.P)) * (kRowBytes / 2), position);
+                }
+            }
+        };
+        auto add_zero_times = [](const uint16_t* latent, f32x4& o) __attribute__((always_inline)) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(latent);
+            o[0] = fmaf(0.f, bf16lo_to_f32(v[0]), o[0]), o[1] = fmaf(0.f, bf16hi_to_f32(v[0]), o[1]);
+            o[2] = fmaf(0.f, bf16lo_to_f32(v[1]), o[2]), o[3] = fmaf(0.f, bf16hi_to_f32(v[1]), o[3]);
+        };
         // ---- the row tile's output, or this piece's share of it ------------------------------------------
         const float l_tot = l_run + __shfl_xor(l_run, 32, kWave);
         if (begins && (ends || t.r.bad)) {
@@ -414,7 +443,15 @@ void prompt_latent_kernel(PromptArgs a) {
                             f32x4{o[i4 * 4], o[i4 * 4 + 1], o[i4 * 4 + 2], o[i4 * 4 + 3]};
                     }
                 __builtin_amdgcn_wave_barrier();
-#pragma unroll 8
+                if (any_left) {
+                    left_out([&](const uint16_t* latent, int position) __attribute__((always_inline)) {
+#pragma unroll 1
+                        for (int r = 0; r < rows_here; ++r)
+                            if (__builtin_amdgcn_readlane(sees, r) >= position)
+                                add_zero_times(latent + part * kPart + l * 4, *reinterpret_cast<f32x4*>(mine + r * (kPart * 4) + ((l ^ r) << 4)));
+                    });
+                    __builtin_amdgcn_wave_barrier();
+                }
                 for (int r = 0; r < rows_here; ++r) {
                     const f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * (kPart * 4) + ((l ^ r) << 4));
                     const uint32_t to = __builtin_amdgcn_readlane(q_row, r);
@@ -437,6 +474,16 @@ void prompt_latent_kernel(PromptArgs a) {
         for (int dt = 0; dt < kDTiles; ++dt)
 #pragma unroll
             for (int i4 = 0; i4 < 4; ++i4) po[(dt * 4 + i4) * kWave] = f32x4{acc[dt][i4 * 4], acc[dt][i4 * 4 + 1], acc[dt][i4 * 4 + 2], acc[dt][i4 * 4 + 3]};
+        if (any_left)
+            left_out([&](const uint16_t* latent, int position) __attribute__((always_inline)) {
+                if (sees < position) return;
+#pragma unroll 1
+                for (int i = 0; i < kDTiles * 4; ++i) {
+                    f32x4 o = po[i * kWave];
+                    add_zero_times(latent + i * 8 + lg * 4, o);
+                    po[i * kWave] = o;
+                }
+            });
     }
     if (a.status && __any(bad_page) && lane == 0) atomicOr(a.status, 2);
 }

@@ -260,6 +260,24 @@ def test_a_latent_that_is_not_finite_in_one_component(page):
     assert torch.equal(out[30:, :, keep], ref[30:, :, keep])
 
 
+@pytest.mark.parametrize("page", [64, 20])
+@pytest.mark.parametrize("past", [10, 5000])
+def test_zero_times_an_infinite_latent(page, past):
+    """The same position in a tile that all rows see and in one that some see, for whole row tiles and cut ones: 0 * inf in the component, as in the formula."""
+    c = make(15, [160], [past], 16, 1, 576, 512, page, std=0.5)
+    c["q"][..., 7] = c["q"][..., 7].abs() + 0.01
+    c["q"][..., 300] = c["q"][..., 300].abs() + 0.01
+    good, _ = call(c)
+    spoil(c["k"], 0, past + 70, c, -float("inf"), 7)
+    spoil(c["k"], 0, past + 73, c, -float("inf"), 300)
+    out, _ = call(c)
+    for component, first in ((7, 70), (300, 73)):
+        assert torch.equal(out[:70, :, component], good[:70, :, component])      # (behind it the weights are without position 70)
+        assert torch.isfinite(out[:first, :, component]).all() and torch.isnan(out[first:, :, component]).all()
+    keep = [d for d in range(512) if d not in (7, 300)]
+    assert torch.isfinite(out[..., keep]).all()
+
+
 def test_scores_of_nothing_but_minus_infinity_give_zeros():
     c = make(9, [40], [0], 4, 2, 128, 128, 16)
     c["q"][:, 1] = 0
