@@ -1,9 +1,9 @@
 // Work of the prompt attention kernels: how packed tokens of requests of any length are cut into equal shares, on the device.
 //
 // Rows: a request's n tokens times the G heads that share a KV head are n G consecutive query rows (row r = token r / G, head r % G), cut into
-// row tiles of kRowTile.  A row tile reads the positions that its last row sees, so its cost grows along a prompt: with past = ctx - n
+// row tiles of 128 (or 256).  A row tile reads the positions that its last row sees, so its cost grows along a prompt: with past = ctx - n
 // cached positions before the new ones, row tile i of a request costs (in units of a position times a head of the group)
-//     c_i = G (past + tile_cost) + kRowTile (i + 1),     i < R = ceil(n G / kRowTile).
+//     c_i = G (past + tile_cost) + 128 (i + 1),     i < R = ceil(n G / 128).
 // All row tiles -- requests in order, their KV heads in order, their row tiles in order -- lie end to end on one line, whose
 // prefix sums have closed forms in i and in the KV head, and whose sums over requests are one scan.  Workgroup w of W takes the stretch from
 // x_w = total w / W to x_(w+1): equal work whatever the mix of lengths, one launch, no queue.
@@ -19,8 +19,8 @@
 
 namespace seer {
 
-constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves
-constexpr int kPromptThreads = 256;
+constexpr int kRowTile = 128;          // query rows of a workgroup: 32 of each of its four waves (twice that where it has eight)
+constexpr int kPromptThreads = 256, kMostPromptThreads = 512;
 // The exponent reference of a row that has seen no finite score: the lowest float, which no finite score is below.  Every difference of references is then a
 // number or -inf, and a row that stays without a score asks for no rescaling.
 constexpr float kNoScore = -3.402823466e38f;
@@ -45,10 +45,11 @@ struct PromptArgs {
     const int32_t* first;
     int32_t* status;
     PromptCut* cuts;       // [W]
-    float* part_ml;        // [2 W][kRowTile][2]: reference (a raw score), sum
-    float* part_acc;       // [2 W][kRowTile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
+    float* part_ml;        // [2 W][row tile][2]: reference (a raw score), sum
+    float* part_acc;       // [2 W][row tile][Dv]: unnormalised output.  Slot 2 w: the row tile that began before stretch w, 2 w + 1: the one that goes on behind it
     int B, Hq, Hkv, G, P, num_pages, max_pages, n_tokens, Dqk, Dv;
     int W;
+    int row_shift;         // a row tile has 2^row_shift rows
     int tile_cost;         // what a row tile costs beside its positions, in positions
     uint32_t inv_p, inv_g; // 2^32 / P and 2^32 / G, at most 2^32 - 1
     float scale_log2, move_at;      // scale in units of log2 e; raw scores by which a reference is exceeded before it moves, 8 / scale_log2
@@ -92,17 +93,17 @@ __device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int
     r.bad = ctx < r.n || ctx > a.max_ctx;
     if (r.bad) error |= 1;
     r.past = r.bad ? 0 : ctx - r.n;
-    r.tiles = static_cast<int>((static_cast<int64_t>(r.n) * a.G + kRowTile - 1) / kRowTile);
+    r.tiles = static_cast<int>((static_cast<int64_t>(r.n) * a.G + (1 << a.row_shift) - 1) >> a.row_shift);
     return r;
 }
 // Cost of the first i row tiles of a KV head, and of row tile i.
 __device__ __forceinline__ int64_t tiles_before(const PromptArgs& a, int64_t past, int64_t i) {
-    return i * (a.G * (past + a.tile_cost)) + kRowTile / 2 * (i * (i + 1));
+    return i * (a.G * (past + a.tile_cost)) + ((i * (i + 1)) << (a.row_shift - 1));
 }
-__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + kRowTile * (i + 1); }
+__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + ((i + 1) << a.row_shift); }
 
 struct PromptLds {
-    int64_t sums[3][kPromptThreads / kWave];
+    int64_t sums[3][kMostPromptThreads / kWave];
     int64_t base[2], before[2];
     int found[2];
 };
@@ -127,6 +128,7 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 }
 
 // Sum of v over the threads before this one, and over all; two barriers.
+template <int THREADS>
 __device__ __forceinline__ int64_t prompt_before(int64_t v, int64_t* s, int64_t& total) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     int64_t up = v;
@@ -139,7 +141,7 @@ __device__ __forceinline__ int64_t prompt_before(int64_t v, int64_t* s, int64_t&
     __syncthreads();
     int64_t before = 0, all = 0;
 #pragma unroll
-    for (int w = 0; w < kPromptThreads / kWave; ++w) {
+    for (int w = 0; w < THREADS / kWave; ++w) {
         if (w < wave) before += s[w];
         all += s[w];
     }
@@ -155,11 +157,12 @@ __device__ __forceinline__ int64_t stretch_begin(const PromptPlan& p, int w) {
 
 // The line, by all threads of a workgroup (each looks at ceil(B / threads) requests behind one another), and where on it stretch w
 // begins and ends: the row tiles there.  False: there is no stretch w.  No barrier behind it.
+template <int THREADS>
 __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, int w, PromptPlan& p, int64_t (&x)[2], PromptTile (&t)[2], int& error) {
-    const int per = (a.B + kPromptThreads - 1) / kPromptThreads, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
+    const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
     int64_t n = 0, all;
     for (int b = b0; b < b1; ++b) n += prompt_tokens(a, b);
-    const int64_t mine_n = prompt_before(n, s.sums[0], all);
+    const int64_t mine_n = prompt_before<THREADS>(n, s.sums[0], all);
     int64_t mine_cost = 0, before = mine_n, tiles = 0;
     for (int b = b0; b < b1; ++b) {
         const PromptRequest r = prompt_request(a, b, before, error);
@@ -168,8 +171,8 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
         tiles += a.Hkv * static_cast<int64_t>(r.tiles);
     }
     int64_t all_tiles;
-    prompt_before(tiles, s.sums[2], all_tiles);
-    const int64_t mine = prompt_before(mine_cost, s.sums[1], p.total);
+    prompt_before<THREADS>(tiles, s.sums[2], all_tiles);
+    const int64_t mine = prompt_before<THREADS>(mine_cost, s.sums[1], p.total);
     const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
     const int64_t most = max((p.total + least - 1) / least, all_tiles);
     p.W = static_cast<int>(most < a.W ? most : a.W);
@@ -207,8 +210,8 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
         o.kvh = static_cast<int>(d / head);
         const int64_t inside = d - o.kvh * head;
         // the largest i with tiles_before(i) <= inside
-        const double A = static_cast<double>(a.G * (o.r.past + a.tile_cost) + kRowTile / 2);
-        int64_t i = static_cast<int64_t>((sqrt(A * A + 2.0 * kRowTile * static_cast<double>(inside)) - A) / kRowTile);
+        const double A = static_cast<double>(a.G * (o.r.past + a.tile_cost) + (1 << (a.row_shift - 1))), row_tile = 1 << a.row_shift;
+        int64_t i = static_cast<int64_t>((sqrt(A * A + 2.0 * row_tile * static_cast<double>(inside)) - A) / row_tile);
         i = i < 0 ? 0 : (i >= o.r.tiles ? o.r.tiles - 1 : i);
         while (i > 0 && tiles_before(a, o.r.past, i) > inside) --i;
         while (i + 1 < o.r.tiles && tiles_before(a, o.r.past, i + 1) <= inside) ++i;

@@ -37,7 +37,7 @@ namespace seer {
 // has three tiles in flight behind the one in use.
 constexpr int kSlots = 4;
 
-template <int DQK, int DV>
+template <int DQK, int DV, int WAVES>
 struct PromptShape {
     static constexpr int kTile = 32;
     static constexpr int kKRow = DQK * 2, kVRow = DV * 2;                     // bytes of a position's row
@@ -45,13 +45,15 @@ struct PromptShape {
     static constexpr int kVBase = kSlots * kKSlot;                           // the V ring follows the K ring
     static constexpr int kLds = kSlots * (kKSlot + kVSlot);
     static constexpr int kKSteps = DQK / 16, kDTiles = DV / 32, kPv = 2 * kDTiles;      // contraction steps; d-tiles; MFMAs of a product
-    static constexpr int kKLoads = kKSlot / 4096, kVLoads = kVSlot / 4096;   // of 1 KB, per wave and tile
+    static constexpr int kRows = 32 * WAVES;                                 // of a row tile
+    static constexpr int kMine = kTile / WAVES;                              // positions of a tile that a wave loads
+    static constexpr int kKLoads = kKSlot / (1024 * WAVES), kVLoads = kVSlot / (1024 * WAVES);   // of 1 KB, per wave and tile
     static constexpr int kKAhead = kKSteps < 8 ? kKSteps : 8;                // K operands requested ahead of their MFMA
     static constexpr int kVAhead = kPv < 8 ? kPv : 8;                        // V operands (two reads each)
     // Waves that a SIMD holds, by registers (queries, outputs, scores of two tiles, operands) and LDS.  Heads of 192/128 with one: 531 us for four sequences
     // of 4096 on 16 heads, with two 431.
     static constexpr int kWavesPerSimd = DQK <= 64 ? 3 : (DQK <= 192 ? 2 : 1);
-    static_assert(kKSlot % 4096 == 0 && kVSlot % 4096 == 0 && kLds <= 156 * 1024, "");
+    static_assert(kKSlot % (1024 * WAVES) == 0 && kVSlot % (1024 * WAVES) == 0 && kLds <= 156 * 1024, "");
 };
 
 // One LDS read whose completion is waited for by count (LDS answers in order; see wait_lgkm): through the builtins the compiler would wait for the
@@ -83,29 +85,30 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_at(const unsigned char* p
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, unsigned char* to, int offset) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (SEER_AS3 void*)(to), 16, offset, 0, 0, 0);
 }
-// Requests a wave's eight rows of a tile: at_row = row of the pool of the first of them (ANY_PAGE: of the tile's position lane % 32).
-template <int ROW, int LOADS, bool ANY_PAGE>
+// Requests a wave's MINE rows of a tile: at_row = row of the pool of the first of them (ANY_PAGE: of the tile's position lane % 32).
+template <int ROW, int LOADS, int MINE, bool ANY_PAGE>
 __device__ __forceinline__ void issue_rows(const unsigned char* pool, uint32_t at_row, const int (&pat)[LOADS], unsigned char* slot, int wave, int lane) {
     if constexpr (ANY_PAGE) {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
             const int r = (j * kWave + lane) / (ROW / 16);
-            const uint32_t from = __builtin_amdgcn_ds_bpermute((wave * 8 + r) << 2, at_row);
+            const uint32_t from = __builtin_amdgcn_ds_bpermute((wave * MINE + r) << 2, at_row);
             const unsigned char* src = pool + static_cast<size_t>(from) * ROW + (pat[j] - r * ROW);
             __builtin_amdgcn_global_load_lds((const SEER_AS1 void*)(src), (SEER_AS3 void*)(slot + (wave * LOADS + j) * 1024), 16, 0, 0);
         }
     } else {
-        const __amdgpu_buffer_rsrc_t rsrc = rows_at(pool + static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(at_row))) * ROW, 8 * ROW);
+        const __amdgpu_buffer_rsrc_t rsrc = rows_at(pool + static_cast<size_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(at_row))) * ROW, MINE * ROW);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) load_to_lds(rsrc, slot + (wave * LOADS + j) * 1024, pat[j]);
     }
 }
 
-// ANY_PAGE: pages of any size; else of a multiple of 16 positions, so that the eight rows of a tile that a wave loads lie in one page.
-template <int DQK, int DV, bool ANY_PAGE>
-__global__ __launch_bounds__(kPromptThreads) __attribute__((amdgpu_waves_per_eu(PromptShape<DQK, DV>::kWavesPerSimd)))
+// ANY_PAGE: pages of any size; else of a multiple of 16 positions, so that the rows of a tile that a wave loads lie in one page.
+// WAVES: four, or eight with 256 query rows, which read the same tile.
+template <int DQK, int DV, bool ANY_PAGE, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave) __attribute__((amdgpu_waves_per_eu(PromptShape<DQK, DV, WAVES>::kWavesPerSimd)))
 void prompt_tile_kernel(PromptArgs a) {
-    using S = PromptShape<DQK, DV>;
+    using S = PromptShape<DQK, DV, WAVES>;
     using O = tile::Operands<DQK, DV>;
     using tile::k_swz;
     using tile::v_swz;
@@ -125,7 +128,7 @@ void prompt_tile_kernel(PromptArgs a) {
     {
         int64_t at[2];
         PromptTile ends[2];
-        const bool on = prompt_plan(a, s_plan, w, plan, at, ends, error);
+        const bool on = prompt_plan<WAVES * kWave>(a, s_plan, w, plan, at, ends, error);
         if (w == 0 && error && a.status) atomicOr(a.status, error);
         if (!on) {
             if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
@@ -141,7 +144,7 @@ void prompt_tile_kernel(PromptArgs a) {
     }
     bool bad_page = false;
     // ANY_PAGE: window of page ids: request, first logical page; lane l holds the (clamped) id of page win + l.
-    // Else a window of rows: request, KV head, first tile; lane l holds the row of the pool where tile win + l's position 8 wave is; and the window of the request's
+    // Else a window of rows: request, KV head, first tile; lane l holds the row of the pool where tile win + l's first position of this wave is; and the window of the request's
     // first tiles, with which most row tiles begin.
     int win_b = -1, win_h = -1, win = 0, in_win = 0, first_win = 0;
     const int lds0 = tile::lds_addr(lds);
@@ -157,12 +160,12 @@ void prompt_tile_kernel(PromptArgs a) {
 #pragma unroll
     for (int j = 0; j < S::kKLoads; ++j) {
         const int c = j * kWave + lane, r = c / (S::kKRow / 16), pos = c - r * (S::kKRow / 16);
-        k_pat[j] = r * S::kKRow + ((pos ^ k_swz<S::kKRow>(wave * 8 + r)) << 4);
+        k_pat[j] = r * S::kKRow + ((pos ^ k_swz<S::kKRow>(wave * S::kMine + r)) << 4);
     }
 #pragma unroll
     for (int j = 0; j < S::kVLoads; ++j) {
         const int c = j * kWave + lane, r = c / (S::kVRow / 16), pos = c - r * (S::kVRow / 16);
-        v_pat[j] = r * S::kVRow + ((pos ^ v_swz<S::kVRow>(wave * 8 + r)) << 4);
+        v_pat[j] = r * S::kVRow + ((pos ^ v_swz<S::kVRow>(wave * S::kMine + r)) << 4);
     }
 
     while (x < x_end) {
@@ -170,8 +173,8 @@ void prompt_tile_kernel(PromptArgs a) {
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
         // (rows of q are counted in 32 bits)
-        const uint32_t row0 = static_cast<uint32_t>(t.i) * kRowTile;
-        const int rows = static_cast<int>(min(static_cast<uint32_t>(t.r.n) * static_cast<uint32_t>(a.G) - row0, static_cast<uint32_t>(kRowTile)));
+        const uint32_t row0 = static_cast<uint32_t>(t.i) * S::kRows;
+        const int rows = static_cast<int>(min(static_cast<uint32_t>(t.r.n) * static_cast<uint32_t>(a.G) - row0, static_cast<uint32_t>(S::kRows)));
         const int token_first = prompt_token(a, row0), token_last = prompt_token(a, row0 + rows - 1);              // of the request's new tokens
         const int seen = static_cast<int>(t.r.past) + token_last + 1;                                              // positions that the last row sees
         const int all_see = static_cast<int>(t.r.past) + token_first;                                              // the last one that all rows see
@@ -220,8 +223,8 @@ void prompt_tile_kernel(PromptArgs a) {
                     if ((pg < 0 || pg >= a.num_pages) && first + lane <= last_page) bad_page = true;
                     in_win = min(max(pg, 0), a.num_pages - 1);
                 } else {
-                    // (behind the request's last position: its last eight again)
-                    const int position = min((first + lane) * kTile + wave * 8, last & ~7), lp = page_of(position);
+                    // (behind the request's last position: its last ones again)
+                    const int position = min((first + lane) * kTile + wave * S::kMine, last & ~(S::kMine - 1)), lp = page_of(position);
                     pg = table[lp];
                     if (pg < 0 || pg >= a.num_pages) bad_page = true;
                     pg = min(max(pg, 0), a.num_pages - 1);
@@ -229,7 +232,7 @@ void prompt_tile_kernel(PromptArgs a) {
                     if (first == 0) first_win = in_win;
                 }
             };
-            // Row of the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU) of tile u's position 8 wave; ANY_PAGE: of position ln.
+            // Row of the pool (of 128 bytes or more each: 32 bits reach past the memory of the GPU) of tile u's first position of this wave; ANY_PAGE: of position ln.
             // Tiles are asked for in ascending order.
             auto tile_row = [&](int u) __attribute__((always_inline)) -> uint32_t {
                 if constexpr (ANY_PAGE) {
@@ -244,10 +247,10 @@ void prompt_tile_kernel(PromptArgs a) {
                 }
             };
             auto issue_k = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
-                issue_rows<S::kKRow, S::kKLoads, ANY_PAGE>(a.k_pages, at_row, k_pat, lds + (u & (kSlots - 1)) * S::kKSlot, wave, lane);
+                issue_rows<S::kKRow, S::kKLoads, S::kMine, ANY_PAGE>(a.k_pages, at_row, k_pat, lds + (u & (kSlots - 1)) * S::kKSlot, wave, lane);
             };
             auto issue_v = [&](int u, uint32_t at_row) __attribute__((always_inline)) {
-                issue_rows<S::kVRow, S::kVLoads, ANY_PAGE>(a.v_pages, at_row, v_pat, lds + S::kVBase + (u & (kSlots - 1)) * S::kVSlot, wave, lane);
+                issue_rows<S::kVRow, S::kVLoads, S::kMine, ANY_PAGE>(a.v_pages, at_row, v_pat, lds + S::kVBase + (u & (kSlots - 1)) * S::kVSlot, wave, lane);
             };
 
             // ---- softmax ------------------------------------------------------------------------------------
@@ -329,13 +332,13 @@ void prompt_tile_kernel(PromptArgs a) {
                 if (tid == 0) *found_in = 0;
                 wait_reads<0>();
                 bare_barrier();
-                const uint32_t found = tile::tile_nonfinite<DQK, DV>(vl, tid, kPromptThreads);
+                const uint32_t found = tile::tile_nonfinite<DQK, DV>(vl, tid, WAVES * kWave);
                 if (found) atomicOr(found_in, found);
                 wait_reads<0>();
                 bare_barrier();
                 left = __builtin_amdgcn_readfirstlane(*const_cast<volatile uint32_t*>(found_in));
                 if (left) {
-                    tile::tile_clear_rows<DQK, DV>(vl, left, tid, kPromptThreads);
+                    tile::tile_clear_rows<DQK, DV>(vl, left, tid, WAVES * kWave);
                     wait_reads<0>();
                 }
                 bare_barrier();
@@ -534,7 +537,7 @@ void prompt_tile_kernel(PromptArgs a) {
             const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;          // (a row of nothing but -inf: zeros)
             // through LDS, so that a store takes whole rows: 16-byte chunk c of row r at c ^ r (its low bits)
             constexpr int kChunks = DV / 8, kPerStore = kWave / (kChunks < kWave ? kChunks : kWave);      // rows of a store
-            static_assert(4 * 32 * DV * 2 <= S::kLds, "");
+            static_assert(S::kRows * DV * 2 <= S::kLds, "");
             int l = lane;
             asm volatile("" : "+v"(l));             // (the addresses below are made here, not kept in registers through the tiles)
             const int row_l = l & 31;
@@ -559,10 +562,10 @@ void prompt_tile_kernel(PromptArgs a) {
         // a lane's registers as they are, so that a store takes 1 KB: see partial_at
         const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
         if (lg == 0) {
-            const size_t prow = slot * kRowTile + wave * 32 + ln;
+            const size_t prow = slot * S::kRows + wave * 32 + ln;
             a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;
         }
-        f32x4* po = reinterpret_cast<f32x4*>(a.part_acc) + (slot * 4 + wave) * (S::kDTiles * 4 * kWave) + lane;
+        f32x4* po = reinterpret_cast<f32x4*>(a.part_acc) + (slot * WAVES + wave) * (S::kDTiles * 4 * kWave) + lane;
 #pragma unroll
         for (int dt = 0; dt < S::kDTiles; ++dt)
 #pragma unroll
@@ -571,27 +574,27 @@ void prompt_tile_kernel(PromptArgs a) {
     if (a.status && __any(bad_page) && lane == 0) atomicOr(a.status, 2);
 }
 
-// Joins the pieces of the row tile that was cut at the end of stretch blockIdx.x, eight rows a workgroup.
+// Joins the pieces of the row tile that was cut at the end of stretch blockIdx.x, 256 vectors a workgroup.
 // A workgroup takes a quarter of a wave's rows and outputs: one f32x4 of a lane (row ln, outputs dt * 32 + i4 * 8 + lg * 4 .. + 3) per thread.
-template <int DV>
+template <int DV, int ROWS>
 __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs a) {
-    constexpr int kVectors = kRowTile * DV / 4, kBlocks = kVectors / kPromptThreads;
+    constexpr int kVectors = ROWS * DV / 4, kBlocks = kVectors / kPromptThreads;
     const int w = blockIdx.x / kBlocks, e = blockIdx.x % kBlocks * kPromptThreads + threadIdx.x;
     const PromptCut cut = a.cuts[w];
     if (cut.pieces < 2) return;
     const int first = a.first[cut.b], n = a.first[cut.b + 1] - first;
     const int lane = e & (kWave - 1), vec = e / kWave % (DV / 8), wave = e / kWave / (DV / 8);
     const int r = wave * 32 + (lane & 31), d = vec * 8 + (lane >> 5) * 4;
-    const int64_t row = static_cast<int64_t>(cut.tile) * kRowTile + r;
+    const int64_t row = static_cast<int64_t>(cut.tile) * ROWS + r;
     if (row >= static_cast<int64_t>(n) * a.G) return;
     auto slot = [&](int k) { return 2 * static_cast<size_t>(w + k) + (k == 0 ? 1 : 0); };
     float m = kNoScore;
-    for (int k = 0; k < cut.pieces; ++k) m = fmaxf(m, a.part_ml[2 * (slot(k) * kRowTile + r)]);
+    for (int k = 0; k < cut.pieces; ++k) m = fmaxf(m, a.part_ml[2 * (slot(k) * ROWS + r)]);
     float l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < cut.pieces; ++k) {
-        const float mk = a.part_ml[2 * (slot(k) * kRowTile + r)], lk = a.part_ml[2 * (slot(k) * kRowTile + r) + 1];
+        const float mk = a.part_ml[2 * (slot(k) * ROWS + r)], lk = a.part_ml[2 * (slot(k) * ROWS + r) + 1];
         const float f = fast_exp2((mk - m) * a.scale_log2);
         const f32x4 v = *(reinterpret_cast<const f32x4*>(a.part_acc) + slot(k) * kVectors + e);
         l = fmaf(lk, f, l);
@@ -606,20 +609,28 @@ __global__ __launch_bounds__(kPromptThreads) void prompt_join_kernel(PromptArgs 
 
 static hipError_t launch_join(const PromptArgs& a, hipStream_t stream) {
     // (a block table so short that no row tile is cut leaves nothing to join)
-    if (a.G * (a.max_ctx + a.tile_cost) + kRowTile <= static_cast<int64_t>(a.G) * (kWholePositions + a.tile_cost)) return hipSuccess;
-    const dim3 grid(a.W * (kRowTile * a.Dv / 4 / kPromptThreads));
-    if (a.Dv == 64) hipLaunchKernelGGL((prompt_join_kernel<64>), grid, dim3(kPromptThreads), 0, stream, a);
-    else if (a.Dv == 128) hipLaunchKernelGGL((prompt_join_kernel<128>), grid, dim3(kPromptThreads), 0, stream, a);
-    else if (a.Dv == 256) hipLaunchKernelGGL((prompt_join_kernel<256>), grid, dim3(kPromptThreads), 0, stream, a);
-    else hipLaunchKernelGGL((prompt_join_kernel<512>), grid, dim3(kPromptThreads), 0, stream, a);
+    const int rows = 1 << a.row_shift;
+    if (a.G * (a.max_ctx + a.tile_cost) + rows <= static_cast<int64_t>(a.G) * (kWholePositions + a.tile_cost)) return hipSuccess;
+    const dim3 grid(a.W * (rows * a.Dv / 4 / kPromptThreads));
+    if (a.Dv == 64) hipLaunchKernelGGL((prompt_join_kernel<64, kRowTile>), grid, dim3(kPromptThreads), 0, stream, a);
+    else if (a.Dv == 128 && rows > kRowTile) hipLaunchKernelGGL((prompt_join_kernel<128, 2 * kRowTile>), grid, dim3(kPromptThreads), 0, stream, a);
+    else if (a.Dv == 128) hipLaunchKernelGGL((prompt_join_kernel<128, kRowTile>), grid, dim3(kPromptThreads), 0, stream, a);
+    else if (a.Dv == 256) hipLaunchKernelGGL((prompt_join_kernel<256, kRowTile>), grid, dim3(kPromptThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prompt_join_kernel<512, kRowTile>), grid, dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
 template <int DQK, int DV>
 static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
+    if constexpr (DQK == 128) {
+        if (1 << a.row_shift > kRowTile) {
+            hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, false, 8>), dim3(a.W), dim3(8 * kWave), 0, stream, a);
+            return hipGetLastError();
+        }
+    }
     // (pages of 16 through the form for any page, against their own: one prompt of 32 768 tokens on 8/1 heads 2553 | 2162 us, heads of 256 439 | 348, 64 253 | 226)
-    if (a.P % 16 == 0) hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, false>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
-    else hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, true>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    if (a.P % 16 == 0) hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, false, 4>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
+    else hipLaunchKernelGGL((prompt_tile_kernel<DQK, DV, true, 4>), dim3(a.W), dim3(kPromptThreads), 0, stream, a);
     return hipGetLastError();
 }
 
@@ -644,28 +655,39 @@ static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (ctx > 0x7fffffffLL - 65536 || static_cast<int64_t>(p->num_pages) * p->page_size * p->Hkv > 0xffffffffLL) return SEER_ESHAPE;
     if (static_cast<int64_t>(n_tokens) * p->Hq > 0xffffffffLL) return SEER_ESHAPE;
     const double tiles = static_cast<double>(n_tokens) * G / kRowTile + p->B;
-    if (tiles * p->Hkv * (static_cast<double>(G) * (ctx + prompt_tile_cost(p->Dqk)) + static_cast<double>(n_tokens) * G + kRowTile) > 4e15) return SEER_ESHAPE;
+    if (tiles * p->Hkv * (static_cast<double>(G) * (ctx + prompt_tile_cost(p->Dqk)) + static_cast<double>(n_tokens) * G + 2 * kRowTile) > 4e15) return SEER_ESHAPE;
     return SEER_OK;
 }
 struct PromptLayout {
-    int W;
+    int W, row_shift;
     size_t off_ml, off_acc, total;
 };
+constexpr int64_t kEightWavesRows = 131072, kEightWavesRequest = 8192;      // query rows, and those of a KV head and request on average
 constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 64 ? 3 : (dqk <= 192 ? 2 : 1); }
+// Eight waves and 256 rows a workgroup, for heads of 128: half the tile loads.  Four | eight waves: 16 prompts of 256 .. 8192 tokens on 64/8 heads 3121 | 2999 us, one of 32 768
+// on 8/1 2065 | 1990, one of 16 384 on 64/8 4210 | 3973, four of 8192 on 16/16 1204 | 1150, 16 of 2048 on 32/8 681 | 666.  With few rows a request or few of all, coarse
+// row tiles cost more than that: 8 of 1024 on 32/8 105 | 113, four of 4096 on 16/16 335 | 340, one of 600 on 8/1 24.5 | 40, of 4096 62.6 | 64.6, one of 1024 on 64/8 47 | 52, single
+// tokens 902 | 1127.  (Heads of 64 and 256 hold three waves and one a SIMD, a tile of 192 components is no multiple of eight waves' loads.)
+static bool prompt_has_eight_waves(const seer_attn_params& p, int32_t n_tokens) {
+    const int64_t rows = static_cast<int64_t>(n_tokens) * p.Hq;
+    return p.Dqk == 128 && p.page_size % 16 == 0 && rows >= kEightWavesRows && rows / p.Hkv >= kEightWavesRequest * static_cast<int64_t>(p.B);
+}
 static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     PromptLayout w{};
     // no more stretches than the GPU holds at once, nor than the host can see work for
-    int resident = 256 * prompt_waves_per_simd(p.Dqk);
+    const int row_tile = prompt_has_eight_waves(p, n_tokens) ? 2 * kRowTile : kRowTile;
+    int resident = 256 * prompt_waves_per_simd(p.Dqk) * kRowTile / row_tile;
     const int64_t ctx = static_cast<int64_t>(p.max_pages_per_seq) * p.page_size, G = p.Hq / p.Hkv;
     const int64_t requests = p.B < n_tokens ? p.B : n_tokens;
-    const double row_tiles = (static_cast<double>(n_tokens) * G / kRowTile + requests) * p.Hkv;
-    const double most = row_tiles * (static_cast<double>(ctx + prompt_tile_cost(p.Dqk) + kRowTile) / kMinStretch + 1);
+    const double row_tiles = (static_cast<double>(n_tokens) * G / row_tile + requests) * p.Hkv;
+    const double most = row_tiles * (static_cast<double>(ctx + prompt_tile_cost(p.Dqk) + row_tile) / kMinStretch + 1);
     if (most < resident) resident = static_cast<int>(most);
     w.W = (resident + 7) / 8 * 8;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     w.off_ml = up(sizeof(PromptCut) * w.W);
-    w.off_acc = w.off_ml + up(sizeof(float) * 2 * kRowTile * 2 * w.W);
-    w.total = w.off_acc + sizeof(float) * kRowTile * p.Dv * 2 * w.W;
+    w.off_acc = w.off_ml + up(sizeof(float) * 2 * row_tile * 2 * w.W);
+    w.total = w.off_acc + sizeof(float) * row_tile * p.Dv * 2 * w.W;
+    w.row_shift = row_tile == kRowTile ? 7 : 8;
     return w;
 }
 
@@ -700,7 +722,7 @@ extern "C" int seer_prompt_attention(void* out, const void* q, const void* k_pag
     a.part_acc = reinterpret_cast<float*>(ws + layout.off_acc);
     a.B = p->B, a.Hq = p->Hq, a.Hkv = p->Hkv, a.G = p->Hq / p->Hkv, a.P = p->page_size, a.num_pages = p->num_pages, a.max_pages = p->max_pages_per_seq;
     a.inv_g = a.G > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(a.G)) : 0xffffffffu;
-    a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W, a.tile_cost = seer::prompt_tile_cost(p->Dqk);
+    a.n_tokens = n_tokens, a.Dqk = p->Dqk, a.Dv = p->Dv, a.W = layout.W, a.row_shift = layout.row_shift, a.tile_cost = seer::prompt_tile_cost(p->Dqk);
     a.inv_p = p->page_size > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / static_cast<uint32_t>(p->page_size)) : 0xffffffffu;
     a.scale_log2 = p->scale * seer::kLog2e;
     a.move_at = a.scale_log2 > 1e-36f ? 8.f / a.scale_log2 : 8e36f;

@@ -42,7 +42,7 @@ void prompt_latent_kernel(PromptArgs a) {
     {
         int64_t at[2];
         PromptTile ends[2];
-        const bool on = prompt_plan(a, s_plan, w, plan, at, ends, error);
+        const bool on = prompt_plan<kPromptThreads>(a, s_plan, w, plan, at, ends, error);
         if (w == 0 && error && a.status) atomicOr(a.status, error);
         if (!on) {
             if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
