@@ -68,6 +68,11 @@ __device__ __forceinline__ int prompt_page(const PromptArgs& a, int position) {
 // Token of a query row of a request.
 __device__ __forceinline__ int prompt_token(const PromptArgs& a, uint32_t row) { return static_cast<int>(quotient(row, static_cast<uint32_t>(a.G), a.inv_g)); }
 
+// A row tile of a workgroup of THREADS has 2^kRowShift rows, half as many.
+template <int THREADS>
+constexpr int kRowShift = THREADS == kPromptThreads ? 7 : 8;
+static_assert(1 << kRowShift<kPromptThreads> == kRowTile && 1 << kRowShift<kMostPromptThreads> == 2 * kRowTile, "");
+
 // A request as the line counts it.
 struct PromptRequest {
     int64_t past;          // positions before the new tokens
@@ -81,6 +86,7 @@ __device__ __forceinline__ int prompt_tokens(const PromptArgs& a, int b) {
     return lo >= 0 && hi >= lo && hi <= a.n_tokens ? hi - lo : 0;
 }
 // before: the sum of prompt_tokens over the requests before b (with a limit to it the line is finite whatever the array holds).
+template <int THREADS>
 __device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int b, int64_t before, int& error) {
     PromptRequest r{0, 0, 0, 0, false};
     const int lo = a.first[b], hi = a.first[b + 1], ctx = a.ctx_len[b];
@@ -93,14 +99,16 @@ __device__ __forceinline__ PromptRequest prompt_request(const PromptArgs& a, int
     r.bad = ctx < r.n || ctx > a.max_ctx;
     if (r.bad) error |= 1;
     r.past = r.bad ? 0 : ctx - r.n;
-    r.tiles = static_cast<int>((static_cast<int64_t>(r.n) * a.G + (1 << a.row_shift) - 1) >> a.row_shift);
+    r.tiles = static_cast<int>((static_cast<int64_t>(r.n) * a.G + (1 << kRowShift<THREADS>) - 1) >> kRowShift<THREADS>);
     return r;
 }
 // Cost of the first i row tiles of a KV head, and of row tile i.
+template <int THREADS>
 __device__ __forceinline__ int64_t tiles_before(const PromptArgs& a, int64_t past, int64_t i) {
-    return i * (a.G * (past + a.tile_cost)) + ((i * (i + 1)) << (a.row_shift - 1));
+    return i * (a.G * (past + a.tile_cost)) + ((i * (i + 1)) << (kRowShift<THREADS> - 1));
 }
-__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + ((i + 1) << a.row_shift); }
+template <int THREADS>
+__device__ __forceinline__ int64_t tile_cost(const PromptArgs& a, int64_t past, int64_t i) { return a.G * (past + a.tile_cost) + ((i + 1) << kRowShift<THREADS>); }
 
 struct PromptLds {
     int64_t sums[3][kMostPromptThreads / kWave];
@@ -165,9 +173,9 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
     const int64_t mine_n = prompt_before<THREADS>(n, s.sums[0], all);
     int64_t mine_cost = 0, before = mine_n, tiles = 0;
     for (int b = b0; b < b1; ++b) {
-        const PromptRequest r = prompt_request(a, b, before, error);
+        const PromptRequest r = prompt_request<THREADS>(a, b, before, error);
         before += prompt_tokens(a, b);
-        mine_cost += a.Hkv * tiles_before(a, r.past, r.tiles);
+        mine_cost += a.Hkv * tiles_before<THREADS>(a, r.past, r.tiles);
         tiles += a.Hkv * static_cast<int64_t>(r.tiles);
     }
     int64_t all_tiles;
@@ -188,8 +196,8 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
         int64_t begin = mine;
         before = mine_n;
         for (int b = b0; b < b1; ++b) {
-            const PromptRequest r = prompt_request(a, b, before, ignored);
-            const int64_t cost = a.Hkv * tiles_before(a, r.past, r.tiles);
+            const PromptRequest r = prompt_request<THREADS>(a, b, before, ignored);
+            const int64_t cost = a.Hkv * tiles_before<THREADS>(a, r.past, r.tiles);
             if (at < begin + cost) {
                 s.found[e] = b, s.base[e] = begin, s.before[e] = before;
                 break;
@@ -205,25 +213,26 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
         PromptTile& o = t[e];
         o.b = __builtin_amdgcn_readfirstlane(s.found[e]);
         o.before = uniform64(s.before[e]);
-        o.r = prompt_request(a, o.b, o.before, ignored);
-        const int64_t begin = uniform64(s.base[e]), head = tiles_before(a, o.r.past, o.r.tiles), d = at - begin;
+        o.r = prompt_request<THREADS>(a, o.b, o.before, ignored);
+        const int64_t begin = uniform64(s.base[e]), head = tiles_before<THREADS>(a, o.r.past, o.r.tiles), d = at - begin;
         o.kvh = static_cast<int>(d / head);
         const int64_t inside = d - o.kvh * head;
         // the largest i with tiles_before(i) <= inside
-        const double A = static_cast<double>(a.G * (o.r.past + a.tile_cost) + (1 << (a.row_shift - 1))), row_tile = 1 << a.row_shift;
+        const double A = static_cast<double>(a.G * (o.r.past + a.tile_cost) + (1 << (kRowShift<THREADS> - 1))), row_tile = 1 << kRowShift<THREADS>;
         int64_t i = static_cast<int64_t>((sqrt(A * A + 2.0 * row_tile * static_cast<double>(inside)) - A) / row_tile);
         i = i < 0 ? 0 : (i >= o.r.tiles ? o.r.tiles - 1 : i);
-        while (i > 0 && tiles_before(a, o.r.past, i) > inside) --i;
-        while (i + 1 < o.r.tiles && tiles_before(a, o.r.past, i + 1) <= inside) ++i;
+        while (i > 0 && tiles_before<THREADS>(a, o.r.past, i) > inside) --i;
+        while (i + 1 < o.r.tiles && tiles_before<THREADS>(a, o.r.past, i + 1) <= inside) ++i;
         o.i = static_cast<int>(i);
-        o.begin = begin + o.kvh * head + tiles_before(a, o.r.past, i);
-        o.cost = tile_cost(a, o.r.past, i);
+        o.begin = begin + o.kvh * head + tiles_before<THREADS>(a, o.r.past, i);
+        o.cost = tile_cost<THREADS>(a, o.r.past, i);
     }
     return true;
 }
 
 // The row tile behind t on the line, which must not end there; by each wave for itself.  Of the KV head, of the next one, of the next request with
 // tokens: 64 requests are looked at together.
+template <int THREADS>
 __device__ __forceinline__ void next_tile(const PromptArgs& a, PromptTile& t) {
     t.begin += t.cost;
     if (t.i + 1 < t.r.tiles) {
@@ -243,7 +252,7 @@ __device__ __forceinline__ void next_tile(const PromptArgs& a, PromptTile& t) {
                 continue;
             }
             t.b = b0 + __builtin_ctzll(some);
-            t.r = prompt_request(a, t.b, t.before, ignored);       // (nothing, if the tokens before it fill the array)
+            t.r = prompt_request<THREADS>(a, t.b, t.before, ignored);       // (nothing, if the tokens before it fill the array)
             if (t.r.tiles == 0) t.before += prompt_tokens(a, t.b), b0 = t.b + 1;
         }
         t.before = uniform64(t.before);
@@ -251,7 +260,7 @@ __device__ __forceinline__ void next_tile(const PromptArgs& a, PromptTile& t) {
         t.r.past = uniform64(t.r.past), t.r.n = __builtin_amdgcn_readfirstlane(t.r.n), t.r.tiles = __builtin_amdgcn_readfirstlane(t.r.tiles);
         t.r.first = __builtin_amdgcn_readfirstlane(t.r.first), t.r.bad = __builtin_amdgcn_readfirstlane(t.r.bad);
     }
-    t.cost = tile_cost(a, t.r.past, t.i);
+    t.cost = tile_cost<THREADS>(a, t.r.past, t.i);
 }
 // A cut at x inside row tile t, moved to the row tile's end if that is near.
 __device__ __forceinline__ int64_t moved_cut(const PromptPlan& p, const PromptTile& t, int64_t x) {

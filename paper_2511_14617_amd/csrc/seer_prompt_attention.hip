@@ -169,7 +169,7 @@ void prompt_tile_kernel(PromptArgs a) {
     }
 
     while (x < x_end) {
-        if (x >= t.begin + t.cost) next_tile(a, t);
+        if (x >= t.begin + t.cost) next_tile<WAVES * kWave>(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
         // (rows of q are counted in 32 bits)

@@ -78,7 +78,7 @@ void prompt_latent_kernel(PromptArgs a) {
     auto page_of = [&](int position) __attribute__((always_inline)) -> int { return prompt_page(a, position); };
 
     while (x < x_end) {
-        if (x >= t.begin + t.cost) next_tile(a, t);
+        if (x >= t.begin + t.cost) next_tile<kPromptThreads>(a, t);
         const int64_t end = min(x_end, t.begin + t.cost);
         const bool begins = x == t.begin, ends = end == t.begin + t.cost;
         // (rows of q are counted in 32 bits)
