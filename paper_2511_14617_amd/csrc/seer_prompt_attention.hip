@@ -4,7 +4,7 @@
 // out = sum_j p_j V_j / sum_j p_j, p_j = exp(scale q.K_j - m) over the positions j that a token sees (those before it and itself), in one pass: a
 // running reference m, sums and outputs in fp32.  Positions that no row of the tile sees are not read, a cached row is read once per row tile.
 //
-// Workgroup = 4 waves = a row tile of 128 query rows of one KV head, 32 rows a wave; the work is cut into equal stretches of a line
+// Workgroup = 4 waves = a row tile of 128 query rows of one KV head, 32 rows a wave (8 waves and 256 rows where there are many); the work is cut into equal stretches of a line
 // of row tiles (seer_prompt.h).  A tile of 32 positions goes HBM/L2 -> LDS directly into rings of four tiles, three of them in flight.  S^T = K.Q^T
 // leaves a query row to a lane pair, so its softmax needs one exchange between two lanes, and the probabilities are, packed to bf16 (the matrix
 // operand's type; the sum is taken of the rounded values, so what is common cancels), the operand of O^T += V^T.P^T as they are.
@@ -12,13 +12,14 @@
 // Neighbouring tiles run side by side: behind every MFMA of the scores of tile u stand a K read for a later one and a few of tile u - 1's probabilities,
 // behind those of its product with V the rest of them and the highest scores of tile u.  Before that, scores, softmax and product of a tile one
 // after the other, one prompt of 32 768 tokens on 8/1 heads of 128 took 3.09 ms; side by side 2.67; with the arithmetic pinned beside its
-// MFMA 2.53; with waits and loads without conditions and descriptors in scalar registers 2.25; with today's shares of the line 2.17 (1015 TFLOP/s, where an
-// 8192^3 bf16 library product reaches 1378).
+// MFMA 2.53; with waits and loads without conditions and descriptors in scalar registers 2.25; with today's shares of the line 2.17; with eight waves on a
+// tile 2.06 (1067 TFLOP/s, where an 8192^3 bf16 library product reaches 1378).
 //
-// What bounds it: the power that matrix cores, LDS and vector ALU take together.  In that prompt the matrix cores are busy 56 % of the time, vector
-// instructions 47 %, LDS 30 % (0.15 % of it conflicts), at 1.79 GHz instead of 2.4, and every change that saved cycles lowered the clock by nearly as much:
-// without the exponentials the time is 1 % less, without tile loads 13 to 19, without the product with V 15.  Earlier K reads, loads in the shadow of the scores'
-// MFMAs, other shares of probabilities, wave priorities changed nothing.  Requests of one token are bound by HBM: 64 of 16 384 positions on
+// What bounds it: the power that matrix cores, LDS and vector ALU take together.  In that prompt, with four waves a workgroup, the matrix cores are busy 56 % of
+// the time, vector instructions 47 %, LDS 30 % (0.15 % of it conflicts), at 1.79 GHz instead of 2.4, and changes that saved cycles lowered the clock by nearly
+// as much: without the exponentials the time is 1 % less, without tile loads 13 to 19, without the product with V 15; earlier K reads, loads in the shadow of the
+// scores' MFMAs, other shares of probabilities, wave priorities changed nothing.  Eight waves take 4 % more cycles (54 % busy) and half the loads, at 1.92 GHz.
+// Requests of one token are bound by HBM: 64 of 16 384 positions on
 // 8 KV heads read 4.8 TB/s, though 28 of the 32 rows of a wave and three of four waves have nothing to do (loads that stream past the
 // caches gain 4 % there and cost prompts 30 %, which share what they read: not used).
 //
