@@ -685,7 +685,8 @@ static PromptLayout prompt_layout(const seer_attn_params& p, int32_t n_tokens) {
     if (most < resident) resident = static_cast<int>(most);
     w.W = (resident + 7) / 8 * 8;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    w.off_ml = up(sizeof(PromptCut) * w.W);
+    // (as many bytes for both row tiles: what does for more tokens does for fewer)
+    w.off_ml = up(sizeof(PromptCut) * w.W * (row_tile / kRowTile));
     w.off_acc = w.off_ml + up(sizeof(float) * 2 * row_tile * 2 * w.W);
     w.total = w.off_acc + sizeof(float) * row_tile * p.Dv * 2 * w.W;
     w.row_shift = row_tile == kRowTile ? 7 : 8;

@@ -125,6 +125,16 @@ def pp(**kw):
     return SeerAttnParams(**base)
 
 
+@pytest.mark.parametrize("heads", [(64, 8, 128, 128), (16, 16, 128, 128), (8, 1, 128, 128), (8, 1, 256, 256)])
+def test_prompt_attention_workspace_of_more_tokens_does_for_fewer(lib, heads):
+    from paper_2511_14617_amd import binding as b
+    Hq, Hkv, Dqk, Dv = heads
+    for B in (1, 2, 16, 300):
+        p = b.SeerAttnParams(B, 1, Hq, Hkv, Dqk, Dv, 16, 40000, 4000, 0, 0, 0, 0.1)
+        sizes = [b.seer_prompt_attention_workspace(p, n) for n in (1, 50, 1000, 1024, 1025, 2047, 2048, 2049, 8191, 8192, 16384, 16385, 40000, 500000)]
+        assert sizes[0] > 0 and sizes == sorted(sizes)
+
+
 def test_prompt_attention_workspace(lib):
     from paper_2511_14617_amd import binding as b
     size = b.seer_prompt_attention_workspace
