@@ -624,6 +624,8 @@ SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
  *                held, share_from), 4 = tokens beyond n_tokens, 8 = no pages left: such rows are left as they were.  2 = a page id
  *                outside the pool, 16 = a page with a count below 0: it was given back more often than taken (and is not given out again).  The caller clears it.
  *  workspace     device, >= seer_kv_reserve_workspace(p) bytes, 16-byte aligned
+ * With B = 0 nothing is launched and nothing written, not first_token, slot and position either: entries for n_tokens tokens are then the caller's
+ * to fill (0, -1 and -1).
  * Asynchronous on hip_stream; returns SEER_OK, a negative SEER_E* or a positive hipError_t.
  */
 SEER_API int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_len, const int32_t* n_new, const int32_t* share_from,

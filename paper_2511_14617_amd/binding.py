@@ -737,6 +737,11 @@ def seer_kv_reserve(block_table: torch.Tensor, pages_held: torch.Tensor, page_re
                                pages_held.data_ptr(), page_refs.data_ptr(), step_len.data_ptr(), first_token.data_ptr(), slot.data_ptr(),
                                position.data_ptr(), _ptr(status), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                _stream_handle(stream)))
+    if B == 0:                                              # (the call writes nothing: all tokens are padding)
+        with torch.cuda.stream(stream):
+            first_token.fill_(0)
+            slot.fill_(-1)
+            position.fill_(-1)
     return step_len, first_token, slot, position
 
 
