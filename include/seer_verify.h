@@ -588,7 +588,10 @@ typedef struct seer_reserve_params {
     int32_t num_pages;          /* pages in the pool, up to 2^30                                           */
     int32_t max_pages_per_seq;  /* row stride of block_table                                               */
     int32_t n_tokens;           /* entries of slot and position: room for all new tokens of the call       */
+    int32_t flags;              /* 0 or SEER_RESERVE_OWN_PAGES                                             */
 } seer_reserve_params;
+
+#define SEER_RESERVE_OWN_PAGES 1  /* no slots in pages that another row holds as well                       */
 
 /* Bytes of device scratch seer_kv_reserve needs; 0 on invalid params.  Host-only. */
 SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
@@ -601,6 +604,11 @@ SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
  * page_refs[p] counts the rows that hold page p, and the caller if it has a use of its own for it: 0 = free.  A request that starts (pages_held[b] = 0) may take over the leading pages of row r = share_from[b] that hold its first
  * ctx_len[b] positions, a multiple of page_size and no more than row r holds before the call: the
  * whole pages of a prompt that a group has in common (the rest of the prompt is among its new tokens).
+ *
+ * A row's new tokens must not begin inside a page that another row holds: the call gives out the slots behind ctx_len[b] in every page of the row, and what
+ * seer_kv_append writes there is the other row's cache too.  It comes to that when a row is cut (ctx_len[b] lowered) into a page that it shares, or
+ * when a row takes over a page that row r holds but has not filled.  SEER_RESERVE_OWN_PAGES refuses such slots: a new token in a page whose count is above 1
+ * after the call (the caller's own use of a page counts) gets slot and position -1, and status bit 32 is raised; all else is as without the flag.
  *
  * All rows are judged by the state before the call.  Shared pages are counted up, then pages counted down, then the free pages, the lowest
  * ids first, go to the rows in ascending order; a row that needs pages gets them if those before it that need any and it itself
@@ -622,7 +630,7 @@ SEER_API size_t seer_kv_reserve_workspace(const seer_reserve_params* p);
  *  position      device [n_tokens] int32, written: ctx_len[b] + i for the row's i-th token (but see tree_mask); -1 as for slot
  *  status        device [1] int32 or NULL; bits are OR-ed in: 1 = numbers out of range (n_new, ctx_len beyond the table or the pages
  *                held, share_from), 4 = tokens beyond n_tokens, 8 = no pages left: such rows are left as they were.  2 = a page id
- *                outside the pool, 16 = a page with a count below 0: it was given back more often than taken (and is not given out again).  The caller clears it.
+ *                outside the pool, 16 = a page with a count below 0: it was given back more often than taken (and is not given out again), 32 = a slot refused by SEER_RESERVE_OWN_PAGES.  The caller clears it.
  *  workspace     device, >= seer_kv_reserve_workspace(p) bytes, 16-byte aligned
  * With B = 0 nothing is launched and nothing written, not first_token, slot and position either: entries for n_tokens tokens are then the caller's
  * to fill (0, -1 and -1).

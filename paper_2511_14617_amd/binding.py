@@ -54,7 +54,7 @@ class SeerEvictParams(ctypes.Structure):
 
 class SeerReserveParams(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
-                ("n_tokens", ctypes.c_int32)]
+                ("n_tokens", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
 class SeerAppendParams(ctypes.Structure):
@@ -66,6 +66,7 @@ class SeerAppendParams(ctypes.Structure):
 
 SEER_F32, SEER_BF16 = 0, 1
 SEER_MAX_ALTERNATIVES = 32
+SEER_RESERVE_OWN_PAGES = 1
 SEER_ATTN_GENERAL_KERNEL = 1
 SEER_ATTN_FIXED_SPLIT = 2
 SEER_ATTN_STREAM_ONLY = 4
@@ -700,12 +701,13 @@ def seer_kv_reserve_workspace(params: SeerReserveParams) -> int:
 
 
 def seer_kv_reserve(block_table: torch.Tensor, pages_held: torch.Tensor, page_refs: torch.Tensor, ctx_len: torch.Tensor, n_new: torch.Tensor,
-                    n_tokens: int, page_size: int, *, share_from: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None,
+                    n_tokens: int, page_size: int, *, share_from: Optional[torch.Tensor] = None, tree_mask: Optional[torch.Tensor] = None, own_pages: bool = False,
                     out: Optional[Tuple[torch.Tensor, ...]] = None, status: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Pages for n_new [B] tokens (-1: the request is over) behind the ctx_len [B] positions of every request, in place in block_table
     [B,max_pages], pages_held [B] and page_refs [num_pages]; share_from [B]: row whose leading pages a starting request takes over.  All int32 on
-    the device; tree_mask [n_tokens] int64 (the uint64 ancestor bits).  Returns (step_len [B], first_token [B+1], slot [n_tokens],
+    the device; tree_mask [n_tokens] int64 (the uint64 ancestor bits).  A row's new tokens must not begin inside a page that another row holds too;
+    own_pages: such tokens get no slot (-1) and raise status bit 32.  Returns (step_len [B], first_token [B+1], slot [n_tokens],
     position [n_tokens]), all int32; `out`: such a tuple to write to."""
     lib = load_library()
     for value, name in ((n_tokens, "n_tokens"), (page_size, "page_size")):
@@ -714,7 +716,7 @@ def seer_kv_reserve(block_table: torch.Tensor, pages_held: torch.Tensor, page_re
     if block_table.dim() != 2 or page_refs.dim() != 1:
         raise ValueError("want block_table [B,max_pages] and page_refs [num_pages]")
     B, max_pages = block_table.shape
-    p = SeerReserveParams(B, int(page_size), page_refs.shape[0], max_pages, int(n_tokens))
+    p = SeerReserveParams(B, int(page_size), page_refs.shape[0], max_pages, int(n_tokens), SEER_RESERVE_OWN_PAGES if own_pages else 0)
     ref, scratch = ctypes.byref(p), 0
     if workspace is None:
         scratch = (int(lib.seer_kv_reserve_workspace(ref)) + 255) // 256 * 64 or 64        # (in int32)

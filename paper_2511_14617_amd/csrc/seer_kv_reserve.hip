@@ -423,12 +423,30 @@ __global__ __launch_bounds__(kThreads) void reserve_give(ReserveArgs a, int toke
     raise(a, error);
 }
 
+// SEER_RESERVE_OWN_PAGES: slots in pages that more than one row holds are taken back.  In a launch of its own, since only behind the others a count is what it stays (shared
+// pages of rows that got nothing are counted down again last), so that the result depends on nothing else.  64 rows of 9 tokens 12.9 -> 15.3 us, 64 whole prompts 19.7 -> 23.5:
+// what shares no page that way does without.
+__global__ __launch_bounds__(kThreads) void reserve_own_pages(ReserveArgs a) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+    if (i >= a.n_tokens) return;
+    const int slot = a.slot[i];
+    if (slot < 0 || a.refs[reserve_page(a, slot)] <= 1) return;
+    a.slot[i] = -1, a.position[i] = -1;
+    raise(a, 32);
+}
+static hipError_t launch_own_pages(const seer_reserve_params& p, const ReserveArgs& a, hipStream_t stream) {
+    if (!(p.flags & SEER_RESERVE_OWN_PAGES) || p.n_tokens == 0) return hipSuccess;
+    hipLaunchKernelGGL(reserve_own_pages, dim3((p.n_tokens + kThreads - 1) / kThreads), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
 static int check_reserve_params(const seer_reserve_params* p) {
     if (!p) return SEER_EINVAL;
     if (p->B < 0 || p->page_size < 1 || p->num_pages < 1 || p->max_pages_per_seq < 1 || p->n_tokens < 0) return SEER_EINVAL;
+    if (p->flags & ~SEER_RESERVE_OWN_PAGES) return SEER_EINVAL;
     if (p->B > kReserveMaxB || p->num_pages > 1 << 30 || static_cast<int64_t>(p->num_pages) * p->page_size > 0x7fffffffLL || p->n_tokens > 0x7fffffff - (1 << 20)) return SEER_ESHAPE;
     if (static_cast<int64_t>(p->max_pages_per_seq) * p->page_size > 0x7fffffffLL) return SEER_ESHAPE;
     return SEER_OK;
@@ -490,7 +508,8 @@ extern "C" int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     if (seer::reserve_is_small(*p)) {
         hipLaunchKernelGGL(seer::reserve_small, dim3(1), dim3(seer::kSmallThreads), 0, stream, a);
-        const hipError_t err = hipGetLastError();
+        hipError_t err = hipGetLastError();
+        if (err == hipSuccess) err = seer::launch_own_pages(*p, a, stream);
         return err == hipSuccess ? SEER_OK : static_cast<int>(err);
     }
     char* ws = static_cast<char*>(workspace);
@@ -506,5 +525,6 @@ extern "C" int seer_kv_reserve(const seer_reserve_params* p, const int32_t* ctx_
     if (err != hipSuccess) return static_cast<int>(err);
     hipLaunchKernelGGL(seer::reserve_give, dim3(token_blocks + row_blocks), dim3(seer::kThreads), 0, stream, a, token_blocks);
     err = hipGetLastError();
+    if (err == hipSuccess) err = seer::launch_own_pages(*p, a, stream);
     return err == hipSuccess ? SEER_OK : static_cast<int>(err);
 }
