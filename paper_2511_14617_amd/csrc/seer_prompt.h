@@ -24,9 +24,9 @@ constexpr int kPromptThreads = 256, kMostPromptThreads = 512;
 // The exponent reference of a row that has seen no finite score: the lowest float, which no finite score is below.  Every difference of references is then a
 // number or -inf, and a row that stays without a score asks for no rescaling.
 constexpr float kNoScore = -3.402823466e38f;
-// Measured with 128 | 256 | 512 positions a stretch: 8 single tokens behind 2048 positions, 8/1 heads, 32.4 | 26.2 | 27.2 us, one prompt of 900 34.5 | 31.1 | 29.1, short
-// requests over the latent 30.9 | 31.3 | 41.7; large calls do not notice.  Row tiles left whole up to 128 | 512 | 1024: eight prompts of 17 .. 300
-// tokens 22.7 | 18.6 | 18.6, the single tokens 26.3 | 26.2 | 36.5, short requests over the latent 48.6 | 31.3 | 31.3, 32 prompts of 600 61.5 | 61.4 | 57.6.
+// Measured with 128 | 256 | 512 positions a stretch: 8 single tokens behind 2048 positions, 8/1 heads, 30.7 | 26.3 | 27.7 us, 16 behind 4096 45.5 | 36.6 | 34.0, one prompt of 900
+// 33.4 | 31.2 | 28.9, the 8 single tokens over the latent on 16 heads 44.8 | 43.2 | 54.0; large calls do not notice.  Row tiles left whole up to 128 | 512 | 1024: eight prompts of
+// 17 .. 300 tokens 21.7 | 16.8 | 16.9, the single tokens 26.3 | 26.3 | 36.7, over the latent 43.4 | 43.2 | 77.3, 32 prompts of 600 62.1 | 53.4 | 52.9, one of 900 25.3 | 31.2 | 26.7.
 constexpr int kMinStretch = 256;       // positions per head of the group
 constexpr int kWholePositions = 512;
 
@@ -163,10 +163,19 @@ __device__ __forceinline__ int64_t stretch_begin(const PromptPlan& p, int w) {
     return each * w + rest * w / p.W;
 }
 
-// The line, by all threads of a workgroup (each looks at ceil(B / threads) requests behind one another), and where on it stretch w
-// begins and ends: the row tiles there.  False: there is no stretch w.  No barrier behind it.
+// The stretch of workgroup `block`, of W in use; -1: none.  Neighbouring stretches read the same positions: one XCD (ids are dealt round-robin to eight) takes
+// an eighth of the line.  An eighth of what is in use, not of the launch: with wide block tables the host cannot see how little there is to do (8 single tokens behind
+// 2048 positions, 8/1 heads, a table for 32 768: of 512 workgroups 73 have a stretch, by eighths of the launch on two XCDs 32.6 us, on all eight 26.3; eight prompts of 17 .. 300 18.4 | 16.8).
+constexpr int kXcds = 8;
+__host__ __device__ constexpr int stretch_of(int block, int W) {
+    const int xcd = block % kXcds, w = xcd * W / kXcds + block / kXcds;
+    return w < (xcd + 1) * W / kXcds ? w : -1;
+}
+
+// The line, by all threads of a workgroup (each looks at ceil(B / threads) requests behind one another), the workgroup's stretch w, and where on it
+// that begins and ends: the row tiles there.  False: it has no stretch.  No barrier behind it.
 template <int THREADS>
-__device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, int w, PromptPlan& p, int64_t (&x)[2], PromptTile (&t)[2], int& error) {
+__device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, int& w, PromptPlan& p, int64_t (&x)[2], PromptTile (&t)[2], int& error) {
     const int per = (a.B + THREADS - 1) / THREADS, b0 = threadIdx.x * per, b1 = min(b0 + per, a.B);
     int64_t n = 0, all;
     for (int b = b0; b < b1; ++b) n += prompt_tokens(a, b);
@@ -183,10 +192,14 @@ __device__ __forceinline__ bool prompt_plan(const PromptArgs& a, PromptLds& s, i
     const int64_t mine = prompt_before<THREADS>(mine_cost, s.sums[1], p.total);
     const int64_t least = static_cast<int64_t>(a.G) * kMinStretch;
     const int64_t most = max((p.total + least - 1) / least, all_tiles);
-    p.W = static_cast<int>(most < a.W ? most : a.W);
+    p.W = __builtin_amdgcn_readfirstlane(static_cast<int>(most < a.W ? most : a.W));
     p.snap = least / 2;
     p.whole = static_cast<int64_t>(a.G) * (kWholePositions + a.tile_cost);
-    if (w >= p.W) return false;
+    // (of stretches that are not in use nothing is joined)
+    if (blockIdx.x == 0)
+        for (int i = p.W + static_cast<int>(threadIdx.x); i < a.W; i += THREADS) a.cuts[i] = PromptCut{0, 0, 0, 0};
+    w = __builtin_amdgcn_readfirstlane(stretch_of(static_cast<int>(blockIdx.x), p.W));
+    if (w < 0) return false;
     int ignored = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) {

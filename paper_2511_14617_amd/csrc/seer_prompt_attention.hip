@@ -119,10 +119,7 @@ void prompt_tile_kernel(PromptArgs a) {
     PromptLds& s_plan = *reinterpret_cast<PromptLds*>(lds);
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    // neighbouring stretches read the same positions: one XCD (ids are dealt round-robin to eight) takes an eighth of the line
-    const int w = (blockIdx.x & 7) * (a.W >> 3) + (blockIdx.x >> 3);
-
-    int error = 0;
+    int w, error = 0;
     PromptPlan plan;
     int64_t x, x_end;
     PromptTile t;
@@ -130,11 +127,8 @@ void prompt_tile_kernel(PromptArgs a) {
         int64_t at[2];
         PromptTile ends[2];
         const bool on = prompt_plan<WAVES * kWave>(a, s_plan, w, plan, at, ends, error);
-        if (w == 0 && error && a.status) atomicOr(a.status, error);
-        if (!on) {
-            if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
-            return;
-        }
+        if (blockIdx.x == 0 && error && a.status) atomicOr(a.status, error);
+        if (!on) return;
         x = moved_cut(plan, ends[0], at[0]);
         x_end = moved_cut(plan, ends[1], at[1]);
         t = ends[0];
@@ -142,6 +136,8 @@ void prompt_tile_kernel(PromptArgs a) {
         if (x_end > ends[1].begin && x_end < ends[1].begin + ends[1].cost && ends[1].begin >= x && !ends[1].r.bad)
             cut = PromptCut{ends[1].b, ends[1].kvh, ends[1].i, pieces_of(plan, ends[1], w)};
         if (tid == 0) a.cuts[w] = cut;
+        // (w is wanted next where a partial result is stored: in a vector register; in a scalar one it takes others' place through the tiles, 0.5 % of the time)
+        asm volatile("" : "+v"(w));
     }
     bool bad_page = false;
     // ANY_PAGE: window of page ids: request, first logical page; lane l holds the (clamped) id of page win + l.
@@ -561,7 +557,7 @@ void prompt_tile_kernel(PromptArgs a) {
             continue;
         }
         // a lane's registers as they are, so that a store takes 1 KB: see partial_at
-        const size_t slot = 2 * static_cast<size_t>(w) + (begins ? 1 : 0);
+        const size_t slot = 2 * static_cast<size_t>(__builtin_amdgcn_readfirstlane(w)) + (begins ? 1 : 0);
         if (lg == 0) {
             const size_t prow = slot * S::kRows + wave * 32 + ln;
             a.part_ml[2 * prow] = m_run, a.part_ml[2 * prow + 1] = l_tot;

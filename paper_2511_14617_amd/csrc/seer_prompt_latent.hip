@@ -34,8 +34,7 @@ void prompt_latent_kernel(PromptArgs a) {
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), ln = lane & 31, lg = lane >> 5, l16 = lane >> 4, p16 = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-    const int w = (blockIdx.x & 7) * (a.W >> 3) + (blockIdx.x >> 3);          // (see the kernel for separate pools)
-    int error = 0;
+    int w, error = 0;
     PromptPlan plan;
     int64_t x, x_end;
     PromptTile t;
@@ -43,11 +42,8 @@ void prompt_latent_kernel(PromptArgs a) {
         int64_t at[2];
         PromptTile ends[2];
         const bool on = prompt_plan<kPromptThreads>(a, s_plan, w, plan, at, ends, error);
-        if (w == 0 && error && a.status) atomicOr(a.status, error);
-        if (!on) {
-            if (tid == 0) a.cuts[w] = PromptCut{0, 0, 0, 0};
-            return;
-        }
+        if (blockIdx.x == 0 && error && a.status) atomicOr(a.status, error);
+        if (!on) return;
         x = moved_cut(plan, ends[0], at[0]);
         x_end = moved_cut(plan, ends[1], at[1]);
         t = ends[0];
