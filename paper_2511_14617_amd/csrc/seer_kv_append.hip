@@ -208,9 +208,11 @@ extern "C" int seer_kv_append(const seer_append_params* p, const void* q, const 
     a.jobs = (p->Hq + p->Hkv) * a.jobs_qk + (shared ? 0 : p->Hkv * a.jobs_v);
     auto reciprocal = [](int d) { return static_cast<uint32_t>(((uint64_t{1} << 32) + d - 1) / d); };     // (d = 1: not looked at)
     a.inv_qk = reciprocal(a.jobs_qk), a.inv_v = reciprocal(a.jobs_v);
-    // Small tokens are taken up to four at a time where there are enough of them, large ones shared by several workgroups, as long as a thread has its
-    // jobs in flight.  With one | two | four tokens: 16 384 tokens on 8/1 heads of 128 33.6 | 24.2 | 18.9 us (four taken), on 64/8 128.7 | 131.5 | 136.5 (one), 1500 on 64/8
-    // 11.6 | 12.8 | 13.8 (one); calls of a few hundred are alike.
+    // Tokens of fewer than 1024 jobs are taken two, of fewer than 512 four at a time where there are enough of them; large ones are shared by several workgroups, as long as a thread has
+    // its jobs in flight.  With one | two | four tokens, in us: 16 384 tokens on 8/1 heads of 128 (88 jobs) 33.6 | 24.1 | 18.2 (four taken), on 16/4 of 64 40.6 | 30.7 | 24.5 (four), on
+    // 20/4 of 128 (256) 55.6 | 52.6 | 52.5 (four), on 32/8 (448) 85.8 | 83.6 | 83.7 (four; neighbouring pairs, 768: 91.1 | 87.1 | 83.2, two), on 16/16 of 192 (896) 117.9 | 115.0 | 116.1 (two), on
+    // 40/8 with half of 128 rotated (704) 104.9 | 102.2 | 103.0 (two), on 64/8 (704) 129.7 | 131.6 | 136.7 (two, the one case here that loses by it); 2048 on 64/8 16.0 | 15.7 | 17.9; calls of a
+    // few hundred are alike.
     a.tokens = 1, a.parts = 1;
     while (a.tokens < seer::kAppendTokens && a.tokens * a.jobs < seer::kJobsWanted && p->n_tokens / (2 * a.tokens) >= seer::kManyBlocks) a.tokens *= 2;
     if (a.tokens == 1) a.parts = (a.jobs + 2 * seer::kJobsWanted - 1) / (2 * seer::kJobsWanted);
