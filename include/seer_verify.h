@@ -680,7 +680,8 @@ SEER_API size_t seer_prompt_attention_workspace(const seer_attn_params* p, int32
  * Causal attention of packed tokens over the paged cache.  Request b's tokens are its last n_b = first_token[b + 1] -
  * first_token[b] positions, their keys and values already in the cache; its i-th token sees positions 0 .. ctx_len[b] - n_b + i:
  *   out[first_token[b] + i, h, :] = softmax_j(scale * q[.., h, :] . K[j, h/G, :]) . V[j, h/G, :],
- * with scores, sums and outputs in fp32, rounded to bf16 once (nearest even); probabilities enter the product with V as bf16.
+ * with scores, sums and outputs in fp32, rounded to bf16 once (nearest even); probabilities enter the product with V as bf16 (and the sum that
+ * divides it is taken of the same rounded values).  A row whose scores are all -inf gives zeros.
  * Any mix of lengths: whole prompts, pieces of prompts behind a cached beginning, single tokens, requests without a token.
  * The result depends on the arguments only.  A key or value with a NaN or an infinity in a position that a token does not see does
  * not reach it; rows behind the last request's are left as they are.

@@ -11,8 +11,9 @@
 //   give    a thread per new token finds its row, its page, its slot; the thread of a page's first position writes the page's
 //           entries, so tables and references cost no pass of their own
 // Calls of up to kSmallPages pages, kSmallRows rows and some thousand tokens take one workgroup and one launch, in which a barrier separates the
-// phases and the pages' counts stay as bits in LDS: 64 rows of 9 tokens, 16 384 pages, 11.9 us.  Beyond that they are three launches, 6.3 + 5.0 + 5.3 us for
-// 512 rows and 327 680 pages, 10.6 + 5.5 + 6.3 for 64 whole prompts and a million pages (4 MB): each is a launch and three or four loads that wait for one another.
+// phases and the pages' counts stay as bits in LDS: 64 rows of 9 tokens, 16 384 pages, 12.3 us.  Beyond that they are three launches, 6.0 + 5.3 + 5.7 us for
+// 512 rows and 327 680 pages, 8.7 + 5.7 + 6.4 for 64 whole prompts and a million pages (4 MB; all medians): each is a launch and three or four loads that wait for
+// one another, and to release a row of 2048 pages is four rounds of 512 page ids, one behind the other, by the row's one wave.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

@@ -19,9 +19,10 @@
 // the time, vector instructions 47 %, LDS 30 % (0.15 % of it conflicts), at 1.79 GHz instead of 2.4, and changes that saved cycles lowered the clock by nearly
 // as much: without the exponentials the time is 1 % less, without tile loads 13 to 19, without the product with V 15; earlier K reads, loads in the shadow of the
 // scores' MFMAs, other shares of probabilities, wave priorities changed nothing.  Eight waves take 4 % more cycles (54 % busy) and half the loads, at 1.92 GHz.
-// Requests of one token are bound by HBM: 64 of 16 384 positions on
-// 8 KV heads read 4.8 TB/s, though 28 of the 32 rows of a wave and three of four waves have nothing to do (loads that stream past the
-// caches gain 4 % there and cost prompts 30 %, which share what they read: not used).
+// Requests of one token are bound by HBM where they are alone: 64 of 16 384 positions on 8 KV heads read 4.8 TB/s (loads that stream past the caches gain 4 % there and cost
+// prompts 30 %, which share what they read: not used).  A row tile costs its matrix work whether it has rows or not, though: one token on 32/8 heads has 4 rows, and the waves without
+// rows compute scores and products of zeros.  Beside a piece of a prompt that takes power from it: 2048 tokens behind 16 384 and 63 single tokens need 1.15 TFLOP, the kernel executes 1.73
+// (by its count of MFMAs), 0.6 of them for single tokens, at the 930 TFLOP/s that it reaches with prompts.
 //
 // Infinities and NaN: scores of positions that a row does not see are replaced by selection.  In the product with V a position's row is
 // multiplied into all query rows, so in tiles with masked positions V rows that hold an infinity or NaN are taken out and added to the rows that see
@@ -636,7 +637,8 @@ static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
 // ---------------------------------------------------------------------------
 // What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.  Measured, with 1 | 128 | 256 | 384 | 512:
 // heads of 64, 12 prompts of up to 6000 tokens 289 | 248 | 250 | 259 | 266 us; of 128, 16 prompts of up to 8192 4175 | 3499 | 3253 | 3297 | 3411 (256 rows a row tile, 128 | 256 | 384: 3643 | 3081 | 3131); of 256, four
-// of 4096 531 | 392 | 346 | 353 | 358; shared latent, four pieces of up to 2048 2269 | 1667 | 1498 | 1482 | 1491.
+// of 4096 531 | 392 | 346 | 353 | 358; shared latent, four pieces of up to 2048 2269 | 1667 | 1498 | 1482 | 1491.  Heads of 192 take what 128 and 256 take: four of 4096 on 16 heads 462 | 439 | 424 | 424
+// (128 | 256 | 384 | 512, a slower box: heads of 256 415 | 375 | 380 | 382 there), 12 of up to 6000 542 | 524 | 522 | 527.
 constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 384); }
 static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (!p) return SEER_EINVAL;
@@ -664,7 +666,8 @@ constexpr int prompt_waves_per_simd(int dqk) { return dqk <= 64 ? 3 : (dqk <= 19
 // Eight waves and 256 rows a workgroup, for heads of 128: half the tile loads.  Four | eight waves: 16 prompts of 256 .. 8192 tokens on 64/8 heads 3121 | 2999 us, one of 32 768
 // on 8/1 2065 | 1990, one of 16 384 on 64/8 4210 | 3973, four of 8192 on 16/16 1204 | 1150, 16 of 2048 on 32/8 681 | 666.  With few rows a request or few of all, coarse
 // row tiles cost more than that: 8 of 1024 on 32/8 105 | 113, four of 4096 on 16/16 335 | 340, one of 600 on 8/1 24.5 | 40, of 4096 62.6 | 64.6, one of 1024 on 64/8 47 | 52, single
-// tokens 902 | 1127.  (Heads of 64 and 256 hold three waves and one a SIMD, a tile of 192 components is no multiple of eight waves' loads.)
+// tokens 902 | 1127.  The host knows the rows and the requests, not which rows are padding and which requests have none: padding raises the average, requests without tokens lower it, and
+// either may call for the dearer form of the two, whose results are within the same bounds.  (Heads of 64 and 256 hold three waves and one a SIMD, a tile of 192 components is no multiple of eight waves' loads.)
 static bool prompt_has_eight_waves(const seer_attn_params& p, int32_t n_tokens) {
     const int64_t rows = static_cast<int64_t>(n_tokens) * p.Hq;
     return p.Dqk == 128 && p.page_size % 16 == 0 && rows >= kEightWavesRows && rows / p.Hkv >= kEightWavesRequest * static_cast<int64_t>(p.B);
