@@ -638,7 +638,7 @@ static hipError_t launch_prompt(const PromptArgs& a, hipStream_t stream) {
 // What a row tile costs beside its positions -- queries, first loads, masked tiles, output -- in positions.  Measured, with 1 | 128 | 256 | 384 | 512:
 // heads of 64, 12 prompts of up to 6000 tokens 289 | 248 | 250 | 259 | 266 us; of 128, 16 prompts of up to 8192 4175 | 3499 | 3253 | 3297 | 3411 (256 rows a row tile, 128 | 256 | 384: 3643 | 3081 | 3131); of 256, four
 // of 4096 531 | 392 | 346 | 353 | 358; shared latent, four pieces of up to 2048 2269 | 1667 | 1498 | 1482 | 1491.  Heads of 192 take what 128 and 256 take: four of 4096 on 16 heads 462 | 439 | 424 | 424
-// (128 | 256 | 384 | 512, a slower box: heads of 256 415 | 375 | 380 | 382 there), 12 of up to 6000 542 | 524 | 522 | 527.
+// (128 | 256 | 384 | 512, a slower card: heads of 256 415 | 375 | 380 | 382 there), 12 of up to 6000 542 | 524 | 522 | 527.
 constexpr int prompt_tile_cost(int dqk) { return dqk <= 64 ? 128 : (dqk <= 256 ? 256 : 384); }
 static int check_prompt_params(const seer_attn_params* p, int32_t n_tokens) {
     if (!p) return SEER_EINVAL;
